@@ -37,7 +37,9 @@ EXPORTED = ("rafiki_ensemble_create", "rafiki_ensemble_infer", "rafiki_ensemble_
             "rafiki_ensemble_serve_rl",
             "rafiki_rl_create", "rafiki_rl_destroy", "rafiki_rl_info", "rafiki_rl_get_params", "rafiki_rl_set_params",
             "rafiki_rl_forward", "rafiki_rl_gradient", "rafiki_rl_adam_step", "rafiki_rl_run_episode",
-            "rafiki_rl_train", "rafiki_last_error")
+            "rafiki_rl_train", "rafiki_combine_workspace", "rafiki_combine_sample", "rafiki_combine_topk",
+            "rafiki_distill_loss", "rafiki_quantize_rows_i8", "rafiki_fc_i8", "rafiki_fc_i8_workspace",
+            "rafiki_last_error")
 KERNEL_CLASSES = ("conv_mfma", "splitk_reduce", "conv_f32", "stage", "pool", "embed", "concat", "combine", "vote",
                   "fused_net", "tap_table")
 
@@ -169,6 +171,14 @@ def load_library(path: str = LIB_PATH):
                                                        P(RafikiGreedyPolicy), C.c_uint32, C.c_void_p, C.c_void_p,
                                                        P(C.c_int64), P(RafikiDispatch), C.c_int64, P(C.c_int64),
                                                        C.c_void_p]
+    L, V, I, F = C.c_longlong, C.c_void_p, C.c_int, C.c_float
+    lib.rafiki_combine_workspace.argtypes = [I, I, I, P(L)]
+    lib.rafiki_combine_sample.argtypes = [V, I, L, L, I, I, I] + [V] * 8 + [L, V]
+    lib.rafiki_combine_topk.argtypes = [V, I, L, L, I, I, I, F, I, V, V, V, L, V]
+    lib.rafiki_distill_loss.argtypes = [V, I, L, I, I, V, V, I, F, I, V, V, V, L, V]
+    lib.rafiki_quantize_rows_i8.argtypes = [V, I, L, I, I, V, L, V, V]
+    lib.rafiki_fc_i8.argtypes = [V, L, V, V, L, V, V, I, I, I, I, V, I, L, V, L, V]
+    lib.rafiki_fc_i8_workspace.argtypes = [I, I, I, P(L)]
     lib.rafiki_last_error.restype = C.c_char_p
     for name in EXPORTED[:-1]:
         getattr(lib, name).restype = C.c_int
@@ -467,6 +477,177 @@ def global_avgpool_nhwc_bf16(x, y, stream=None):
     _expect(x, (n, h, w, c), torch.bfloat16, "x")
     _expect(y, (n, c), torch.bfloat16, "y")
     _check(load_library().rafiki_global_avgpool_nhwc_bf16(_ptr(x), _ptr(y), n, h, w, c, _stream(stream)))
+
+
+# ---------------------------------------------------------------- answers over a vocabulary
+
+def _dtype_code(t, name):
+    """RAFIKI_FP32 or RAFIKI_BF16 of a device tensor."""
+    import torch
+    if t.is_cuda and t.dtype == torch.float32:
+        return RAFIKI_FP32
+    if t.is_cuda and t.dtype == torch.bfloat16:
+        return RAFIKI_BF16
+    raise ValueError(f"{name}: expected a device tensor of float32 or bfloat16, got {t.dtype} on {t.device}")
+
+
+def _rows(t, name):
+    """Distance between the rows of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name}: expected a matrix with contiguous rows, got {tuple(t.shape)} with strides {t.stride()}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _same_device(first, *others):
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"tensors on {first.device} and {t.device}")
+
+
+def _call(first, stream, need, workspace, fn, *args):
+    """Calls a C function on the device of tensor ``first`` and on ``stream`` (None: the current stream of
+    that device), with a workspace of ``need`` bytes where it takes one (need None: it does not).  A workspace
+    that is not given is taken from torch's allocator for the time of the work."""
+    import torch
+    if torch.cuda.current_device() != first.device.index:
+        with torch.cuda.device(first.device):
+            return _call(first, stream, need, workspace, fn, *args)
+    if not isinstance(stream, (int, type(None))) and stream.device != first.device:
+        raise ValueError(f"stream of {stream.device}, tensors on {first.device}")
+    handle = _stream(stream)
+    if need is None:
+        return _check(fn(*args, handle))
+    if workspace is not None:
+        if not workspace.is_cuda or not workspace.is_contiguous():
+            raise ValueError("workspace: expected a contiguous device tensor")
+        _same_device(first, workspace)
+    elif need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=first.device)
+        if stream is not None:          # allocated for the current stream: kept until `stream` has passed
+            workspace.record_stream(torch.cuda.ExternalStream(handle, device=first.device))
+    return _check(fn(*args, _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                     handle))
+
+
+def _model_rows(logits):
+    """[S, n, C] (or [n, C]: one model) with contiguous rows -> (S, n, C, ld_model, ld_row)."""
+    if logits.dim() == 2:
+        logits = logits.unsqueeze(0)
+    if logits.dim() != 3 or (logits.stride(2) != 1 and logits.shape[2] > 1):
+        raise ValueError(f"logits: expected [S, n, C] or [n, C] with contiguous rows, got {tuple(logits.shape)} with "
+                         f"strides {logits.stride()}")
+    return (*logits.shape, logits.stride(0), logits.stride(1))
+
+
+def combine_workspace(n_models: int, n: int, n_classes: int) -> int:
+    """Bytes of workspace of combine_sample and combine_topk."""
+    b = C.c_longlong()
+    _check(load_library().rafiki_combine_workspace(n_models, n, n_classes, C.byref(b)))
+    return b.value
+
+
+def combine_sample(logits, uniform, out_labels, out_probs, temperature=None, top_k=None, top_p=None, min_p=None,
+                   workspace=None, stream=None):
+    """Draw one class per row from the ensemble's mean softmax: logits [S, n, C] (or [n, C]) fp32 or bf16 with
+    any row and model stride; uniform [n] in [0, 1), temperature, top_p, min_p fp32 [n], top_k int32 [n] (None:
+    off) -> labels int32 [n] (-1: no distribution) and their probabilities fp32 [n]."""
+    import torch
+    code = _dtype_code(logits, "logits")
+    S, n, nc, ld_model, ld_row = _model_rows(logits)
+    for t, dt, name in ((uniform, torch.float32, "uniform"), (temperature, torch.float32, "temperature"),
+                        (top_k, torch.int32, "top_k"), (top_p, torch.float32, "top_p"),
+                        (min_p, torch.float32, "min_p"), (out_labels, torch.int32, "labels"),
+                        (out_probs, torch.float32, "probabilities")):
+        if t is not None:
+            _expect(t, (n,), dt, name)
+    _same_device(logits, uniform, temperature, top_k, top_p, min_p, out_labels, out_probs)
+    _call(logits, stream, combine_workspace(S, n, nc), workspace, load_library().rafiki_combine_sample,
+          _ptr(logits), code, ld_model, ld_row, S, n, nc, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
+          _ptr(uniform), _ptr(out_labels), _ptr(out_probs))
+
+
+def combine_topk(logits, out_labels, out_logp, temperature: float = 1.0, workspace=None, stream=None):
+    """The k best classes of the ensemble's mean softmax, best first, and their log-probabilities: logits as in
+    combine_sample -> labels int32 [n, k], logp fp32 [n, k] (-1 and -inf past the last class with a probability)."""
+    import torch
+    code = _dtype_code(logits, "logits")
+    S, n, nc, ld_model, ld_row = _model_rows(logits)
+    k = out_labels.shape[-1]
+    _expect(out_labels, (n, k), torch.int32, "labels")
+    _expect(out_logp, (n, k), torch.float32, "log-probabilities")
+    _same_device(logits, out_labels, out_logp)
+    _call(logits, stream, combine_workspace(S, n, nc), workspace, load_library().rafiki_combine_topk,
+          _ptr(logits), code, ld_model, ld_row, S, n, nc, temperature, k, _ptr(out_labels), _ptr(out_logp))
+
+
+def distill_loss(logits, teacher_labels, teacher_logp, out_loss=None, grad_logits=None, grad_loss=None,
+                 temperature: float = 1.0, rest: bool = False, stream=None):
+    """Distillation loss fp32 [n] of the student's logits [n, C] (fp32 or bf16) against a teacher's top k (labels
+    int32 [n, k], logp fp32 [n, k], as combine_topk gives them at the same temperature) and, in grad_logits, its
+    gradient times grad_loss [n] (None: 1).  Either output may be None."""
+    import torch
+    code = _dtype_code(logits, "logits")
+    ld_row = _rows(logits, "logits")
+    n, nc = logits.shape
+    k = teacher_labels.shape[-1]
+    _expect(teacher_labels, (n, k), torch.int32, "teacher_labels")
+    _expect(teacher_logp, (n, k), torch.float32, "teacher_logp")
+    for t, name in ((out_loss, "loss"), (grad_loss, "grad_loss")):
+        if t is not None:
+            _expect(t, (n,), torch.float32, name)
+    ld_grad = 0
+    if grad_logits is not None:
+        if grad_logits.shape != logits.shape or grad_logits.dtype != logits.dtype:
+            raise ValueError("grad_logits: expected the shape and dtype of the logits")
+        ld_grad = _rows(grad_logits, "grad_logits")
+    _same_device(logits, teacher_labels, teacher_logp, out_loss, grad_logits, grad_loss)
+    _call(logits, stream, None, None, load_library().rafiki_distill_loss, _ptr(logits), code, ld_row, n, nc,
+          _ptr(teacher_labels), _ptr(teacher_logp), k, temperature, 1 if rest else 0, _ptr(grad_loss), _ptr(out_loss),
+          _ptr(grad_logits), ld_grad)
+
+
+def quantize_rows_i8(x, q, scale, stream=None):
+    """Rows of x [n, c] (fp32 or bf16) in 8 bits: q int8 [n, c] and scale fp32 [n] = max |x| / 127."""
+    import torch
+    code = _dtype_code(x, "x")
+    ld_x, ld_q = _rows(x, "x"), _rows(q, "q")
+    if q.shape != x.shape or q.dtype != torch.int8:
+        raise ValueError("q: expected int8 of the shape of x")
+    _expect(scale, (x.shape[0],), torch.float32, "scale")
+    _same_device(x, q, scale)
+    _call(x, stream, None, None, load_library().rafiki_quantize_rows_i8, _ptr(x), code, ld_x, *x.shape, _ptr(q), ld_q,
+          _ptr(scale))
+
+
+def fc_i8_workspace(n: int, c_in: int, c_out: int) -> int:
+    """Bytes of workspace of fc_i8."""
+    b = C.c_longlong()
+    _check(load_library().rafiki_fc_i8_workspace(n, c_in, c_out, C.byref(b)))
+    return b.value
+
+
+def fc_i8(x, x_scale, w, w_scale, y, bias=None, relu: bool = False, workspace=None, stream=None):
+    """FC layer in 8 bits: y [n, c_out] (fp32 or bf16) = act(x_scale w_scale (x w^T) + bias) for int8 x [n, c_in]
+    and w [c_out, c_in], whose rows start on 16-byte boundaries (a view of a padded matrix where c_in is no
+    multiple of 16)."""
+    import torch
+    code = _dtype_code(y, "y")
+    n, c_in = x.shape
+    c_out = w.shape[0]
+    ld_x, ld_w, ld_y = _rows(x, "x"), _rows(w, "w"), _rows(y, "y")
+    if x.dtype != torch.int8 or w.dtype != torch.int8 or w.shape[1] != c_in or y.shape != (n, c_out):
+        raise ValueError("expected int8 x [n, c_in], int8 w [c_out, c_in] and y [n, c_out]")
+    for t, ld, name in ((x, ld_x, "x"), (w, ld_w, "w")):     # rows are read up to a multiple of 16
+        end = t.storage_offset() + (t.shape[0] - 1) * ld + (c_in + 15) // 16 * 16
+        if end > t.untyped_storage().nbytes():
+            raise ValueError(f"{name}: the last row is not readable up to the next multiple of 16")
+    _expect(x_scale, (n,), torch.float32, "x_scale")
+    _expect(w_scale, (c_out,), torch.float32, "w_scale")
+    if bias is not None:
+        _expect(bias, (c_out,), torch.float32, "bias")
+    _same_device(x, x_scale, w, w_scale, y, bias)
+    _call(y, stream, fc_i8_workspace(n, c_in, c_out), workspace, load_library().rafiki_fc_i8, _ptr(x), ld_x,
+          _ptr(x_scale), _ptr(w), ld_w, _ptr(w_scale), _ptr(bias), n, c_in, c_out, 1 if relu else 0, _ptr(y), code, ld_y)
 
 
 def tile_configs():

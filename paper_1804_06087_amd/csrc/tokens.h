@@ -1,0 +1,73 @@
+// Internal interface of the vocabulary operators (rafiki_tokens.h): launch arguments.
+#pragma once
+#include "kernels.h"
+
+namespace rafiki {
+
+constexpr int kMaxTokenModels = 32;
+constexpr int kMaxTokenClasses = 1 << 20;
+constexpr int kMaxTokenK = 1024;
+// Classes of one statistics group: 64 lanes of one wave, 4 classes each.
+constexpr int kGroupClasses = 256;
+
+// A group's largest logit of one model and its sum of exp((z - max) / T), in the workspace as
+// [row][model][group].  top: NaN where the group holds a NaN.
+struct GroupStat {
+  double sum;
+  float top;
+  float pad;
+};
+
+struct TokenArgs {
+  const void* logits;
+  long long ld_model, ld_row;
+  int S, n, C, groups;
+  const float* temperature;   // [n] or null (then t_all)
+  float t_all;
+  GroupStat* stats;
+  int32_t* labels;
+  float* out;                 // probabilities [n] / log-probabilities [n][k]
+  // sample
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* uniform;
+  // topk
+  int k;
+};
+
+struct DistillArgs {
+  const void* logits;
+  long long ld_row;
+  int n, C, k;
+  const int32_t* labels;
+  const float* logp;
+  float t;
+  int rest;
+  const float* grad_loss;
+  float* loss;
+  void* grad;
+  long long ld_grad;
+};
+
+struct FcI8Args {
+  const int8_t* x;
+  const int8_t* w;
+  long long ld_x, ld_w, ld_y;
+  const float* sx;
+  const float* sw;
+  const float* bias;
+  int n, c_in, c_out, relu, out_bf16;
+  void* y;
+  int* partial;               // [splits][n][c_out] int32 sums (splits > 1)
+};
+
+hipError_t launch_sample(const TokenArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_topk(const TokenArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_quantize(const void* x, bool bf16, long long ld_x, int n, int c, int8_t* q, long long ld_q,
+                           float* scale, hipStream_t s);
+hipError_t launch_fc_i8(const FcI8Args& a, hipStream_t s);
+long long fc_i8_workspace_bytes(int n, int c_in, int c_out);
+
+}  // namespace rafiki

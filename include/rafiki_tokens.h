@@ -57,7 +57,8 @@ int rafiki_combine_workspace(int n_models, int n, int n_classes, long long* byte
  *                the last kept class, u < 0 or NaN: as 0).  Required.
  * out_labels int32 [n]; out_probs fp32 [n]: the label's p over the sum of all kept (1 for
  * T = 0).  A row without a distribution has label -1, and probability 0 if a mask left it
- * empty, NaN otherwise.  Comparisons are exact for sums held in units of 2^-62.
+ * empty, NaN otherwise.  Sums are held in units of 2^-62; that of a row of more than 1024 classes
+ * comes from partial sums in 64-bit floating point.
  * 1 <= n_models <= 32, n >= 1. */
 int rafiki_combine_sample(const void* logits, int dtype, long long ld_model, long long ld_row, int n_models, int n,
                           int n_classes, const float* temperature, const int32_t* top_k, const float* top_p,

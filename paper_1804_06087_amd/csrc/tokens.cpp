@@ -23,7 +23,7 @@ bool aligned_to(const void* p, int dtype) { return ((uintptr_t)p & (dtype == RAF
 bool known(int dtype) { return dtype == RAFIKI_FP32 || dtype == RAFIKI_BF16; }
 
 long long combine_bytes(int n_models, int n, int n_classes) {
-  return (long long)n_models * n * ((n_classes + kGroupClasses - 1) / kGroupClasses) * (long long)sizeof(GroupStat);
+  return (long long)n_models * n * token_stat_stride(n_classes);
 }
 
 int check_combine(const void* logits, int dtype, long long ld_model, long long ld_row, int n_models, int n,
@@ -50,9 +50,10 @@ TokenArgs token_args(const void* logits, long long ld_model, long long ld_row, i
   a.S = n_models;
   a.n = n;
   a.C = n_classes;
-  a.groups = (n_classes + kGroupClasses - 1) / kGroupClasses;
+  a.units = token_units(n_classes);
+  a.stat_stride = token_stat_stride(n_classes);
   a.t_all = 1.f;
-  a.stats = (GroupStat*)workspace;
+  a.stats = (char*)workspace;
   a.labels = labels;
   a.out = out;
   return a;

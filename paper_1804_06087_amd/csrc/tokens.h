@@ -7,24 +7,24 @@ namespace rafiki {
 constexpr int kMaxTokenModels = 32;
 constexpr int kMaxTokenClasses = 1 << 20;
 constexpr int kMaxTokenK = 1024;
-// Classes of one statistics group: 64 lanes of one wave, 4 classes each.
-constexpr int kGroupClasses = 256;
-
-// A group's largest logit of one model and its sum of exp((z - max) / T), in the workspace as
-// [row][model][group].  top: NaN where the group holds a NaN.
-struct GroupStat {
-  double sum;
-  float top;
-  float pad;
-};
+// Statistics of the logits in the workspace: per row and model, the maximum of every 64 classes
+// (16 a unit of 1024 classes; +inf throughout a unit that holds NaN or +inf), then every unit's
+// sum of 2^((z - its maximum) log2(e) / T).
+constexpr int kUnitClasses = 1024;
+constexpr int kUnitTops = kUnitClasses / 64;
+inline int token_units(int C) { return (C + kUnitClasses - 1) / kUnitClasses; }
+inline long long token_stat_stride(int C) {   // bytes, a multiple of 16
+  return ((long long)token_units(C) * (kUnitTops * 4 + 8) + 15) / 16 * 16;
+}
 
 struct TokenArgs {
   const void* logits;
   long long ld_model, ld_row;
-  int S, n, C, groups;
+  int S, n, C, units;
   const float* temperature;   // [n] or null (then t_all)
   float t_all;
-  GroupStat* stats;
+  char* stats;
+  long long stat_stride;
   int32_t* labels;
   float* out;                 // probabilities [n] / log-probabilities [n][k]
   // sample

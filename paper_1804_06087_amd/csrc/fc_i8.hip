@@ -59,50 +59,296 @@ __global__ __launch_bounds__(256) void quantize_kernel(const void* x, long long 
   }
 }
 
-__device__ __forceinline__ void store_out(const FcI8Args& a, int row, int o, int acc) {
-  float v = (float)acc * (a.sx[row] * a.sw[o]);
-  if (a.bias) v += a.bias[o];
-  if (a.relu && v < 0.f) v = 0.f;                            // NaN stays NaN
-  if (a.out_bf16) ((__bf16*)a.y)[row * a.ld_y + o] = (__bf16)v;
-  else ((float*)a.y)[row * a.ld_y + o] = v;
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) void lds_void;
+
+// s_waitcnt with only the vector-memory counter constrained (gfx9 encoding).
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
+}
+// Waits until at most `ahead` tiles of PER loads each are in flight.
+template <int PER, int MAX>
+__device__ __forceinline__ void wait_tiles(int ahead) {
+  if constexpr (MAX > 0) {
+    if (ahead >= MAX) {
+      wait_vmcnt<PER * MAX>();
+      return;
+    }
+    wait_tiles<PER, MAX - 1>(ahead);
+  } else {
+    wait_vmcnt<0>();
+  }
 }
 
-// 16 bytes of a row from k on; bytes behind c_in are 0.
-__device__ __forceinline__ i32x4 chunk16(const int8_t* p, int k, int c_in) {
-  i32x4 v = {0, 0, 0, 0};
-  if (k >= c_in) return v;
-  v = *(const i32x4*)(p + k);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int left = c_in - (k + 4 * i);                     // valid bytes from this word on
-    if (left <= 0) v[i] = 0;
-    else if (left < 4) v[i] &= (1 << (8 * left)) - 1;
-  }
-  return v;
+// Row r of an LDS tile (128 bytes, 8 chunks of 16) keeps chunk c in slot c ^ swz(r): 16 rows' equal
+// chunks then lie on 64 different banks.
+__device__ __forceinline__ int swz(int r) { return (r & 7) ^ ((r >> 3) & 1); }
+
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef __bf16 bf16x8_any __attribute__((ext_vector_type(8), aligned(2)));
+
+__device__ __forceinline__ float finish(int acc, float scale, float bias, int relu) {
+  float v = (float)acc * scale + bias;
+  return relu && v < 0.f ? 0.f : v;                          // NaN stays NaN
 }
 
-// A wave per 16 rows of x by 16 rows of w, fragments straight from memory.  v_mfma_i32_16x16x64_i8:
-// lane l holds 16 consecutive k (from 16 (l / 16)) of row l % 16 of either operand, and sums 4 (l / 16) .. + 3
-// of the first operand's rows for row l % 16 of the second.
-__global__ __launch_bounds__(256) void fc_i8_kernel(FcI8Args a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int tiles_o = (a.c_out + 63) / 64;
-  const int o0 = (int)(blockIdx.x % tiles_o) * 64 + wave * 16;
-  const int r0 = (int)(blockIdx.x / tiles_o) * 16;
-  if (o0 >= a.c_out) return;
-  const int xr = std::min(r0 + (lane & 15), a.n - 1), wr = std::min(o0 + (lane & 15), a.c_out - 1);
-  const int8_t* xp = a.x + xr * a.ld_x;
-  const int8_t* wp = a.w + wr * a.ld_w;
-  i32x4 acc = {0, 0, 0, 0};
-  for (int k = 16 * (lane >> 4); k - 16 * (lane >> 4) < a.c_in; k += 64) {
-    const i32x4 wv = chunk16(wp, k, a.c_in), xv = chunk16(xp, k, a.c_in);
-    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv, xv, acc, 0, 0, 0);
-  }
-  const int row = r0 + (lane & 15);
+// One wave's loads of a K tile: instruction j of wave w fills rows (j NW + w) 8 .. + 7, lane l slot l % 8 of
+// row l / 8 of those.  Rows and 16-byte chunks past the operands get an offset past the buffer's end,
+// for which the hardware writes zeros.
+template <int BM, int BN, int NW>
+struct TileLoader {
+  static constexpr int RA = BM / (8 * NW), RB = BN / (8 * NW), PER = RA + RB;
+  static constexpr unsigned kOut = 0x60000000u;              // past every tile (at most 2^30 bytes and a row)
+  static_assert(RA >= 1 && RB >= 1 && NW % 2 == 0, "tile shape");
+  __amdgpu_buffer_rsrc_t xr, wr;
+  unsigned xo[RA], wo[RB];
+  int chunk, wave, kt_begin, k16;
+
+  __device__ __forceinline__ void init(const FcI8Args& a, int m0, int n0, int wave_, int lane, int kt_begin_, int k16_) {
+    wave = wave_;
+    kt_begin = kt_begin_;
+    k16 = k16_;
+    const int lrow = lane >> 3;
+    chunk = (lane & 7) ^ lrow ^ (wave & 1);
+    const int x_rows = min(BM, a.n - m0), w_rows = min(BN, a.c_out - n0);
+    xr = __builtin_amdgcn_make_buffer_rsrc((void*)(a.x + m0 * a.ld_x), (short)0, (int)((x_rows - 1) * a.ld_x) + k16,
+                                           0x00020000);
+    wr = __builtin_amdgcn_make_buffer_rsrc((void*)(a.w + n0 * a.ld_w), (short)0, (int)((w_rows - 1) * a.ld_w) + k16,
+                                           0x00020000);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int o = o0 + 4 * (lane >> 4) + i;
-    if (row < a.n && o < a.c_out) store_out(a, row, o, acc[i]);
+    for (int j = 0; j < RA; ++j) {
+      const int r = (j * NW + wave) * 8 + lrow;
+      xo[j] = r < x_rows ? (unsigned)(r * a.ld_x) + chunk * 16 : kOut;
+    }
+#pragma unroll
+    for (int j = 0; j < RB; ++j) {
+      const int r = (j * NW + wave) * 8 + lrow;
+      wo[j] = r < w_rows ? (unsigned)(r * a.ld_w) + chunk * 16 : kOut;
+    }
+  }
+
+  // K tile t of this split into `base` (x's rows, then w's).
+  __device__ __forceinline__ void issue(int t, uint4* base) const {
+    const int k0 = (kt_begin + t) * 128;
+    const bool inside = k0 + chunk * 16 < k16;
+#pragma unroll
+    for (int j = 0; j < RA; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (lds_void*)(base + (j * NW + wave) * 64), 16, inside ? xo[j] : kOut,
+                                               k0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < RB; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void*)(base + BM * 8 + (j * NW + wave) * 64), 16,
+                                               inside ? wo[j] : kOut, k0, 0, 0);
+  }
+};
+
+// Tiled product: BM rows of x by BN rows of w per workgroup of WM x WN waves, K in tiles of 128 bytes
+// that go from memory to an LDS ring of STAGES tiles without registers (buffer loads ... lds);
+// v_mfma_i32_32x32x32_i8 with w as the first operand, so that a lane sums 4 neighbouring outputs of
+// one row.  Splits (grid y) each sum a range of K tiles; with more than one the
+// int32 sums go to the workspace and fc_i8_reduce_kernel joins them.
+template <int BM, int BN, int WM, int WN, int STAGES, int OCC>
+__global__ __launch_bounds__(WM * WN * 64, OCC) void fc_i8_tile_kernel(FcI8Args a) {
+  constexpr int NW = WM * WN;
+  constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
+  constexpr int PER = TileLoader<BM, BN, NW>::PER;
+  constexpr int STAGE = (BM + BN) * 8;                       // 16-byte chunks
+  static_assert(TM >= 1 && TN >= 1, "tile shape");
+  static_assert(STAGES >= 2 && STAGE * 16 * STAGES <= 160 * 1024, "LDS budget");
+  constexpr int CW = TN >= 2 ? 64 : 32;                      // outputs of a row staged at once
+  static_assert(NW * 32 * CW * 4 <= STAGE * 16 * STAGES, "epilogue staging fits in LDS");
+  __shared__ uint4 lds[STAGE * STAGES];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave % WM, wn = wave / WM;
+  // Workgroups are dealt round-robin to the 8 XCDs: each XCD takes a contiguous range of tiles, walked in
+  // bands of `band` row tiles, rows fastest, so that the tiles running together on one XCD share
+  // rows of x and of w in its L2.
+  const int G = gridDim.x, q = G >> 3, r8 = G & 7, xcd = blockIdx.x & 7, loc = blockIdx.x >> 3;
+  const int tile = (xcd < r8 ? xcd * (q + 1) : r8 * (q + 1) + (xcd - r8) * q) + loc;
+  const int tiles_m = (a.n + BM - 1) / BM, tiles_n = (a.c_out + BN - 1) / BN;
+  constexpr int kBand = 8;
+  const int band = tile / (kBand * tiles_n), in_band = tile - band * kBand * tiles_n;
+  const int rows = min(kBand, tiles_m - band * kBand);
+  const int m0 = (band * kBand + in_band % rows) * BM, n0 = in_band / rows * BN;
+
+  const int k16 = (a.c_in + 15) / 16 * 16, ktiles = (k16 + 127) / 128;
+  const int kt_begin = blockIdx.y * a.kt_per_split;
+  const int nk = min(a.kt_per_split, ktiles - kt_begin);
+
+  TileLoader<BM, BN, NW> loader;
+  loader.init(a, m0, n0, wave, lane, kt_begin, k16);
+  auto issue = [&](int t, int stage) { loader.issue(t, lds + stage * STAGE); };
+
+  i32x16 acc[TN][TM];
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+
+  const int frow = lane & 31, fk = lane >> 5;
+  auto frag = [&](const uint4* base, int r, int c) { return __builtin_bit_cast(i32x4, base[r * 8 + (c ^ swz(r))]); };
+  // Bytes of x behind c_in in the last K tile's last chunk become 0 (a barrier for all waves).
+  const int tail = a.c_in & 15;
+  auto clear_tail = [&](int t, uint4* tile_x) {
+    if (tail == 0 || kt_begin + t != ktiles - 1) return;
+    const int c = (a.c_in & 127) >> 4;
+    for (int r = threadIdx.x; r < BM; r += NW * 64) {
+      uint4& v = tile_x[r * 8 + (c ^ swz(r))];
+      uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int left = tail - 4 * i;
+        w[i] = left <= 0 ? 0u : left < 4 ? w[i] & ((1u << (8 * left)) - 1u) : w[i];
+      }
+      v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __syncthreads();
+  };
+
+  i32x4 xf[2][TM], wf[2][TN];
+  if (nk > 0) {
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s)
+      if (s < nk) issue(s, s);
+    wait_tiles<PER, STAGES - 1>(min(STAGES, nk) - 1);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    clear_tail(0, lds);
+#pragma unroll
+    for (int tm = 0; tm < TM; ++tm) xf[0][tm] = frag(lds, wm * WTM + tm * 32 + frow, fk);
+#pragma unroll
+    for (int tn = 0; tn < TN; ++tn) wf[0][tn] = frag(lds + BM * 8, wn * WTN + tn * 32 + frow, fk);
+  }
+  for (int kt = 0; kt < nk; ++kt) {
+    const int cur = kt % STAGES;
+    const uint4* As = lds + cur * STAGE;
+    const uint4* Bs = As + BM * 8;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int b = s & 1;
+      if (s < 3) {
+#pragma unroll
+        for (int tm = 0; tm < TM; ++tm) xf[b ^ 1][tm] = frag(As, wm * WTM + tm * 32 + frow, 2 * (s + 1) + fk);
+#pragma unroll
+        for (int tn = 0; tn < TN; ++tn) wf[b ^ 1][tn] = frag(Bs, wn * WTN + tn * 32 + frow, 2 * (s + 1) + fk);
+      }
+      __builtin_amdgcn_sched_barrier(0);                     // the next step's reads ahead of this one's products
+#pragma unroll
+      for (int tn = 0; tn < TN; ++tn)
+#pragma unroll
+        for (int tm = 0; tm < TM; ++tm)
+          acc[tn][tm] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[b][tn], xf[b][tm], acc[tn][tm], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (kt + 1 < nk) {
+      // tile kt's fragments are in registers; wait for tile kt + 1, then stage `cur` takes tile kt + STAGES
+      asm volatile("" ::: "memory");
+      wait_tiles<PER, STAGES - 2>(min(STAGES - 2, nk - 2 - kt));
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (kt + STAGES < nk) issue(kt + STAGES, cur);
+      uint4* An = lds + ((kt + 1) % STAGES) * STAGE;
+      clear_tail(kt + 1, An);
+#pragma unroll
+      for (int tm = 0; tm < TM; ++tm) xf[0][tm] = frag(An, wm * WTM + tm * 32 + frow, fk);
+#pragma unroll
+      for (int tn = 0; tn < TN; ++tn) wf[0][tn] = frag(An + BM * 8, wn * WTN + tn * 32 + frow, fk);
+    }
+  }
+
+  // ---- epilogue: each wave transposes 32 rows by CW outputs at a time through its own part of LDS (slots
+  // swizzled by the row), and lanes then hold 8 neighbouring outputs of a row: CW / 8 lanes write one run.
+  constexpr int OL = CW / 8, RP = 64 / OL;                   // lanes per row, rows per pass
+  __syncthreads();
+  int4* stg = (int4*)lds + wave * (32 * CW / 4);
+  const int oct = lane % OL, prow = lane / OL;
+#pragma unroll
+  for (int t0 = 0; t0 < TN; t0 += CW / 32) {
+    const int o = n0 + wn * WTN + t0 * 32 + oct * 8;
+    float sw[8], bias[8];
+    if (gridDim.y == 1) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int c = min(o + j, a.c_out - 1);
+        sw[j] = a.sw[c];
+        bias[j] = a.bias ? a.bias[c] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int tm = 0; tm < TM; ++tm) {
+#pragma unroll
+      for (int tn = 0; tn < CW / 32; ++tn)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const i32x16& v = acc[t0 + tn][tm];
+          stg[frow * (CW / 4) + ((tn * 8 + 2 * g + fk) ^ (frow & (CW / 4 - 1)))] =
+              make_int4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+        }
+      __builtin_amdgcn_s_waitcnt(0xC07F);                    // lgkmcnt(0): this wave's writes have landed
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int p = 0; p < 32; p += RP) {
+        const int r = p + prow, row = m0 + wm * WTM + tm * 32 + r;
+        const int4 lo = stg[r * (CW / 4) + ((2 * oct) ^ (r & (CW / 4 - 1)))];
+        const int4 hi = stg[r * (CW / 4) + ((2 * oct + 1) ^ (r & (CW / 4 - 1)))];
+        const int v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+        if (row >= a.n || o >= a.c_out) continue;
+        if (gridDim.y > 1) {
+          int* out = a.partial + ((long long)blockIdx.y * a.n + row) * a.c_out + o;
+          if (o + 8 <= a.c_out) {
+            *(i32x4_any*)out = i32x4_any{v[0], v[1], v[2], v[3]};
+            *(i32x4_any*)(out + 4) = i32x4_any{v[4], v[5], v[6], v[7]};
+          } else {
+            for (int j = 0; j < a.c_out - o; ++j) out[j] = v[j];
+          }
+          continue;
+        }
+        const float sx = a.sx[row];
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = finish(v[j], sx * sw[j], bias[j], a.relu);
+        const long long at = row * a.ld_y + o;
+        if (o + 8 <= a.c_out) {
+          if (a.out_bf16) {
+            bf16x8_any h;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) h[j] = (__bf16)f[j];
+            *(bf16x8_any*)((__bf16*)a.y + at) = h;
+          } else {
+            *(f32x4_any*)((float*)a.y + at) = f32x4_any{f[0], f[1], f[2], f[3]};
+            *(f32x4_any*)((float*)a.y + at + 4) = f32x4_any{f[4], f[5], f[6], f[7]};
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (o + j < a.c_out) {
+              if (a.out_bf16) ((__bf16*)a.y)[at + j] = (__bf16)f[j];
+              else ((float*)a.y)[at + j] = f[j];
+            }
+        }
+      }
+      __builtin_amdgcn_s_waitcnt(0xC07F);                    // reads done before the region is rewritten
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+}
+
+// Joins the splits' sums: a thread per output.
+__global__ __launch_bounds__(256) void fc_i8_reduce_kernel(FcI8Args a, int splits) {
+  const long long total = (long long)a.n * a.c_out;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
+    const int row = (int)(i / a.c_out), o = (int)(i - (long long)row * a.c_out);
+    int acc = 0;
+    for (int s = 0; s < splits; ++s) acc += a.partial[s * total + i];
+    const float v = finish(acc, a.sx[row] * a.sw[o], a.bias ? a.bias[o] : 0.f, a.relu);
+    if (a.out_bf16) ((__bf16*)a.y)[row * a.ld_y + o] = (__bf16)v;
+    else ((float*)a.y)[row * a.ld_y + o] = v;
   }
 }
 
@@ -116,12 +362,59 @@ hipError_t launch_quantize(const void* x, bool bf16, long long ld_x, int n, int 
   return hipGetLastError();
 }
 
-long long fc_i8_workspace_bytes(int, int, int) { return 0; }
+// The tile configurations, largest first.
+struct FcConfig {
+  int bm, bn, per_cu;        // workgroups that fit on a compute unit
+};
+constexpr FcConfig kConfigs[] = {{256, 256, 1}, {128, 128, 2}, {64, 128, 2}, {32, 128, 2}};
 
-hipError_t launch_fc_i8(const FcI8Args& a, hipStream_t s) {
-  const long long tiles = (long long)((a.c_out + 63) / 64) * ((a.n + 15) / 16);
-  if (tiles > (1 << 23)) return hipErrorInvalidValue;
-  launch(fc_i8_kernel, dim3((unsigned)tiles), dim3(256), s, a);
+struct FcPlan {
+  int cfg, splits, kt_per_split;
+};
+
+FcPlan plan_fc(int n, int c_in, int c_out) {
+  const int ktiles = (c_in + 127) / 128;
+  FcPlan best{0, 1, ktiles};
+  int cfg = n > 128 ? 0 : n > 64 ? 1 : n > 32 ? 2 : 3;
+  auto tiles = [&](int c) {
+    return (long long)((n + kConfigs[c].bm - 1) / kConfigs[c].bm) * ((c_out + kConfigs[c].bn - 1) / kConfigs[c].bn);
+  };
+  if (cfg == 0 && tiles(0) < 256) cfg = 1;
+  best.cfg = cfg;
+  const long long slots = 256 * kConfigs[cfg].per_cu, t = tiles(cfg);
+  int splits = (int)std::max<long long>(1, std::min<long long>(slots / t, ktiles / 4));
+  best.kt_per_split = (ktiles + splits - 1) / splits;
+  best.splits = (ktiles + best.kt_per_split - 1) / best.kt_per_split;
+  return best;
+}
+
+template <int BM, int BN, int WM, int WN, int STAGES, int OCC>
+hipError_t launch_tile(const FcI8Args& a, int splits, hipStream_t s) {
+  const long long tiles = (long long)((a.n + BM - 1) / BM) * ((a.c_out + BN - 1) / BN);
+  if (tiles > (1 << 22)) return hipErrorInvalidValue;
+  launch(fc_i8_tile_kernel<BM, BN, WM, WN, STAGES, OCC>, dim3((unsigned)tiles, splits), dim3(WM * WN * 64), s, a);
+  return hipGetLastError();
+}
+
+long long fc_i8_workspace_bytes(int n, int c_in, int c_out) {
+  const FcPlan p = plan_fc(n, c_in, c_out);
+  return p.splits > 1 ? (long long)p.splits * n * c_out * 4 : 0;
+}
+
+hipError_t launch_fc_i8(const FcI8Args& args, hipStream_t s) {
+  FcI8Args a = args;
+  const FcPlan p = plan_fc(a.n, a.c_in, a.c_out);
+  a.kt_per_split = p.kt_per_split;
+  hipError_t st;
+  switch (p.cfg) {
+    case 0: st = launch_tile<256, 256, 2, 4, 2, 2>(a, p.splits, s); break;
+    case 1: st = launch_tile<128, 128, 2, 2, 2, 2>(a, p.splits, s); break;
+    case 2: st = launch_tile<64, 128, 1, 4, 3, 2>(a, p.splits, s); break;
+    default: st = launch_tile<32, 128, 1, 4, 3, 2>(a, p.splits, s); break;
+  }
+  if (st != hipSuccess || p.splits == 1) return st;
+  const long long total = (long long)a.n * a.c_out;
+  launch(fc_i8_reduce_kernel, dim3((unsigned)std::min<long long>((total + 255) / 256, 1 << 16)), dim3(256), s, a, p.splits);
   return hipGetLastError();
 }
 

@@ -58,6 +58,7 @@ struct FcI8Args {
   const float* sw;
   const float* bias;
   int n, c_in, c_out, relu, out_bf16;
+  int kt_per_split;           // K tiles of 128 bytes per split
   void* y;
   int* partial;               // [splits][n][c_out] int32 sums (splits > 1)
 };

@@ -1,12 +1,17 @@
 // Distillation of a teacher's top classes into a student, loss and gradient (rafiki_tokens.h).
 //
-// With x = z / T, K the row's teacher classes and r the other classes, the row needs the sums of
-// exponentials of K and of r; then log p_j = x_j - lse and, for c outside K,
-//     dz_c = T g e^(x_c - lse_r) (Q p_r - q_r),
-// one exponential and one product per class; K's classes are written after the others.  Without
-// rest the split is not needed and dz_c = T g Q e^(x_c - lse).  Taking r's own maximum and sum
-// (K's classes are marked in a bitmap in LDS) keeps log p_r exact where p_r is small, which
-// 1 - sum p_j does not.
+// With y_c = z_c s, s = log2(e) / T, K the row's teacher classes and r the other classes:
+//     S_r = sum_{c not in K} 2^(y_c - y_r),  y_r their maximum,   S the same sum over all classes,
+//     p_c = 2^(y_c - y) / S,  p_r = S_r 2^(y_r - y) / S,
+//     dz_c = T g (Q p_c - q_c) in K,  T g (Q p_r - q_r) 2^(y_c - y_r) / S_r otherwise,
+// one power and one product per class outside K; K's classes are written after the others.  K's classes
+// are marked in a bitmap in LDS and left out of r's sum, which keeps p_r exact where it is small
+// (1 - sum p_j does not).  Without rest nothing is marked, r is all classes and q_r = 0.
+//
+// One workgroup per row, the row in its registers: the logits are read once and the gradient written
+// once, which is the floor.  Chunks of 16 bytes lie on 16-byte boundaries of the logits, so a row may
+// start anywhere.  Rows too long for the registers are read again for each pass (CH = 0), from the L2
+// or the memory-side cache.
 #include "tokens.h"
 
 #include <algorithm>
@@ -15,12 +20,17 @@ namespace rafiki {
 
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kWaves = kThreads / 64;
 constexpr float kRestMin = 0x1p-20f;
+constexpr float kLn2 = 0.693147180559945f, kLog2e = 1.44269504088896f;
+
+typedef unsigned long long u64;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+__device__ __forceinline__ float power2(float t) { return __builtin_amdgcn_exp2f(t); }
 
 template <bool BF16>
-__device__ __forceinline__ float student(const void* p, long long i) {
+__device__ __forceinline__ float element(const void* p, long long i) {
   if constexpr (BF16) return __uint_as_float((uint32_t)((const bf16_t*)p)[i] << 16);
   else return ((const float*)p)[i];
 }
@@ -32,144 +42,365 @@ __device__ __forceinline__ void put(void* p, long long i, float v) {
   else ((float*)p)[i] = v;
 }
 
-// A running maximum and the sum of exponentials below it.
-struct MaxSum {
-  float top, sum;
-  // A NaN in t makes the sum NaN (fmaxf drops it from the maximum).
-  __device__ __forceinline__ void join(float t, float s) {
-    const float m = fmaxf(top, t);
-    sum = sum * (top == m ? 1.f : expf(top - m)) + s * (t == m ? 1.f : expf(t - m));
-    top = m;
-  }
-};
-
-__device__ __forceinline__ MaxSum block_join(MaxSum v, MaxSum* waves) {
+// A 16-byte chunk of V values: unpacked, packed.
+template <bool BF16, int V>
+__device__ __forceinline__ void unpack(u32x4 q, float z[V]) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v.join(__shfl_xor(v.top, o, 64), __shfl_xor(v.sum, o, 64));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = waves[0];
-  for (int w = 1; w < kWaves; ++w) v.join(waves[w].top, waves[w].sum);
-  return v;
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (BF16) {
+      z[2 * j] = __uint_as_float(q[j] << 16);
+      z[2 * j + 1] = __uint_as_float(q[j] & 0xFFFF0000u);
+    } else {
+      z[j] = __uint_as_float(q[j]);
+    }
+  }
+}
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+template <bool BF16, int V>
+__device__ __forceinline__ u32x4 pack(const float z[V]) {
+  u32x4 q;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (BF16) q[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{z[2 * j], z[2 * j + 1]}, bf16x2));
+    else q[j] = __float_as_uint(z[j]);
+  }
+  return q;
 }
 
-__device__ __forceinline__ float block_add(float v, float* waves) {
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+__device__ __forceinline__ float wave_add(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0.f;
-  for (int w = 0; w < kWaves; ++w) v += waves[w];
   return v;
 }
 
-// One workgroup per row.  Thread j < k holds slot j; of the slots of one class the first holds
-// the class.
-template <bool BF16>
-__global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a) {
-  extern __shared__ uint32_t marks[];                       // rest: one bit per class
-  __shared__ MaxSum wave_ms[kWaves];
-  __shared__ float wave_f[kWaves];
+// The maximum as a reference for powers: an empty row has none and takes 0.
+__device__ __forceinline__ float reference(float top) { return top == -INFINITY ? 0.f : top; }
+
+// NT threads hold a row of up to NT CH + 2 chunks, the two edges among them (CH = 0: any length, not held).
+template <bool BF16, int NT, int CH, int OCC>
+__global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
+  constexpr int V = BF16 ? 8 : 4, NW = NT / 64;
+  extern __shared__ uint32_t marks[];                        // rest: bit c + shift is set for c in K
+  __shared__ float w_top[NW], w_member_top[NW], w_members[NW], w_q[NW], w_sum[NW], w_member_sum[NW], w_part[NW];
   __shared__ int ids[kMaxTokenK];
-  __shared__ float qs[kMaxTokenK];
-  const int tid = threadIdx.x;
-  const float inv_t = 1.f / a.t;
-  for (int row = blockIdx.x; row < a.n; row += gridDim.x) {
-    __syncthreads();
-    const long long base = row * a.ld_row, gbase = row * a.ld_grad;
-    const float g = a.grad_loss ? a.grad_loss[row] : 1.f;
-    int id = -1;
-    float t_logp = -INFINITY;
-    if (tid < a.k) {
-      id = a.labels[(long long)row * a.k + tid];
-      if ((unsigned)id >= (unsigned)a.C) id = -1;
-      if (id >= 0) t_logp = a.logp[(long long)row * a.k + tid];
-      ids[tid] = id;
-    }
-    // q of this slot
-    float q = expf(t_logp);
-    if (!a.rest) {
-      const MaxSum all = block_join(MaxSum{t_logp, id < 0 ? 0.f : t_logp == -INFINITY ? 0.f : 1.f}, wave_ms);
-      const bool any = !(all.top == -INFINITY && all.sum == 0.f);
-      if (!any) {                                            // no teacher: nothing to learn
-        if (a.loss && tid == 0) a.loss[row] = 0.f;
-        if (a.grad)
-          for (int c = tid; c < a.C; c += kThreads) put<BF16>(a.grad, gbase + c, 0.f);
-        continue;
+  __shared__ float slot_q[kMaxTokenK];                       // teacher_logp, then q of the slot
+  constexpr uint32_t kMasked = BF16 ? 0xFF80FF80u : 0xFF800000u;     // -inf in every place
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const float s = kLog2e / a.t;
+  const int row = a.row0 + blockIdx.x;
+  const float g = a.grad_loss ? a.grad_loss[row] : 1.f;
+  const long long base = row * a.ld_row, gbase = row * a.ld_grad;
+  const int shift = (int)((((uintptr_t)a.logits / (16 / V)) + base) & (V - 1));   // classes behind a boundary
+  const int chunks = (a.C + shift + V - 1) / V;
+  // Chunk c: classes c V - shift .. + V - 1, on a 16-byte boundary.  The first and the last may stand out of
+  // the row: thread 0 and thread 1 hold, beside the others, the row's first and last V classes instead (the
+  // edges), of which those that another chunk has too count there.  Gradients are the same from both.
+  const char* const x_row = (const char*)a.logits + (base - shift) * (16 / V);
+  char* const d_row = (char*)a.grad + (gbase - shift) * (16 / V);
+  const int edge_at = tid == 0 ? 0 : a.C - V;              // its first class, where C >= V
+  const bool has_edge = tid == 0 || (tid == 1 && chunks > 1);
+  // the edge's classes that count: a bit each (a row shorter than a chunk is thread 0's)
+  const uint32_t edge_own = a.C < V ? (tid == 0 ? (1u << a.C) - 1 : 0u)
+                            : tid == 0 ? (1u << (V - shift)) - 1
+                                       : ~0u << (chunks * V - shift - a.C) & ((1u << V) - 1);
+  auto load = [&](int i) {
+    return __builtin_nontemporal_load((const u32x4*)(x_row + (long long)i * NT * 16 + (unsigned)(tid + 1) * 16u));
+  };
+  auto store = [&](int i, const float d[V]) {
+    *(u32x4_any*)(d_row + (long long)i * NT * 16 + (unsigned)(tid + 1) * 16u) = pack<BF16, V>(d);
+  };
+  auto load_edge = [&]() {
+    u32x4 q = {kMasked, kMasked, kMasked, kMasked};
+    if (has_edge) {
+      if (a.C >= V) {
+        q = *(const u32x4_any*)(x_row + (shift + edge_at) * (16 / V));
+      } else {
+        float z[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) z[j] = tid == 0 && j < a.C ? element<BF16>(a.logits, base + j) : -INFINITY;
+        q = pack<BF16, V>(z);
       }
-      q = t_logp == -INFINITY ? 0.f : expf(t_logp - all.top) / all.sum;
     }
-    if (tid < a.k) qs[tid] = q;
-    if (a.rest)
-      for (int w = tid; w < (a.C + 31) / 32; w += kThreads) marks[w] = 0;
-    __syncthreads();
-    // slots of one class
-    bool first = id >= 0;
-    float q_class = 0.f;
-    if (id >= 0)
-      for (int j = 0; j < a.k; ++j)
-        if (ids[j] == id) {
-          if (j < tid) first = false;
-          q_class += qs[j];
-        }
-    if (a.rest && first) atomicOr(&marks[id >> 5], 1u << (id & 31));
-    __syncthreads();
-    const float x_member = first ? student<BF16>(a.logits, base + id) * inv_t : -INFINITY;
-    const int members = (int)block_add(first ? 1.f : 0.f, wave_f);
-    const float q_sum = block_add(first ? q_class : 0.f, wave_f);
-    // the sums of exponentials
-    MaxSum ms{-INFINITY, 0.f};
-    for (int c = tid; c < a.C; c += kThreads) {
-      if (a.rest && (marks[c >> 5] >> (c & 31) & 1)) continue;
-      const float x = student<BF16>(a.logits, base + c) * inv_t;
-      if (x != -INFINITY) ms.join(x, 1.f);
+    return q;
+  };
+  auto store_edge = [&](const float d[V]) {
+    if (has_edge && a.C >= V) {
+      *(u32x4_any*)(d_row + (shift + edge_at) * (16 / V)) = pack<BF16, V>(d);
+    } else if (tid == 0) {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (j < a.C) put<BF16>(a.grad, gbase + j, d[j]);
     }
-    ms = block_join(ms, wave_ms);
-    const float lse_r = ms.top + logf(ms.sum);               // rest = 0: of all classes
-    float lse = lse_r;
-    float q_r = 0.f;
-    if (a.rest) {
-      MaxSum k = block_join(MaxSum{x_member, x_member == -INFINITY ? 0.f : 1.f}, wave_ms);
-      k.join(ms.top, ms.sum);
-      lse = k.top + logf(k.sum);
-      q_r = 1.f - q_sum;
-      if (q_r < kRestMin || members == a.C) q_r = 0.f;
-    }
-    const float big_q = a.rest ? q_sum + q_r : q_sum;
-    float part = first && q_class != 0.f ? q_class * (logf(q_class) - (x_member - lse)) : 0.f;
-    part = block_add(part, wave_f);
-    const bool defined = lse > -INFINITY && lse < INFINITY;  // false for NaN too
-    if (a.loss && tid == 0) {
-      if (q_r > 0.f) part += q_r * (logf(q_r) - (lse_r - lse));
-      a.loss[row] = defined ? a.t * a.t * part : NAN;
-    }
-    if (!a.grad) continue;
-    const float scale = defined ? a.t * g : NAN;
-    if (g == 0.f) {
-      for (int c = tid; c < a.C; c += kThreads) put<BF16>(a.grad, gbase + c, 0.f);
-      continue;
-    }
-    const float p_r = a.rest ? expf(lse_r - lse) : 1.f;
-    const float factor = scale * (p_r == 0.f ? 0.f : big_q * p_r - q_r);   // NaN stays
-    for (int c = tid; c < a.C; c += kThreads) {
-      const float x = student<BF16>(a.logits, base + c) * inv_t;
-      put<BF16>(a.grad, gbase + c, x == -INFINITY && defined ? 0.f : factor * expf(x - lse_r));
-    }
-    __syncthreads();
-    if (first) put<BF16>(a.grad, gbase + id, scale * (big_q * expf(x_member - lse) - q_class));
+  };
+  auto zero_row = [&]() {
+    float d[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) d[j] = 0.f;
+    for (int i = 0; i * NT + tid + 1 < chunks - 1; ++i) store(i, d);
+    store_edge(d);
+  };
+  if (g == 0.f && !a.loss) {                               // of no weight: the row is not read
+    if (a.grad) zero_row();
+    return;
   }
+  u32x4 held[CH > 0 ? CH : 1], edge = load_edge();
+  if constexpr (CH > 0) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      held[i] = u32x4{kMasked, kMasked, kMasked, kMasked};
+      if (i * NT + tid + 1 < chunks - 1) held[i] = load(i);
+    }
+  }
+  // K's classes as -inf in the V classes whose first has bit `at` of the marks
+  auto without_members = [&](u32x4 q, int at) {
+    const u64 two = (u64)marks[(at >> 5) + 1] << 32 | marks[at >> 5];
+    const uint32_t m = (uint32_t)(two >> (at & 31)) & ((1u << V) - 1);
+    if (m) {
+      float z[V];
+      unpack<BF16, V>(q, z);
+#pragma unroll
+      for (int j = 0; j < V; ++j) z[j] = m >> j & 1 ? -INFINITY : z[j];
+      q = pack<BF16, V>(z);
+    }
+    return q;
+  };
+  // f(a chunk's logits, the bits that count) for every chunk of this thread; store_chunk(d) puts its gradient
+  auto for_chunks = [&](auto&& f) {
+    float z[V];
+    constexpr uint32_t kAll = (1u << V) - 1;
+    if constexpr (CH > 0) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        // opaque here, or the compiler keeps every pass's unpacked values for the next one
+        asm volatile("" : "+v"(held[i][0]), "+v"(held[i][1]), "+v"(held[i][2]), "+v"(held[i][3]));
+        unpack<BF16, V>(held[i], z);
+        f(z, kAll, [&](const float* d) { if (i * NT + tid + 1 < chunks - 1) store(i, d); });
+        __builtin_amdgcn_sched_barrier(0);                 // one chunk's values at a time in registers
+      }
+    } else {
+      for (int i = 0; i * NT + tid + 1 < chunks - 1; ++i) {
+        unpack<BF16, V>(a.rest ? without_members(load(i), (i * NT + tid + 1) * V) : load(i), z);
+        f(z, kAll, [&](const float* d) { store(i, d); });
+      }
+    }
+    if (has_edge) {
+      unpack<BF16, V>(edge, z);
+      f(z, edge_own, store_edge);
+    }
+  };
+
+  // ---- the teacher's slots
+  for (int j = tid; j < a.k; j += NT) {
+    const int id = a.labels[(long long)row * a.k + j];
+    const bool valid = (unsigned)id < (unsigned)a.C;
+    ids[j] = valid ? id : -1;
+    slot_q[j] = valid ? a.logp[(long long)row * a.k + j] : -INFINITY;
+  }
+  if (a.rest)
+    for (int w = tid; w < (chunks * V + 31) / 32 + 1; w += NT) marks[w] = 0;
+  __syncthreads();
+  float t_top = 0.f, t_sum = 1.f;                          // rest = 0: q = 2^(..) / sum, in every wave
+  if (!a.rest) {
+    t_top = -INFINITY;
+    for (int j = lane; j < a.k; j += 64) t_top = fmaxf(t_top, slot_q[j]);
+    t_top = reference(wave_max(t_top));
+    t_sum = 0.f;
+    for (int j = lane; j < a.k; j += 64) t_sum += expf(slot_q[j] - t_top);   // NaN stays NaN
+    t_sum = wave_add(t_sum);
+    if (t_sum == 0.f) {                                    // no teacher: nothing to learn
+      if (a.loss && tid == 0) a.loss[row] = 0.f;
+      if (a.grad) zero_row();
+      return;
+    }
+  }
+  __syncthreads();
+  for (int j = tid; j < a.k; j += NT) {
+    const int id = ids[j];
+    slot_q[j] = expf(slot_q[j] - t_top) / t_sum;
+    if (a.rest && id >= 0) atomicOr(&marks[(id + shift) >> 5], 1u << ((id + shift) & 31));
+  }
+  __syncthreads();
+  if (a.rest) {
+    if constexpr (CH > 0) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i)
+        if (i * NT + tid + 1 < chunks - 1) held[i] = without_members(held[i], (i * NT + tid + 1) * V);
+    }
+    if (has_edge) edge = without_members(edge, a.C >= V ? shift + edge_at : shift);
+  }
+  // of the slots of one class the first holds the class: its logit, and the sum of their q
+  constexpr int SLOTS = kMaxTokenK / NT;
+  float z_class[SLOTS], q_class[SLOTS];
+  float member_top = -INFINITY, members = 0.f, q_sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < SLOTS; ++i) {
+    const int j = tid + i * NT;
+    z_class[i] = -INFINITY;
+    q_class[i] = -1.f;                                     // no class
+    const int id = j < a.k ? ids[j] : -1;
+    if (id >= 0) {
+      float q = 0.f;
+      bool first = true;
+#pragma unroll 1
+      for (int o = 0; o < a.k; ++o)
+        if (ids[o] == id) {
+          first &= o >= j;
+          q += slot_q[o];
+        }
+      if (first) {
+        z_class[i] = element<BF16>(a.logits, base + id);
+        q_class[i] = q;
+        member_top = fmaxf(member_top, z_class[i]);
+        members += 1.f;
+        q_sum += q;
+      }
+    }
+  }
+
+  // ---- maxima, then sums of powers
+  float top = -INFINITY;
+  for_chunks([&](const float* z, uint32_t, auto&&) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) top = fmaxf(top, z[j]);
+  });
+  top = wave_max(top);
+  member_top = wave_max(member_top);
+  members = wave_add(members);
+  q_sum = wave_add(q_sum);
+  if (lane == 0) {
+    w_top[wave] = top;
+    w_member_top[wave] = member_top;
+    w_members[wave] = members;
+    w_q[wave] = q_sum;
+  }
+  __syncthreads();
+  top = member_top = -INFINITY;
+  members = q_sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    top = fmaxf(top, w_top[w]);
+    member_top = fmaxf(member_top, w_member_top[w]);
+    members += w_members[w];
+    q_sum += w_q[w];
+  }
+  const float top_r = reference(top), top_all = a.rest ? reference(fmaxf(top, member_top)) : top_r;
+  const float off_r = -top_r * s, off_all = -top_all * s;
+  float sum = 0.f;
+  for_chunks([&](const float* z, uint32_t own, auto&&) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum += own >> j & 1 ? power2(__builtin_fmaf(z[j], s, off_r)) : 0.f;
+  });
+  float member_sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < SLOTS; ++i)
+    if (q_class[i] >= 0.f || q_class[i] != q_class[i]) member_sum += power2(__builtin_fmaf(z_class[i], s, off_all));
+  sum = wave_add(sum);
+  member_sum = wave_add(member_sum);
+  if (lane == 0) {
+    w_sum[wave] = sum;
+    w_member_sum[wave] = member_sum;
+  }
+  __syncthreads();
+  sum = member_sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    sum += w_sum[w];
+    member_sum += w_member_sum[w];
+  }
+  const float part_r = sum * power2((top_r - top_all) * s);        // r's share of the sum over all
+  const float sum_all = a.rest ? part_r + member_sum : sum;
+  const bool defined = sum_all > 0.f && sum_all < INFINITY && top_all < INFINITY && member_top < INFINITY;
+  float q_r = 0.f;
+  if (a.rest) {
+    q_r = 1.f - q_sum;
+    if (q_r < kRestMin || members == (float)a.C) q_r = 0.f;
+  }
+  const float big_q = q_sum + q_r;
+  const float log_all = log2f(sum_all);
+
+  // ---- loss: a wave's part of the sum over K
+  if (a.loss) {
+    float part = 0.f;
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+      const float q = q_class[i];
+      if (q > 0.f || q != q) part += q * (logf(q) - kLn2 * (__builtin_fmaf(z_class[i], s, off_all) - log_all));
+    }
+    part = wave_add(part);
+    if (lane == 0) w_part[wave] = part;
+  }
+  // ---- gradient outside K
+  const float scale = defined ? a.t * g : NAN;
+  if (a.grad) {
+    if (g == 0.f) {
+      zero_row();
+    } else {
+      const float p_r = a.rest ? part_r / sum_all : 1.f;
+      const float factor = sum == 0.f ? (defined ? 0.f : NAN) : scale * (big_q * p_r - q_r) / sum;
+      for_chunks([&](const float* z, uint32_t, auto&& store_chunk) {
+        float d[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) d[j] = factor * power2(__builtin_fmaf(z[j], s, off_r));
+        store_chunk(d);
+      });
+      __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0): K's classes are written after these
+    }
+  }
+  __syncthreads();
+  if (a.loss && tid == 0) {
+    float part = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) part += w_part[w];
+    if (q_r > 0.f) part += sum == 0.f ? INFINITY : q_r * (logf(q_r) - kLn2 * (log2f(part_r) - log_all));
+    a.loss[row] = defined ? a.t * a.t * part : NAN;
+  }
+  if (a.grad && g != 0.f) {
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+      const float q = q_class[i];
+      if (q >= 0.f || q != q)
+        put<BF16>(a.grad, gbase + ids[tid + i * NT], scale * (big_q * (power2(__builtin_fmaf(z_class[i], s, off_all)) / sum_all) - q));
+    }
+  }
+}
+
+template <bool BF16, int NT, int CH, int OCC>
+hipError_t launch_rows(const DistillArgs& a, hipStream_t s) {
+  const size_t lds = a.rest ? ((size_t)a.C + 16 + 31) / 32 * 4 + 4 : 0;   // and a word behind
+  DistillArgs part = a;
+  for (long long row = 0; row < a.n; row += 1 << 20) {       // 2^20 rows a launch at most
+    part.row0 = (int)row;
+    const int rows = (int)std::min<long long>(a.n - row, 1 << 20);
+    hipLaunchKernelGGL((distill_kernel<BF16, NT, CH, OCC>), dim3(rows), dim3(NT), lds, s, part);
+    const hipError_t st = hipGetLastError();
+    if (st != hipSuccess) return st;
+  }
+  return hipSuccess;
+}
+
+template <bool BF16>
+hipError_t launch_by_length(const DistillArgs& a, hipStream_t s) {
+  constexpr int V = BF16 ? 8 : 4;
+  const int held = a.C + V - 1 - 2 * V;                      // classes between the edges, with the longest shift
+  if (held <= 256 * 1 * V) return launch_rows<BF16, 256, 1, 4>(a, s);
+  if (held <= 256 * 4 * V) return launch_rows<BF16, 256, 4, 4>(a, s);
+  if (held <= 512 * 8 * V) return launch_rows<BF16, 512, 8, 4>(a, s);
+  if (held <= 1024 * 8 * V) return launch_rows<BF16, 1024, 8, 4>(a, s);
+  if (held <= 1024 * 16 * V) return launch_rows<BF16, 1024, 16, 4>(a, s);
+  if (held <= 1024 * 20 * V) return launch_rows<BF16, 1024, 20, 4>(a, s);
+  return launch_rows<BF16, 1024, 0, 4>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t s) {
-  const size_t lds = a.rest ? (size_t)(a.C + 31) / 32 * 4 : 0;
-  const dim3 grid((unsigned)std::min(a.n, 1 << 20));
-  if (bf16) hipLaunchKernelGGL(distill_kernel<true>, grid, dim3(kThreads), lds, s, a);
-  else hipLaunchKernelGGL(distill_kernel<false>, grid, dim3(kThreads), lds, s, a);
-  return hipGetLastError();
+  return bf16 ? launch_by_length<true>(a, s) : launch_by_length<false>(a, s);
 }
 
 }  // namespace rafiki

@@ -39,7 +39,7 @@ struct TokenArgs {
 struct DistillArgs {
   const void* logits;
   long long ld_row;
-  int n, C, k;
+  int n, C, k, row0;          // row0: the launch's first row
   const int32_t* labels;
   const float* logp;
   float t;

@@ -23,7 +23,7 @@ bool aligned_to(const void* p, int dtype) { return ((uintptr_t)p & (dtype == RAF
 bool known(int dtype) { return dtype == RAFIKI_FP32 || dtype == RAFIKI_BF16; }
 
 long long combine_bytes(int n_models, int n, int n_classes) {
-  return (long long)n_models * n * token_stat_stride(n_classes);
+  return (long long)n_models * n * token_stat_stride(n_classes) + ((long long)n * 4 + 15) / 16 * 16;
 }
 
 int check_combine(const void* logits, int dtype, long long ld_model, long long ld_row, int n_models, int n,
@@ -54,6 +54,7 @@ TokenArgs token_args(const void* logits, long long ld_model, long long ld_row, i
   a.stat_stride = token_stat_stride(n_classes);
   a.t_all = 1.f;
   a.stats = (char*)workspace;
+  a.flat = (int32_t*)(a.stats + (long long)n_models * n * a.stat_stride);
   a.labels = labels;
   a.out = out;
   return a;

@@ -8,21 +8,27 @@ constexpr int kMaxTokenModels = 32;
 constexpr int kMaxTokenClasses = 1 << 20;
 constexpr int kMaxTokenK = 1024;
 // Statistics of the logits in the workspace: per row and model, the maximum of every 64 classes
-// (16 a unit of 1024 classes; +inf throughout a unit that holds NaN or +inf), then every unit's
-// sum of 2^((z - its maximum) log2(e) / T).
+// (16 a unit of 1024 classes; +inf throughout a unit that holds NaN or +inf), then a UnitStat of every
+// unit: its maximum and its sum of 2^((z - maximum) log2(e) / T).
+struct UnitStat {
+  double sum;
+  float top;
+  float pad;
+};
 constexpr int kUnitClasses = 1024;
 constexpr int kUnitTops = kUnitClasses / 64;
 inline int token_units(int C) { return (C + kUnitClasses - 1) / kUnitClasses; }
 inline long long token_stat_stride(int C) {   // bytes, a multiple of 16
-  return ((long long)token_units(C) * (kUnitTops * 4 + 8) + 15) / 16 * 16;
+  return (long long)token_units(C) * (kUnitTops * (long long)sizeof(float) + (long long)sizeof(UnitStat));
 }
 
 struct TokenArgs {
   const void* logits;
   long long ld_model, ld_row;
-  int S, n, C, units;
+  int S, n, C, units, row0;   // row0: the launch's first row
   const float* temperature;   // [n] or null (then t_all)
   float t_all;
+  int32_t* flat;              // [n] in the workspace: rows left to the histogram kernels
   char* stats;
   long long stat_stride;
   int32_t* labels;

@@ -7,7 +7,7 @@
 // 64-bit FMA as fast as a 32-bit one, and a power is about 20 of them.  Sums that are compared
 // are sums of integers floor(p 2^62), which do not depend on their order.
 //
-// Two launches.  stats_kernel reads the logits once: the maximum of every 64 classes and the
+// stats_kernel reads the logits once: the maximum of every 64 classes and the
 // sum of powers of every 1024 (a wave each).  The row kernels, a workgroup per row, then work
 // from these: a plain draw locates its unit of 1024 classes by the sums and reads only that;
 // top-k and the filters need only the groups of 64 whose maximum reaches a bound.  The bound is the
@@ -24,8 +24,6 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kRowThreads = 512;
-constexpr int kRowWaves = kRowThreads / 64;
 constexpr int kList = 1024;                                // classes sorted in LDS
 constexpr int kBins = 2048;
 constexpr int kMaxGroupsListed = 4096;
@@ -36,23 +34,28 @@ constexpr u64 kLeastKey = (u64)(1023 - 1000) << 52;         // bits of 2^-1000
 constexpr float kSlack = 1.f / 64;
 constexpr float kBinsPerOctave = 16.f;
 
-// 2^t, t <= 0 (-inf and NaN as -1100: 0): t = n + f, |f| <= 1/2, and 2^f = 1 + f q(f) with q of degree 9
-// through (2^f - 1) / f at Chebyshev's nodes: within 6e-16, and exactly 1 at f = 0.
+// 2^t, t <= 0 (below -1010, for -inf and for NaN: 2^-1010, less than any probability that counts).
+// t = n + f, |f| <= 1/2: adding 1.5 2^52 leaves n in the low bits, and n goes into the exponent as an integer,
+// since conversions, rint and ldexp of 64 bits take four times an FMA's cycles (with them stats_kernel
+// took 300 us for 2 x 1024 x 131072).  2^f = 1 + f q(f) with q of degree 8 through (2^f - 1) / f at
+// Chebyshev's nodes: within 4e-14, and exactly 1 at f = 0.
 __device__ __forceinline__ double power2(double t) {
-  t = __builtin_fmax(t, -1100.0);
-  const double n = __builtin_rint(t), f = t - n;
-  double y = 7.070977866508138e-09;
-  y = __builtin_fma(y, f, 1.0205905413765595e-07);
-  y = __builtin_fma(y, f, 1.3215451633221434e-06);
-  y = __builtin_fma(y, f, 1.5252672924850737e-05);
-  y = __builtin_fma(y, f, 0.00015403530424776529);
-  y = __builtin_fma(y, f, 0.0013333558200794592);
-  y = __builtin_fma(y, f, 0.009618129107618665);
-  y = __builtin_fma(y, f, 0.05550410866465167);
-  y = __builtin_fma(y, f, 0.24022650695910075);
-  y = __builtin_fma(y, f, 0.6931471805599462);
+  constexpr double kRound = 6755399441055744.0;
+  t = __builtin_fmax(t, -1010.0);
+  const double u = t + kRound, f = t - (u - kRound);
+  double y = 1.0203121063391729e-07;
+  y = __builtin_fma(y, f, 1.3255224878668817e-06);
+  y = __builtin_fma(y, f, 1.525268684626772e-05);
+  y = __builtin_fma(y, f, 0.00015403455852453838);
+  y = __builtin_fma(y, f, 0.0013333558179043112);
+  y = __builtin_fma(y, f, 0.009618129159402558);
+  y = __builtin_fma(y, f, 0.055504108664760424);
+  y = __builtin_fma(y, f, 0.2402265069581299);
+  y = __builtin_fma(y, f, 0.6931471805599453);
   y = __builtin_fma(y, f, 1.0);
-  return __builtin_ldexp(y, (int)n);
+  const int n = (int)__double_as_longlong(u);
+  const u64 bits = (u64)__double_as_longlong(y);
+  return __longlong_as_double((long long)((u64)((uint32_t)(bits >> 32) + ((uint32_t)n << 20)) << 32 | (uint32_t)bits));
 }
 
 // The exact difference of the logits first: the scaled values of two lowest logits do not cancel.
@@ -75,8 +78,8 @@ __device__ __forceinline__ double log2_scale(float t) { return t == 0.f ? 1.4426
 __device__ __forceinline__ float* stat_tops(const TokenArgs& a, long long rm) {
   return (float*)(a.stats + rm * a.stat_stride);
 }
-__device__ __forceinline__ double* stat_sums(const TokenArgs& a, long long rm) {
-  return (double*)(a.stats + rm * a.stat_stride + (long long)a.units * kUnitTops * sizeof(float));
+__device__ __forceinline__ UnitStat* stat_units(const TokenArgs& a, long long rm) {
+  return (UnitStat*)(a.stats + rm * a.stat_stride + (long long)a.units * kUnitTops * sizeof(float));
 }
 
 // Lanes exchanged within 16 by DPP: xor 1, xor 2, then mirrors of 8 and 16, which after those pair
@@ -135,50 +138,48 @@ __device__ __forceinline__ void load_logits(const void* p, long long at, int c, 
 template <bool BF16>
 __global__ __launch_bounds__(256) void stats_kernel(TokenArgs a) {
   constexpr int V = BF16 ? 8 : 4, LOADS = 16 / V;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long long total = (long long)a.n * a.S * a.units;
-  for (long long id = (long long)blockIdx.x * 4 + wave; id < total; id += (long long)gridDim.x * 4) {
-    const long long rm = total >> 32 ? id / a.units : (uint32_t)id / (uint32_t)a.units;
-    const int u = (int)(id - rm * a.units);
-    const int row = (int)(total >> 32 ? rm / a.S : (uint32_t)rm / (uint32_t)a.S), m = (int)(rm - (long long)row * a.S);
-    const double k = log2_scale(row_temperature(a, row));
-    const long long base = m * a.ld_model + row * a.ld_row;
-    float z[16], top[LOADS];
+  const int lane = threadIdx.x & 63;
+  const int u = __builtin_amdgcn_readfirstlane(blockIdx.y * (blockDim.x >> 6) + (threadIdx.x >> 6));
+  if (u >= a.units) return;
+  const int row = a.row0 + blockIdx.x, m = blockIdx.z;
+  const long long rm = (long long)row * a.S + m;
+  const double k = log2_scale(row_temperature(a, row));
+  const long long base = m * a.ld_model + row * a.ld_row;
+  float z[16], top[LOADS];
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j)
-      load_logits<BF16, V>(a.logits, base, u * kUnitClasses + (j * 64 + lane) * V, a.C, z + j * V);
-    bool bad = false;
-    float all = -INFINITY;
+  for (int j = 0; j < LOADS; ++j)
+    load_logits<BF16, V>(a.logits, base, u * kUnitClasses + (j * 64 + lane) * V, a.C, z + j * V);
+  bool bad = false;
+  float all = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) {
-      top[j] = z[j * V];
+  for (int j = 0; j < LOADS; ++j) {
+    top[j] = z[j * V];
 #pragma unroll
-      for (int i = 1; i < V; ++i) top[j] = fmaxf(top[j], z[j * V + i]);
+    for (int i = 1; i < V; ++i) top[j] = fmaxf(top[j], z[j * V + i]);
 #pragma unroll
-      for (int i = 0; i < V; ++i) bad |= !(z[j * V + i] < INFINITY);
-      top[j] = fmaxf(top[j], dpp<kXor1>(top[j]));
-      top[j] = fmaxf(top[j], dpp<kXor2>(top[j]));
-      top[j] = fmaxf(top[j], dpp<kHalfMirror>(top[j]));
-      if (!BF16) top[j] = fmaxf(top[j], dpp<kMirror>(top[j]));
-      all = fmaxf(all, top[j]);
-    }
-    if (BF16) all = fmaxf(all, dpp<kMirror>(all));
-    all = fmaxf(all, __shfl_xor(all, 16, 64));
-    all = fmaxf(all, __shfl_xor(all, 32, 64));
-    const bool any_bad = __ballot(bad) != 0;
-    float* tops = stat_tops(a, rm) + u * kUnitTops;
-    constexpr int kLanes = 64 / V;                         // lanes of one group of 64 classes
-#pragma unroll
-    for (int j = 0; j < LOADS; ++j)
-      if (lane % kLanes == 0) tops[j * (64 / kLanes) + lane / kLanes] = any_bad ? INFINITY : top[j];
-    double sum = 0.0;
-    if (!any_bad && all > -INFINITY) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sum += weight(z[i], all, k);
-    }
-    sum = wave_sum(sum);
-    if (lane == 0) stat_sums(a, rm)[u] = sum;
+    for (int i = 0; i < V; ++i) bad |= !(z[j * V + i] < INFINITY);
+    top[j] = fmaxf(top[j], dpp<kXor1>(top[j]));
+    top[j] = fmaxf(top[j], dpp<kXor2>(top[j]));
+    top[j] = fmaxf(top[j], dpp<kHalfMirror>(top[j]));
+    if (!BF16) top[j] = fmaxf(top[j], dpp<kMirror>(top[j]));
+    all = fmaxf(all, top[j]);
   }
+  if (BF16) all = fmaxf(all, dpp<kMirror>(all));
+  all = fmaxf(all, __shfl_xor(all, 16, 64));
+  all = fmaxf(all, __shfl_xor(all, 32, 64));
+  const bool any_bad = __ballot(bad) != 0;
+  float* tops = stat_tops(a, rm) + u * kUnitTops;
+  constexpr int kLanes = 64 / V;                         // lanes of one group of 64 classes
+#pragma unroll
+  for (int j = 0; j < LOADS; ++j)
+    if (lane % kLanes == 0) tops[j * (64 / kLanes) + lane / kLanes] = any_bad ? INFINITY : top[j];
+  double sum = 0.0;
+  if (!any_bad && all > -INFINITY) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += weight(z[i], all, k);
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) stat_units(a, rm)[u] = UnitStat{sum, any_bad ? INFINITY : all, 0.f};
 }
 
 // ---------------------------------------------------------------- one workgroup per row
@@ -189,16 +190,16 @@ struct RowShared {
   int state;                        // as init() returns
   u64 sums[kBins];                  // histogram; also the listed groups, and the units' masses
   uint32_t counts[kBins];
-  u64 wave_a[kRowWaves], wave_b[kRowWaves];
-  float wave_f[kRowWaves];
+  u64 wave_a[16], wave_b[16];
   u64 found_a, found_b, found_c;
   int found_class;
   uint32_t n_groups, n_list, overflow;
-  u64 list_key[kList];
-  int list_class[kList];
+  u64 list_key[kList], run_key[kList];
+  int list_class[kList], run_class[kList];
 };
 
 // Sum of v over the threads before this one; total = the sum over all.
+template <int NT>
 __device__ __forceinline__ u64 block_scan(u64 v, u64* waves, u64& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   u64 s = v;
@@ -212,24 +213,13 @@ __device__ __forceinline__ u64 block_scan(u64 v, u64* waves, u64& total) {
   __syncthreads();
   u64 before = 0;
   total = 0;
-#pragma unroll
-  for (int w = 0; w < kRowWaves; ++w) {
-    before += w < wave ? waves[w] : 0;
-    total += waves[w];
+#pragma unroll 4
+  for (int w = 0; w < NT / 64; ++w) {
+    const u64 t = waves[w];
+    before += w < wave ? t : 0;
+    total += t;
   }
   return before + s - v;
-}
-
-__device__ __forceinline__ float block_max(float v, float* waves) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = waves[0];
-#pragma unroll
-  for (int w = 1; w < kRowWaves; ++w) v = fmaxf(v, waves[w]);
-  return v;
 }
 
 __device__ __forceinline__ u64 units_of(u64 key) { return (u64)(__longlong_as_double((long long)key) * kUnit); }
@@ -267,8 +257,9 @@ struct Cut {
   u64 key, ties, mass;
 };
 
-template <bool BF16>
+template <bool BF16, int NT>
 struct Row {
+  static constexpr int kWaves = NT / 64;
   const TokenArgs& a;
   RowShared& sh;
   int row;
@@ -280,20 +271,16 @@ struct Row {
     const int lane = threadIdx.x & 63;
     if (threadIdx.x == 0) sh.state = 0;
     __syncthreads();
-    for (int m = threadIdx.x >> 6; m < a.S; m += kRowWaves) {
+    for (int m = threadIdx.x >> 6; m < a.S; m += kWaves) {
       const long long rm = (long long)row * a.S + m;
-      const float4* tops = (const float4*)stat_tops(a, rm);
-      const double* sums = stat_sums(a, rm);
+      const UnitStat* units = stat_units(a, rm);
       float top = -INFINITY;
-      for (int i = lane; i < a.units * 4; i += 64) {
-        const float4 t = tops[i];
-        top = fmaxf(top, fmaxf(fmaxf(t.x, t.y), fmaxf(t.z, t.w)));
-      }
+      for (int u = lane; u < a.units; u += 64) top = fmaxf(top, units[u].top);
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
       double s = 0.0;
       if (top > -INFINITY && top < INFINITY)
-        for (int u = lane; u < a.units; u += 64) s += sums[u] * weight(unit_top(tops, u), top, k);
+        for (int u = lane; u < a.units; u += 64) s += units[u].sum * weight(units[u].top, top, k);
       s = wave_sum(s);
       if (lane == 0) {
         sh.top[m] = top;
@@ -307,23 +294,14 @@ struct Row {
     return sh.state;
   }
 
-  static __device__ __forceinline__ float unit_top(const float4* tops, int u) {
-    float v = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float4 t = tops[u * 4 + i];
-      v = fmaxf(v, fmaxf(fmaxf(t.x, t.y), fmaxf(t.z, t.w)));
-    }
-    return v;
-  }
-
   // Units of the mass of all classes of unit u.
   __device__ u64 unit_mass(int u) const {
     double p = 0.0;
 #pragma unroll 1
     for (int m = 0; m < a.S; ++m) {
       const long long rm = (long long)row * a.S + m;
-      p += stat_sums(a, rm)[u] * sh.scale[m] * weight(unit_top((const float4*)stat_tops(a, rm), u), sh.top[m], k);
+      const UnitStat st = stat_units(a, rm)[u];
+      p += st.sum * sh.scale[m] * weight(st.top, sh.top[m], k);
     }
     return (u64)(p * kUnit);
   }
@@ -337,6 +315,38 @@ struct Row {
       p = __builtin_fma(weight(logit<BF16>(a.logits, at + m * a.ld_model), sh.top[m], k), sh.scale[m], p);
     const u64 bits = (u64)__double_as_longlong(p);
     return bits < kLeastKey ? 0 : bits;
+  }
+
+  // This lane's 16 logits of one model of unit u, as stats_kernel holds them, and the class of the i-th.
+  static constexpr int V = BF16 ? 8 : 4;
+  __device__ __forceinline__ void unit_logits(int u, int m, float z[16]) const {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < 16 / V; ++j)
+      load_logits<BF16, V>(a.logits, row * a.ld_row + m * a.ld_model, u * kUnitClasses + (j * 64 + lane) * V, a.C, z + j * V);
+  }
+  static __device__ __forceinline__ int unit_class(int u, int i) {
+    return u * kUnitClasses + (i / V * 64 + (threadIdx.x & 63)) * V + i % V;
+  }
+  // Their keys; 0 past the row's end.
+  __device__ __forceinline__ void unit_keys(int u, u64 x[16]) const {
+    double p[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) p[i] = 0.0;
+#pragma unroll 1
+    for (int m = 0; m < a.S; ++m) {
+      float z[16];
+      unit_logits(u, m, z);
+      const float top = sh.top[m];
+      const double scale = sh.scale[m];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = __builtin_fma(weight(z[i], top, k), scale, p[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const u64 bits = (u64)__double_as_longlong(p[i]);
+      x[i] = bits < kLeastKey ? 0 : bits;
+    }
   }
 
   // Bounds of log2 p over group g of 64 classes: one of its classes reaches `low`, none exceeds `high`.
@@ -367,20 +377,20 @@ struct Row {
   __device__ float bound(int need, float best) {
     const int groups = a.units * kUnitTops;
     __syncthreads();
-    for (int b = threadIdx.x; b < kBins; b += kRowThreads) sh.counts[b] = 0;
+    for (int b = threadIdx.x; b < kBins; b += NT) sh.counts[b] = 0;
     if (threadIdx.x == 0) sh.found_a = kBins - 1;
     __syncthreads();
-    for (int g = threadIdx.x; g < groups; g += kRowThreads) {
+    for (int g = threadIdx.x; g < groups; g += NT) {
       float low, high;
       group_scores(g, low, high);
       if (low > -INFINITY) atomicAdd(&sh.counts[(int)fminf((best - low) * kBinsPerOctave, (float)(kBins - 1))], 1u);
     }
     __syncthreads();
-    constexpr int PER = kBins / kRowThreads;
+    constexpr int PER = kBins / NT;
     u64 n = 0, total;
 #pragma unroll
     for (int i = 0; i < PER; ++i) n += sh.counts[threadIdx.x * PER + i];
-    u64 at = block_scan(n, sh.wave_a, total);
+    u64 at = block_scan<NT>(n, sh.wave_a, total);
     if (at < (u64)need && at + n >= (u64)need) {
       int b = threadIdx.x * PER;
       while (at + sh.counts[b] < (u64)need) at += sh.counts[b++];
@@ -391,14 +401,11 @@ struct Row {
     return b == kBins - 1 ? -INFINITY : best - (float)(b + 1) / kBinsPerOctave - kSlack;
   }
 
-  __device__ float best_score() {
+  // The largest of the groups' lower bounds: that of the class at which a model has its maximum.
+  __device__ __forceinline__ float best_score() const {
     float best = -INFINITY;
-    for (int g = threadIdx.x; g < a.units * kUnitTops; g += kRowThreads) {
-      float low, high;
-      group_scores(g, low, high);
-      best = fmaxf(best, low);
-    }
-    return block_max(best, sh.wave_f);
+    for (int m = 0; m < a.S; ++m) best = fmaxf(best, sh.log_scale[m]);
+    return best;
   }
 
   // Lists every class whose p reaches 2^(score) (and some below it); false where they do not fit.
@@ -409,7 +416,7 @@ struct Row {
     if (threadIdx.x == 0) sh.n_groups = sh.n_list = sh.overflow = 0;
     __syncthreads();
     const int n = (a.C + 63) / 64;
-    for (int g = threadIdx.x; g < n; g += kRowThreads) {
+    for (int g = threadIdx.x; g < n; g += NT) {
       float low, high;
       group_scores(g, low, high);
       if (high >= score - kSlack) {
@@ -421,7 +428,7 @@ struct Row {
     const int listed = (int)sh.n_groups;
     if (listed > kMaxGroupsListed) return false;
     const u64 least = score > -1000.f ? (u64)__double_as_longlong((double)exp2f(fmaxf(score - kSlack, -120.f))) : 1;
-    for (int i = threadIdx.x >> 6; i < listed; i += kRowWaves) {
+    for (int i = threadIdx.x >> 6; i < listed; i += kWaves) {
       const int c = (int)groups[i] * 64 + lane;
       const u64 x = c < a.C ? key(c) : 0;
       const bool take = x >= (score > -120.f ? least : 1);
@@ -438,64 +445,52 @@ struct Row {
     return sh.n_list <= kList;
   }
 
-  // Sorts the list by key down and class up.
+  // Sorts the list by key down and class up: every 64 by rank in a wave, then every class's place among the
+  // other runs of 64 by bisection.  (A bitonic sort of 1024 with a barrier a step took 60 us.)
   __device__ void sort() {
-    const int n = (int)sh.n_list;
+    const int n = (int)sh.n_list, lane = threadIdx.x & 63;
+    const int runs = (n + 63) / 64;
     __syncthreads();
-    if (n <= 256) {                                          // by rank: every element against all others
-      u64 mine = 0;
-      int cls = 0, rank = 0;
-      const int i = threadIdx.x % 256, part = threadIdx.x / 256;
-      if (threadIdx.x < 256) sh.counts[threadIdx.x] = 0;
-      __syncthreads();
+    for (int run = threadIdx.x >> 6; run < runs; run += kWaves) {
+      const int i = run * 64 + lane, m = min(64, n - run * 64);
+      const u64 x = i < n ? sh.list_key[i] : 0;
+      const int c = i < n ? sh.list_class[i] : 0x7fffffff;
+      int rank = 0;
+      for (int j = 0; j < m; ++j) {
+        const u64 y = sh.list_key[run * 64 + j];
+        rank += (y > x) | ((y == x) & (sh.list_class[run * 64 + j] < c));
+      }
       if (i < n) {
-        mine = sh.list_key[i];
-        cls = sh.list_class[i];
-        for (int j = part; j < n; j += kRowThreads / 256) {
-          const u64 o = sh.list_key[j];
-          rank += (o > mine) | ((o == mine) & (sh.list_class[j] < cls));
-        }
-        atomicAdd(&sh.counts[i], (uint32_t)rank);
+        sh.run_key[run * 64 + rank] = x;
+        sh.run_class[run * 64 + rank] = c;
       }
-      __syncthreads();
-      if (threadIdx.x < n) {
-        sh.list_key[sh.counts[threadIdx.x]] = mine;
-        sh.list_class[sh.counts[threadIdx.x]] = cls;
-      }
-      __syncthreads();
-      return;
-    }
-    int size = 512;
-    while (size < n) size *= 2;
-    for (int i = n + threadIdx.x; i < size; i += kRowThreads) {
-      sh.list_key[i] = 0;
-      sh.list_class[i] = 0x7fffffff;
     }
     __syncthreads();
-    for (int span = 2; span <= size; span *= 2)
-      for (int d = span / 2; d > 0; d /= 2) {
-        for (int t = threadIdx.x; t < size / 2; t += kRowThreads) {
-          const int i = (t & ~(d - 1)) * 2 | (t & (d - 1)), j = i | d;
-          const u64 ki = sh.list_key[i], kj = sh.list_key[j];
-          const int ci = sh.list_class[i], cj = sh.list_class[j];
-          const bool after = (ki < kj) | ((ki == kj) & (ci > cj));    // i belongs behind j
-          if (after == ((i & span) == 0)) {
-            sh.list_key[i] = kj;
-            sh.list_key[j] = ki;
-            sh.list_class[i] = cj;
-            sh.list_class[j] = ci;
-          }
+    for (int i = threadIdx.x; i < n; i += NT) {
+      const u64 x = sh.run_key[i];
+      const int c = sh.run_class[i];
+      int place = i & 63;
+      for (int run = 0; run < runs; ++run) {
+        if (run == i >> 6) continue;
+        int lo = 0, hi = min(64, n - run * 64);             // classes of the run before this one
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          const u64 y = sh.run_key[run * 64 + mid];
+          if ((y > x) | ((y == x) & (sh.run_class[run * 64 + mid] < c))) lo = mid + 1;
+          else hi = mid;
         }
-        __syncthreads();
+        place += lo;
       }
+      sh.list_key[place] = x;
+      sh.list_class[place] = c;
+    }
+    __syncthreads();
   }
 
-  // Sum of the units of the first n listed classes, and the number of leading classes whose sum
-  // reaches target (n + 1 where all n do not).
-  __device__ u64 prefix(int n, u64 target, int& reached) {
-    constexpr int PER = kList / kRowThreads;
-    __syncthreads();
-    if (threadIdx.x == 0) sh.found_class = n + 1;
+  // run_key[i] = the units of the listed classes up to and with i.
+  __device__ void accumulate() {
+    constexpr int PER = kList / NT;
+    const int n = (int)sh.n_list;
     u64 p[PER], sum = 0, total;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -503,15 +498,48 @@ struct Row {
       p[j] = i < n ? units_of(sh.list_key[i]) : 0;
       sum += p[j];
     }
-    u64 at = block_scan(sum, sh.wave_a, total);
+    u64 at = block_scan<NT>(sum, sh.wave_a, total);
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      if (at < target && at + p[j] >= target) sh.found_class = threadIdx.x * PER + j + 1;
+      const int i = threadIdx.x * PER + j;
       at += p[j];
+      if (i < n) sh.run_key[i] = at;
     }
     __syncthreads();
-    reached = sh.found_class;
-    return total;
+  }
+
+  // The number of the first n accumulated classes whose sum reaches target (n + 1 where all do not).
+  __device__ int reach(int n, u64 target) {
+    __syncthreads();
+    if (threadIdx.x == 0) sh.found_class = n + 1;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += NT)
+      if (sh.run_key[i] >= target && (i == 0 || sh.run_key[i - 1] < target)) sh.found_class = i + 1;
+    __syncthreads();
+    return sh.found_class;
+  }
+
+  // The largest key, from the groups that may hold it.
+  __device__ u64 best_key(float best) {
+    u64 top = 0;
+    const int lane = threadIdx.x & 63;
+    for (int g = threadIdx.x >> 6; g < (a.C + 63) / 64; g += kWaves) {
+      float low, high;
+      group_scores(g, low, high);
+      if (high < best - kSlack) continue;
+      const u64 x = g * 64 + lane < a.C ? key(g * 64 + lane) : 0;
+      top = x > top ? x : top;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const u64 other = __shfl_xor(top, o, 64);
+      top = other > top ? other : top;
+    }
+    __syncthreads();
+    if (lane == 0) sh.wave_a[threadIdx.x >> 6] = top;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) top = sh.wave_a[w] > top ? sh.wave_a[w] : top;
+    return top;
   }
 
   // The cut at which the number (by_sum: the sum of the units) of the classes from the top reaches
@@ -525,32 +553,35 @@ struct Row {
     int shift = whole ? 52 : 47, up = 64;
     for (;;) {
       __syncthreads();
-      for (int b = threadIdx.x; b < kBins; b += kRowThreads) {
+      for (int b = threadIdx.x; b < kBins; b += NT) {
         sh.sums[b] = 0;
         sh.counts[b] = 0;
       }
       if (threadIdx.x == 0) sh.found_a = kBins;
       __syncthreads();
-      for (int c = threadIdx.x; c < a.C; c += kRowThreads) {
-        const u64 x = key(c);
-        if (x != 0 && (up == 64 || x >> up == prefix_bits >> up)) {
-          // bins ascend as keys descend
-          const u64 top_bin = up == 64 ? (whole ? 2047 : first_bin) : (prefix_bits >> shift) | (((u64)1 << (up - shift)) - 1);
-          const u64 below = top_bin - (x >> shift);
-          const int b = (x >> shift) > top_bin ? 0 : below < kBins - 1 ? (int)below : kBins - 1;
-          atomicAdd(&sh.sums[b], units_of(x));
-          atomicAdd(&sh.counts[b], 1u);
-        }
+      // bins ascend as keys descend
+      const u64 top_bin = up == 64 ? (whole ? 2047 : first_bin) : (prefix_bits >> shift) | (((u64)1 << (up - shift)) - 1);
+      for (int u = threadIdx.x >> 6; u < a.units; u += kWaves) {
+        u64 x[16];
+        unit_keys(u, x);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (x[i] != 0 && (up == 64 || x[i] >> up == prefix_bits >> up)) {
+            const u64 below = top_bin - (x[i] >> shift);
+            const int b = (x[i] >> shift) > top_bin ? 0 : below < kBins - 1 ? (int)below : kBins - 1;
+            atomicAdd(&sh.sums[b], units_of(x[i]));
+            atomicAdd(&sh.counts[b], 1u);
+          }
       }
       __syncthreads();
-      constexpr int PER = kBins / kRowThreads;
+      constexpr int PER = kBins / NT;
       u64 n = 0, s = 0, total_n, total_s;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         n += sh.counts[threadIdx.x * PER + i];
         s += sh.sums[threadIdx.x * PER + i];
       }
-      u64 at_n = above_n + block_scan(n, sh.wave_a, total_n), at_s = above_sum + block_scan(s, sh.wave_b, total_s);
+      u64 at_n = above_n + block_scan<NT>(n, sh.wave_a, total_n), at_s = above_sum + block_scan<NT>(s, sh.wave_b, total_s);
       const u64 at = by_sum ? at_s : at_n, part = by_sum ? s : n;
       if (at < target && at + part >= target) {
         int b = threadIdx.x * PER;
@@ -566,7 +597,6 @@ struct Row {
       const int b = (int)sh.found_a;
       if (b == kBins) return false;
       if (up == 64 && !whole && b == kBins - 1) return false;         // beyond 63 octaves
-      const u64 top_bin = up == 64 ? (whole ? 2047 : first_bin) : (prefix_bits >> shift) | (((u64)1 << (up - shift)) - 1);
       prefix_bits = (top_bin - b) << shift;
       above_n = sh.found_b;
       above_sum = sh.found_c;
@@ -574,11 +604,18 @@ struct Row {
       if (count <= kList) {
         list_prefix(prefix_bits, shift);
         sort();
-        int r;
-        if (by_sum) prefix(count, target - above_sum, r);
-        else r = (int)(target - above_n);
+        accumulate();
+        const int r = by_sum ? reach(count, target - above_sum) : (int)(target - above_n);
         cut.key = sh.list_key[r - 1];
-        finish(r, above_sum, cut);
+        cut.mass = above_sum + sh.run_key[r - 1];
+        __syncthreads();
+        if (threadIdx.x == 0) sh.found_class = 0;
+        __syncthreads();
+        int same = 0;
+        for (int i = threadIdx.x; i < r; i += NT) same += sh.list_key[i] == cut.key;
+        if (same) atomicAdd(&sh.found_class, same);
+        __syncthreads();
+        cut.ties = (u64)sh.found_class;
         return true;
       }
       if (shift == 0) {                                                // one key, in more classes than the list holds
@@ -591,20 +628,6 @@ struct Row {
       up = shift;
       shift = shift > 11 ? shift - 11 : 0;
     }
-  }
-
-  // ties and mass of a cut behind the first r listed classes.
-  __device__ void finish(int r, u64 above_sum, Cut& cut) {
-    __syncthreads();
-    if (threadIdx.x == 0) sh.counts[0] = 0;
-    __syncthreads();
-    int same = 0;
-    for (int i = threadIdx.x; i < r; i += kRowThreads) same += sh.list_key[i] == cut.key;
-    if (same) atomicAdd(&sh.counts[0], (uint32_t)same);
-    __syncthreads();
-    cut.ties = sh.counts[0];
-    int unused;
-    cut.mass = above_sum + prefix(r, ~(u64)0, unused);
   }
 
   // Lists the classes whose key starts with prefix_bits.
@@ -622,28 +645,120 @@ struct Row {
       if (!(lo > -120.f)) lo = -INFINITY, hi = INFINITY;
     }
     const float kf = fminf((float)k, 3e38f);
-    for (int c = threadIdx.x; c < a.C; c += kRowThreads) {
-      if (a.S == 1) {
-        const float t = (logit<BF16>(a.logits, row * a.ld_row + c) - sh.top[0]) * kf + sh.log_scale[0];
-        if (t < lo || t > hi) continue;
-      }
-      const u64 x = key(c);
+    auto take = [&](u64 x, int c) {
       if (x != 0 && x >> shift == want) {
-        const uint32_t i = atomicAdd(&sh.n_list, 1u);
-        if (i < kList) {
-          sh.list_key[i] = x;
-          sh.list_class[i] = c;
+        const uint32_t at = atomicAdd(&sh.n_list, 1u);
+        if (at < kList) {
+          sh.list_key[at] = x;
+          sh.list_class[at] = c;
         }
+      }
+    };
+    for (int u = threadIdx.x >> 6; u < a.units; u += kWaves) {
+      if (a.S == 1) {
+        float z[16];
+        unit_logits(u, 0, z);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float t = (z[i] - sh.top[0]) * kf + sh.log_scale[0];
+          if (!(t < lo || t > hi)) {
+            const u64 x = (u64)__double_as_longlong(__builtin_fma(weight(z[i], sh.top[0], k), sh.scale[0], 0.0));
+            take(x < kLeastKey ? 0 : x, unit_class(u, i));
+          }
+        }
+      } else {
+        u64 x[16];
+        unit_keys(u, x);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) take(x[i], unit_class(u, i));
       }
     }
     __syncthreads();
+  }
+
+  // Draws from the first n accumulated classes, in the order of their indices.
+  __device__ void draw_listed(int n, u64 target, u64 mass, bool greedy) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += NT) sh.sums[i] = sh.run_key[i] - (i ? sh.run_key[i - 1] : 0);
+    __syncthreads();
+    if (n > 128) {
+      // sorted by index (as keys: the complement, which descends), their places beside
+      for (int i = threadIdx.x; i < n; i += NT) {
+        sh.list_key[i] = (u64)(0x7fffffff - sh.list_class[i]) << 16 | (u64)i;
+        sh.list_class[i] = 0;
+      }
+      if (threadIdx.x == 0) sh.n_list = n;
+      sort();
+      constexpr int PER = kList / NT;
+      u64 p[PER], sum = 0, total;
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        const int i = threadIdx.x * PER + j;
+        p[j] = i < n ? sh.sums[sh.list_key[i] & 0xFFFF] : 0;
+        sum += p[j];
+      }
+      u64 at = block_scan<NT>(sum, sh.wave_a, total);
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        if (at <= target && at + p[j] > target) {
+          a.labels[row] = 0x7fffffff - (int)(sh.list_key[threadIdx.x * PER + j] >> 16);
+          a.out[row] = (float)((double)p[j] / (double)mass);
+        }
+        at += p[j];
+      }
+      return;
+    }
+    for (int i = threadIdx.x; i < n; i += NT) {
+      const int c = sh.list_class[i];
+      u64 before = 0;                                        // of the classes of lower index
+      for (int j = 0; j < n; ++j) before += sh.list_class[j] < c ? sh.sums[j] : 0;
+      const u64 p = sh.sums[i];
+      if (before <= target && before + p > target) {
+        a.labels[row] = c;
+        a.out[row] = greedy ? 1.f : (float)((double)p / (double)mass);
+      }
+    }
+  }
+
+  // The units' masses into sums, and their sum.
+  __device__ u64 unit_masses() {
+    u64 total = 0;
+    for (int first = 0; first < a.units; first += NT) {
+      const int unit = first + threadIdx.x;
+      const u64 mass = unit < a.units ? unit_mass(unit) : 0;
+      if (unit < a.units) sh.sums[unit] = mass;
+      u64 part;
+      block_scan<NT>(mass, sh.wave_a, part);
+      total += part;
+    }
+    return total;
+  }
+
+  // The unit in which the sums of the units' masses pass target, and what of target lies in it.
+  __device__ void find_unit(u64 target, int& unit, u64& rest) {
+    u64 seen = 0;
+    __syncthreads();
+    for (int first = 0; first < a.units; first += NT) {
+      const int i = first + threadIdx.x;
+      const u64 mass = i < a.units ? sh.sums[i] : 0;
+      u64 part;
+      const u64 at = seen + block_scan<NT>(mass, sh.wave_a, part);
+      if (at <= target && at + mass > target) {
+        sh.found_a = i;
+        sh.found_b = target - at;
+      }
+      seen += part;
+    }
+    __syncthreads();
+    unit = (int)sh.found_a;
+    rest = sh.found_b;
   }
 
   // The class c of [c0, c0 + kUnitClasses) at which the kept units pass `target`, counted from c0; the
   // first `ties` classes with key == cut are kept.  Where they stay below target (it comes from sums of
   // another rounding) the last kept; false where none has any units.
   __device__ bool draw_in_unit(int c0, u64 target, u64 cut, u64 ties, u64 mass, float u) {
-    constexpr int PER = kUnitClasses / kRowThreads;
+    constexpr int PER = kUnitClasses / NT;
     u64 x[PER], equal = 0, part = 0, total;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -651,7 +766,7 @@ struct Row {
       x[j] = c < a.C ? key(c) : 0;
       equal += x[j] == cut;
     }
-    u64 tie = block_scan(equal, sh.wave_a, total);
+    u64 tie = block_scan<NT>(equal, sh.wave_a, total);
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       // selects: from a branch on `x < cut || (x == cut && tie++ >= ties)` the compiler of ROCm 7.2
@@ -661,7 +776,7 @@ struct Row {
       x[j] = keep ? units_of(x[j]) : 0;
       part += x[j];
     }
-    u64 at = block_scan(part, sh.wave_b, total);
+    u64 at = block_scan<NT>(part, sh.wave_b, total);
     if (a.units == 1) {                                      // the row's own sum of units decides
       mass = total;
       target = draw_target(total, u);
@@ -688,275 +803,260 @@ struct Row {
   }
 };
 
-template <bool BF16>
-__global__ __launch_bounds__(kRowThreads, 4) void sample_kernel(TokenArgs a) {
+// A row's filters, each off or within its range.
+struct Filters {
+  int top_k;                  // 0: off
+  float top_p, min_p, u;      // 1, 0: off
+  bool greedy;
+};
+__device__ __forceinline__ Filters row_filters(const TokenArgs& a, int row, float t) {
+  Filters f{a.top_k ? a.top_k[row] : 0, a.top_p ? a.top_p[row] : 1.f, a.min_p ? a.min_p[row] : 0.f, a.uniform[row], t == 0.f};
+  if (f.greedy) f = Filters{1, 1.f, 0.f, 0.f, true};
+  if (f.top_p <= 0.f) f.top_k = 1;
+  if (f.top_k <= 0 || f.top_k >= a.C) f.top_k = 0;
+  if (!(f.top_p > 0.f && f.top_p < 1.f)) f.top_p = 1.f;
+  f.min_p = f.min_p > 0.f ? fminf(f.min_p, 1.f) : 0.f;
+  return f;
+}
+
+// Rows drawn from one unit or from a list; those that need more are left to sample_flat_kernel.  Apart,
+// because a row's time is mostly that of fetching the code it runs through once.
+template <bool BF16, int NT>
+__global__ __launch_bounds__(NT) void sample_kernel(TokenArgs a) {
   __shared__ RowShared sh;
-  for (int row = blockIdx.x; row < a.n; row += gridDim.x) {
-    __syncthreads();
-    const float t = row_temperature(a, row);
-    Row<BF16> r{a, sh, row, log2_scale(t)};
-    const int state = t >= 0.f ? r.init() : 2;
-    if (state != 0) {
-      if (threadIdx.x == 0) {
-        a.labels[row] = -1;
-        a.out[row] = state == 1 ? 0.f : NAN;
-      }
-      continue;
+  const int row = a.row0 + blockIdx.x;
+  const float t = row_temperature(a, row);
+  Row<BF16, NT> r{a, sh, row, log2_scale(t)};
+  const int state = t >= 0.f ? r.init() : 2;
+  if (threadIdx.x == 0) a.flat[row] = 0;
+  if (state != 0) {
+    if (threadIdx.x == 0) {
+      a.labels[row] = -1;
+      a.out[row] = state == 1 ? 0.f : NAN;
     }
-    const bool greedy = t == 0.f;
-    int top_k = greedy ? 1 : a.top_k ? a.top_k[row] : 0;
-    float top_p = greedy || !a.top_p ? 1.f : a.top_p[row];
-    float min_p = greedy || !a.min_p ? 0.f : a.min_p[row];
-    const float u = greedy ? 0.f : a.uniform[row];
-    if (top_p <= 0.f) { top_k = 1; top_p = 1.f; }
-    if (top_k <= 0 || top_k >= a.C) top_k = 0;               // off
-    min_p = min_p > 0.f ? fminf(min_p, 1.f) : 0.f;
-    const bool by_mass = top_p < 1.f;
-
-    // the units' masses
-    u64 total = 0;
-    for (int first = 0; first < a.units; first += kRowThreads) {
-      const int unit = first + threadIdx.x;
-      const u64 mass = unit < a.units ? r.unit_mass(unit) : 0;
-      if (unit < a.units) sh.sums[unit] = mass;
-      u64 part;
-      block_scan(mass, sh.wave_a, part);
-      total += part;
-    }
-    if (!top_k && !by_mass && min_p == 0.f) {
-      const u64 target = draw_target(total, u);
-      u64 seen = 0;
-      __syncthreads();
-      for (int first = 0; first < a.units; first += kRowThreads) {
-        const int unit = first + threadIdx.x;
-        const u64 mass = unit < a.units ? sh.sums[unit] : 0;
-        u64 part;
-        const u64 at = seen + block_scan(mass, sh.wave_a, part);
-        if (at <= target && at + mass > target) {
-          sh.found_a = unit;
-          sh.found_b = target - at;
-        }
-        seen += part;
-      }
-      __syncthreads();
-      const int unit = (int)sh.found_a;
-      const u64 rest = sh.found_b;
-      r.draw(unit, rest, total, u);
-      continue;
-    }
-
-    // the kept classes, from a list where they fit into one
-    const float best = r.best_score();
-    float score;
-    if (a.C <= kList) score = -INFINITY;
-    else if (top_k) score = r.bound(top_k, best);
-    else if (by_mass) score = r.bound(256, best);
-    else score = best + __log2f(min_p) - kSlack;
-    if (r.list(score)) {
-      r.sort();
-      int kept = (int)sh.n_list;
-      if (top_k) kept = min(kept, top_k);
-      bool all = true;
-      if (by_mass) {
-        int unused, reached;
-        const u64 mass = top_k || a.C <= kList ? r.prefix(kept, ~(u64)0, unused) : total;
-        r.prefix(kept, times_fraction(mass, top_p, 1), reached);
-        // past the list: short of the mass, unless the list is everything
-        if (reached > kept) all = top_k || a.C <= kList;
-        else kept = reached;
-      }
-      if (all) {
-        if (min_p > 0.f) {
-          const double least = (double)min_p * __longlong_as_double((long long)sh.list_key[0]);
-          __syncthreads();
-          if (threadIdx.x == 0) sh.found_class = kept;
-          __syncthreads();
-          for (int i = threadIdx.x; i < kept; i += kRowThreads)
-            if (__longlong_as_double((long long)sh.list_key[i]) < least) atomicMin(&sh.found_class, i);
-          __syncthreads();
-          kept = sh.found_class;
-        }
-        int unused;
-        const u64 mass = r.prefix(kept, ~(u64)0, unused), target = draw_target(mass, u);
-        for (int i = threadIdx.x; i < kept; i += kRowThreads) {
-          const int c = sh.list_class[i];
-          u64 before = 0;                                    // of the kept classes of lower index
-          for (int j = 0; j < kept; ++j) before += sh.list_class[j] < c ? units_of(sh.list_key[j]) : 0;
-          const u64 p = units_of(sh.list_key[i]);
-          if (before <= target && before + p > target) {
-            a.labels[row] = c;
-            a.out[row] = greedy ? 1.f : (float)((double)p / (double)mass);
-          }
-        }
+    return;
+  }
+  const Filters f = row_filters(a, row, t);
+  const bool by_mass = f.top_p < 1.f;
+  const u64 total = f.top_k ? 0 : r.unit_masses();
+  if (!f.top_k && !by_mass && f.min_p == 0.f) {
+    int unit;
+    u64 rest;
+    r.find_unit(draw_target(total, f.u), unit, rest);
+    r.draw(unit, rest, total, f.u);
+    return;
+  }
+  const float best = r.best_score();
+  float score;
+  if (f.top_k || by_mass) score = r.bound(f.top_k ? f.top_k : min(64, max(a.units * kUnitTops / 4, 4)), best);
+  else score = best + __log2f(f.min_p) - kSlack;
+  for (bool whole = false; r.list(score); whole = true) {
+    r.sort();
+    r.accumulate();
+    int kept = (int)sh.n_list;
+    whole |= kept == a.C;
+    if (f.top_k) kept = min(kept, f.top_k);
+    if (by_mass) {
+      const u64 mass = f.top_k || whole ? sh.run_key[kept - 1] : total;
+      const int reached = r.reach(kept, times_fraction(mass, f.top_p, 1));
+      if (reached > kept) {                                  // the list is short of the mass
+        if (a.C > kList) break;
+        score = -INFINITY;
         continue;
       }
+      kept = reached;
     }
+    if (f.min_p > 0.f) {
+      const double least = (double)f.min_p * __longlong_as_double((long long)sh.list_key[0]);
+      __syncthreads();
+      if (threadIdx.x == 0) sh.found_class = kept;
+      __syncthreads();
+      for (int i = threadIdx.x; i < kept; i += NT)
+        if (__longlong_as_double((long long)sh.list_key[i]) < least) atomicMin(&sh.found_class, i);
+      __syncthreads();
+      kept = sh.found_class;
+    }
+    const u64 mass = sh.run_key[kept - 1];
+    r.draw_listed(kept, draw_target(mass, f.u), mass, f.greedy);
+    return;
+  }
+  if (threadIdx.x == 0) a.flat[row] = 1;
+}
 
-    // more classes than a list holds: cut by histograms, then a scan of the units
-    Cut cut{1, ~(u64)0, total};
-    if (top_k) r.select(false, (u64)top_k, false, cut);
-    if (by_mass) r.select(true, times_fraction(cut.mass, top_p, 1), false, cut);
-    if (min_p > 0.f) {
-      u64 top = 0;
-      for (int c = threadIdx.x; c < a.C; c += kRowThreads) {
-        const u64 x = r.key(c);
-        top = x > top ? x : top;
-      }
+// Rows with more kept classes than a list holds: cut by histograms, then a scan of the units.
+template <bool BF16, int NT>
+__global__ __launch_bounds__(NT, 4) void sample_flat_kernel(TokenArgs a) {
+  __shared__ RowShared sh;
+  const int row = a.row0 + blockIdx.x;
+  if (!a.flat[row]) return;
+  const float t = row_temperature(a, row);
+  Row<BF16, NT> r{a, sh, row, log2_scale(t)};
+  r.init();
+  const Filters f = row_filters(a, row, t);
+  Cut cut{1, ~(u64)0, r.unit_masses()};
+  if (f.top_k) r.select(false, (u64)f.top_k, false, cut);
+  if (f.top_p < 1.f) r.select(true, times_fraction(cut.mass, f.top_p, 1), false, cut);
+  if (f.min_p > 0.f) {
+    const u64 top = r.best_key(r.best_score());
+    const u64 least = (u64)__double_as_longlong((double)f.min_p * __longlong_as_double((long long)top));
+    if (least > cut.key) { cut.key = least; cut.ties = ~(u64)0; }
+  }
+  __syncthreads();
+  // a wave per unit: the units above the cut, and the ties
+  const int lane = threadIdx.x & 63;
+  for (int unit = threadIdx.x >> 6; unit < a.units; unit += NT / 64) {
+    u64 mass = 0;
+    uint32_t equal = 0;
+    u64 x[16];
+    r.unit_keys(unit, x);
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) {
-        const u64 other = __shfl_xor(top, o, 64);
-        top = other > top ? other : top;
-      }
-      __syncthreads();
-      if ((threadIdx.x & 63) == 0) sh.wave_a[threadIdx.x >> 6] = top;
-      __syncthreads();
-      for (int w = 0; w < kRowWaves; ++w) top = sh.wave_a[w] > top ? sh.wave_a[w] : top;
-      const u64 least = (u64)__double_as_longlong((double)min_p * __longlong_as_double((long long)top));
-      if (least > cut.key) { cut.key = least; cut.ties = ~(u64)0; }
+    for (int i = 0; i < 16; ++i) {
+      mass += x[i] > cut.key ? units_of(x[i]) : 0;
+      equal += x[i] == cut.key;
     }
-    __syncthreads();
-    // a wave per unit: the units above the cut, and the ties
-    const int lane = threadIdx.x & 63;
-    for (int unit = threadIdx.x >> 6; unit < a.units; unit += kRowWaves) {
-      u64 mass = 0;
-      uint32_t equal = 0;
-      for (int i = lane; i < kUnitClasses; i += 64) {
-        const int c = unit * kUnitClasses + i;
-        const u64 x = c < a.C ? r.key(c) : 0;
-        mass += x > cut.key ? units_of(x) : 0;
-        equal += x == cut.key;
-      }
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) {
-        mass += __shfl_xor(mass, o, 64);
-        equal += __shfl_xor(equal, o, 64);
-      }
-      if (lane == 0) {
-        sh.sums[unit] = mass;
-        sh.counts[unit] = equal;
-      }
+    for (int o = 32; o > 0; o >>= 1) {
+      mass += __shfl_xor(mass, o, 64);
+      equal += __shfl_xor(equal, o, 64);
     }
-    __syncthreads();
-    const u64 each = units_of(cut.key);
-    u64 seen_ties = 0;
-    total = 0;
-    for (int first = 0; first < a.units; first += kRowThreads) {
-      const int unit = first + threadIdx.x;
-      const u64 equal = unit < a.units ? sh.counts[unit] : 0;
-      u64 part_ties, part;
-      const u64 before = seen_ties + block_scan(equal, sh.wave_a, part_ties);
-      const u64 kept = before >= cut.ties ? 0 : equal < cut.ties - before ? equal : cut.ties - before;
-      const u64 mass = unit < a.units ? sh.sums[unit] + kept * each : 0;
-      block_scan(mass, sh.wave_b, part);
-      if (unit < a.units) {
-        sh.sums[unit] = mass;
-        sh.counts[unit] = (uint32_t)kept;
-      }
-      seen_ties += part_ties;
-      total += part;
+    if (lane == 0) {
+      sh.sums[unit] = mass;
+      sh.counts[unit] = equal;
     }
-    const u64 target = draw_target(total, u);
-    u64 seen = 0;
-    for (int first = 0; first < a.units; first += kRowThreads) {
-      const int unit = first + threadIdx.x;
-      const u64 mass = unit < a.units ? sh.sums[unit] : 0;
-      u64 part;
-      const u64 at = seen + block_scan(mass, sh.wave_a, part);
-      if (at <= target && at + mass > target) {
-        sh.found_a = unit;
-        sh.found_b = target - at;
-      }
-      seen += part;
+  }
+  __syncthreads();
+  const u64 each = units_of(cut.key);
+  u64 seen_ties = 0, total = 0;
+  for (int first = 0; first < a.units; first += NT) {
+    const int unit = first + threadIdx.x;
+    const u64 equal = unit < a.units ? sh.counts[unit] : 0;
+    u64 part_ties, part;
+    const u64 before = seen_ties + block_scan<NT>(equal, sh.wave_a, part_ties);
+    const u64 kept = before >= cut.ties ? 0 : equal < cut.ties - before ? equal : cut.ties - before;
+    const u64 mass = unit < a.units ? sh.sums[unit] + kept * each : 0;
+    block_scan<NT>(mass, sh.wave_b, part);
+    if (unit < a.units) {
+      sh.sums[unit] = mass;
+      sh.counts[unit] = (uint32_t)kept;
     }
-    __syncthreads();
-    const int unit = (int)sh.found_a;
-    const u64 rest = sh.found_b;
-    r.draw_in_unit(unit * kUnitClasses, rest, cut.key, sh.counts[unit], total, u);
+    seen_ties += part_ties;
+    total += part;
+  }
+  int unit;
+  u64 rest;
+  r.find_unit(draw_target(total, f.u), unit, rest);
+  r.draw_in_unit(unit * kUnitClasses, rest, cut.key, sh.counts[unit], total, f.u);
+}
+
+// Sorts the list of a row's first classes and writes it.
+template <bool BF16, int NT>
+__device__ __forceinline__ void write_topk(const TokenArgs& a, RowShared& sh, Row<BF16, NT>& r, int row) {
+  r.sort();
+  const int n = (int)sh.n_list;
+  for (int j = threadIdx.x; j < a.k; j += NT) {
+    const u64 key = j < n ? sh.list_key[j] : 0;
+    a.labels[(long long)row * a.k + j] = key ? sh.list_class[j] : -1;
+    a.out[(long long)row * a.k + j] = key ? (float)log(__longlong_as_double((long long)key)) : -INFINITY;
   }
 }
 
-template <bool BF16>
-__global__ __launch_bounds__(kRowThreads, 4) void topk_kernel(TokenArgs a) {
+template <bool BF16, int NT>
+__global__ __launch_bounds__(NT) void topk_kernel(TokenArgs a) {
   __shared__ RowShared sh;
-  for (int row = blockIdx.x; row < a.n; row += gridDim.x) {
-    __syncthreads();
-    Row<BF16> r{a, sh, row, log2_scale(a.t_all)};
-    const int state = r.init();
-    int32_t* labels = a.labels + (long long)row * a.k;
-    float* logp = a.out + (long long)row * a.k;
-    if (state != 0) {
-      for (int j = threadIdx.x; j < a.k; j += kRowThreads) {
-        labels[j] = -1;
-        logp[j] = state == 1 ? -INFINITY : NAN;
-      }
-      continue;
+  const int row = a.row0 + blockIdx.x;
+  Row<BF16, NT> r{a, sh, row, log2_scale(a.t_all)};
+  const int state = r.init();
+  const bool listed = state != 0 || r.list(r.bound(a.k, r.best_score()));
+  if (threadIdx.x == 0) a.flat[row] = !listed;
+  if (state != 0) {
+    for (int j = threadIdx.x; j < a.k; j += NT) {
+      a.labels[(long long)row * a.k + j] = -1;
+      a.out[(long long)row * a.k + j] = state == 1 ? -INFINITY : NAN;
     }
-    bool listed;
-    if (a.C <= kList) listed = r.list(-INFINITY);
-    else {
-      const float best = r.best_score();
-      const float score = r.bound(a.k, best);
-      listed = r.list(score);
-    }
-    if (!listed) {
-      // the cut by histograms; the list is then the classes above it and the first ties
-      Cut cut{1, ~(u64)0, 0};
-      r.select(false, (u64)a.k, true, cut);
-      __syncthreads();
-      if (threadIdx.x == 0) sh.n_list = 0;
-      __syncthreads();
-      u64 seen_ties = 0;
-      for (int c0 = 0; c0 < a.C; c0 += kRowThreads) {
-        const int c = c0 + threadIdx.x;
-        const u64 key = c < a.C ? r.key(c) : 0;
-        u64 total;
-        const u64 tie = seen_ties + block_scan(key == cut.key, sh.wave_a, total);
-        if ((key > cut.key) | ((key == cut.key) & (tie < cut.ties))) {
-          const uint32_t i = atomicAdd(&sh.n_list, 1u);
-          if (i < kList) {
-            sh.list_key[i] = key;
-            sh.list_class[i] = c;
-          }
-        }
-        seen_ties += total;
-      }
-    }
-    __syncthreads();
-    r.sort();
-    const int n = (int)sh.n_list;
-    for (int j = threadIdx.x; j < a.k; j += kRowThreads) {
-      const u64 key = j < n ? sh.list_key[j] : 0;
-      labels[j] = key ? sh.list_class[j] : -1;
-      logp[j] = key ? (float)log(__longlong_as_double((long long)key)) : -INFINITY;
-    }
+  } else if (listed) {
+    write_topk<BF16, NT>(a, sh, r, row);
   }
+}
+
+// Rows whose groups do not bound the k-th class closely enough for a list: the cut by histograms; the
+// list is then the classes above it and the first ties.
+template <bool BF16, int NT>
+__global__ __launch_bounds__(NT, 4) void topk_flat_kernel(TokenArgs a) {
+  __shared__ RowShared sh;
+  const int row = a.row0 + blockIdx.x;
+  if (!a.flat[row]) return;
+  Row<BF16, NT> r{a, sh, row, log2_scale(a.t_all)};
+  r.init();
+  Cut cut{1, ~(u64)0, 0};
+  r.select(false, (u64)a.k, true, cut);
+  __syncthreads();
+  if (threadIdx.x == 0) sh.n_list = 0;
+  __syncthreads();
+  u64 seen_ties = 0;
+  for (int c0 = 0; c0 < a.C; c0 += NT) {
+    const int c = c0 + threadIdx.x;
+    const u64 key = c < a.C ? r.key(c) : 0;
+    u64 total;
+    const u64 tie = seen_ties + block_scan<NT>(key == cut.key, sh.wave_a, total);
+    if ((key > cut.key) | ((key == cut.key) & (tie < cut.ties))) {
+      const uint32_t i = atomicAdd(&sh.n_list, 1u);
+      if (i < kList) {
+        sh.list_key[i] = key;
+        sh.list_class[i] = c;
+      }
+    }
+    seen_ties += total;
+  }
+  __syncthreads();
+  write_topk<BF16, NT>(a, sh, r, row);
 }
 
 template <bool BF16>
 hipError_t launch_stats(const TokenArgs& a, hipStream_t s) {
-  const long long waves = (long long)a.n * a.S * a.units;
-  launch(stats_kernel<BF16>, dim3((unsigned)std::min<long long>((waves + 3) / 4, 1 << 20)), dim3(256), s, a);
-  return hipGetLastError();
+  const int waves = std::min(a.units, 4);
+  TokenArgs part = a;
+  for (long long row = 0; row < a.n; row += 1 << 20) {
+    part.row0 = (int)row;
+    launch(stats_kernel<BF16>, dim3((unsigned)std::min<long long>(a.n - row, 1 << 20), (a.units + waves - 1) / waves, a.S),
+           dim3(64 * waves), s, part);
+    const hipError_t st = hipGetLastError();
+    if (st != hipSuccess) return st;
+  }
+  return hipSuccess;
 }
 
-dim3 row_grid(const TokenArgs& a) { return dim3((unsigned)std::min(a.n, 1 << 20)); }
+// A workgroup per row, 2^20 rows a launch at most.
+template <typename F>
+hipError_t launch_row_kernel(F kernel, int threads, const TokenArgs& a, hipStream_t s) {
+  TokenArgs part = a;
+  for (long long row = 0; row < a.n; row += 1 << 20) {
+    part.row0 = (int)row;
+    launch(kernel, dim3((unsigned)std::min<long long>(a.n - row, 1 << 20)), dim3(threads), s, part);
+    const hipError_t st = hipGetLastError();
+    if (st != hipSuccess) return st;
+  }
+  return hipSuccess;
+}
 
 }  // namespace
 
 hipError_t launch_sample(const TokenArgs& a, bool bf16, hipStream_t s) {
-  const hipError_t st = bf16 ? launch_stats<true>(a, s) : launch_stats<false>(a, s);
+  hipError_t st = bf16 ? launch_stats<true>(a, s) : launch_stats<false>(a, s);
   if (st != hipSuccess) return st;
-  if (bf16) launch(sample_kernel<true>, row_grid(a), dim3(kRowThreads), s, a);
-  else launch(sample_kernel<false>, row_grid(a), dim3(kRowThreads), s, a);
-  return hipGetLastError();
+  st = bf16 ? launch_row_kernel(sample_kernel<true, 256>, 256, a, s) : launch_row_kernel(sample_kernel<false, 256>, 256, a, s);
+  if (st != hipSuccess || a.C <= kList) return st;           // every class fits into a list
+  if (!a.temperature && !a.top_k && !a.top_p && !a.min_p) return st;   // a unit always does
+  return bf16 ? launch_row_kernel(sample_flat_kernel<true, 1024>, 1024, a, s)
+              : launch_row_kernel(sample_flat_kernel<false, 1024>, 1024, a, s);
 }
 
 hipError_t launch_topk(const TokenArgs& a, bool bf16, hipStream_t s) {
-  const hipError_t st = bf16 ? launch_stats<true>(a, s) : launch_stats<false>(a, s);
+  hipError_t st = bf16 ? launch_stats<true>(a, s) : launch_stats<false>(a, s);
   if (st != hipSuccess) return st;
-  if (bf16) launch(topk_kernel<true>, row_grid(a), dim3(kRowThreads), s, a);
-  else launch(topk_kernel<false>, row_grid(a), dim3(kRowThreads), s, a);
-  return hipGetLastError();
+  st = bf16 ? launch_row_kernel(topk_kernel<true, 256>, 256, a, s) : launch_row_kernel(topk_kernel<false, 256>, 256, a, s);
+  if (st != hipSuccess || a.C <= kList) return st;
+  return bf16 ? launch_row_kernel(topk_flat_kernel<true, 1024>, 1024, a, s)
+              : launch_row_kernel(topk_flat_kernel<false, 1024>, 1024, a, s);
 }
 
 }  // namespace rafiki

@@ -123,6 +123,18 @@ def test_sample_ties_are_cut_by_index():
     assert np.allclose(host(probs), [1 / 7, 1 / 1000, 1 / 2048, 1 / 1024, 1, 1 / 1024, 1 / 4096, 1], rtol=2.0 ** -23, atol=0)
 
 
+def test_sample_greedy_rows_of_equal_classes():
+    """More equal first classes than any list holds: the lowest index, with and without filters."""
+    z = torch.zeros((2, 3, 5000), device=DEV)
+    z[:, 1, :7] = -1.0
+    z[:, 2] = -math.inf
+    z[:, 2, 1234:4000] = 2.0
+    for par in ({}, {"top_k": np.int32([50] * 3)}, {"top_p": np.float32([0.0] * 3)}):
+        par = {"uniform": np.float32([0.9] * 3), "temperature": np.float32([0] * 3), **par}
+        labels, probs = run_sample(z, par)
+        assert host(labels).tolist() == [0, 7, 1234] and host(probs).tolist() == [1, 1, 1]
+
+
 def test_sample_special_rows():
     lowest = float(torch.finfo(torch.float32).min)
     C = 500

@@ -25,8 +25,10 @@ namespace {
 typedef unsigned long long u64;
 
 constexpr int kList = 1024;                                // classes sorted in LDS
-constexpr int kBins = 2048;
-constexpr int kMaxGroupsListed = 4096;
+constexpr int kBins = 2048;                                // of the bound's histogram
+constexpr int kFlatBins = 4096;                            // of select()'s
+constexpr int kMaxUnits = kMaxTokenClasses / kUnitClasses;
+constexpr int kMaxGroupsListed = 2 * kMaxUnits;
 constexpr double kUnit = 4611686018427387904.0;            // 2^62
 constexpr u64 kLeastKey = (u64)(1023 - 1000) << 52;         // bits of 2^-1000
 // Scores (log2 p in fp32) are compared with this much slack: they are within 2^-10 of log2 p
@@ -183,18 +185,22 @@ __global__ __launch_bounds__(256) void stats_kernel(TokenArgs a) {
 }
 
 // ---------------------------------------------------------------- one workgroup per row
+template <bool FLAT>
 struct RowShared {
   float top[kMaxTokenModels];       // M_m
   double scale[kMaxTokenModels];    // 1 / (S s_m)
   float log_scale[kMaxTokenModels]; // log2 of it
   int state;                        // as init() returns
-  u64 sums[kBins];                  // histogram; also the listed groups, and the units' masses
-  uint32_t counts[kBins];
+  u64 sums[FLAT ? kFlatBins : kMaxUnits];   // the listed groups, the units' masses, units in a draw; FLAT: a histogram
+  union {
+    uint32_t counts[FLAT ? kFlatBins : kBins];
+    u64 run_key[kList];             // sorted runs; sums of units along the list
+  };
   u64 wave_a[16], wave_b[16];
   u64 found_a, found_b, found_c;
   int found_class;
-  uint32_t n_groups, n_list, overflow;
-  u64 list_key[kList], run_key[kList];
+  uint32_t n_groups, n_list;
+  u64 list_key[kList];
   int list_class[kList], run_class[kList];
 };
 
@@ -257,11 +263,11 @@ struct Cut {
   u64 key, ties, mass;
 };
 
-template <bool BF16, int NT>
+template <bool BF16, int NT, bool FLAT>
 struct Row {
   static constexpr int kWaves = NT / 64;
   const TokenArgs& a;
-  RowShared& sh;
+  RowShared<FLAT>& sh;
   int row;
   double k;
 
@@ -306,15 +312,35 @@ struct Row {
     return (u64)(p * kUnit);
   }
 
-  // Bits of p_c (they order as p_c does), 0 for a class without a probability.
-  __device__ __forceinline__ u64 key(int c) const {
-    const long long at = row * a.ld_row + c;
-    double p = 0.0;
+  // Bits of p_c (they order as p_c does) of N classes, 0 for one without a probability or past the row's end:
+  // one model's N logits are in flight together.
+  template <int N>
+  __device__ __forceinline__ void keys(const int (&c)[N], u64 (&x)[N]) const {
+    double p[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] = 0.0;
 #pragma unroll 1
-    for (int m = 0; m < a.S; ++m)
-      p = __builtin_fma(weight(logit<BF16>(a.logits, at + m * a.ld_model), sh.top[m], k), sh.scale[m], p);
-    const u64 bits = (u64)__double_as_longlong(p);
-    return bits < kLeastKey ? 0 : bits;
+    for (int m = 0; m < a.S; ++m) {
+      const long long at = row * a.ld_row + m * a.ld_model;
+      float z[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) z[i] = c[i] < a.C ? logit<BF16>(a.logits, at + c[i]) : -INFINITY;
+      const float top = sh.top[m];
+      const double scale = sh.scale[m];
+#pragma unroll
+      for (int i = 0; i < N; ++i) p[i] = __builtin_fma(weight(z[i], top, k), scale, p[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const u64 bits = (u64)__double_as_longlong(p[i]);
+      x[i] = bits < kLeastKey ? 0 : bits;
+    }
+  }
+  __device__ __forceinline__ u64 key(int c) const {
+    const int one[1] = {c};
+    u64 x[1];
+    keys<1>(one, x);
+    return x[0];
   }
 
   // This lane's 16 logits of one model of unit u, as stats_kernel holds them, and the class of the i-th.
@@ -413,7 +439,7 @@ struct Row {
     const int lane = threadIdx.x & 63;
     uint32_t* groups = (uint32_t*)sh.sums;
     __syncthreads();
-    if (threadIdx.x == 0) sh.n_groups = sh.n_list = sh.overflow = 0;
+    if (threadIdx.x == 0) sh.n_groups = sh.n_list = 0;
     __syncthreads();
     const int n = (a.C + 63) / 64;
     for (int g = threadIdx.x; g < n; g += NT) {
@@ -428,17 +454,25 @@ struct Row {
     const int listed = (int)sh.n_groups;
     if (listed > kMaxGroupsListed) return false;
     const u64 least = score > -1000.f ? (u64)__double_as_longlong((double)exp2f(fmaxf(score - kSlack, -120.f))) : 1;
-    for (int i = threadIdx.x >> 6; i < listed; i += kWaves) {
-      const int c = (int)groups[i] * 64 + lane;
-      const u64 x = c < a.C ? key(c) : 0;
-      const bool take = x >= (score > -120.f ? least : 1);
-      const u64 who = __ballot(take);
-      uint32_t at = 0;
-      if (lane == 0 && who) at = atomicAdd(&sh.n_list, (uint32_t)__popcll(who));
-      at = __shfl(at, 0, 64) + __popcll(who & (((u64)1 << lane) - 1));
-      if (take && at < kList) {
-        sh.list_key[at] = x;
-        sh.list_class[at] = c;
+    constexpr int AT_ONCE = 8;                               // groups of a wave in flight
+    for (int i = (threadIdx.x >> 6) * AT_ONCE; i < listed; i += kWaves * AT_ONCE) {
+      int c[AT_ONCE];
+      u64 x[AT_ONCE];
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j) c[j] = i + j < listed ? (int)groups[i + j] * 64 + lane : a.C;
+      keys<AT_ONCE>(c, x);
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j) {
+        const bool take = x[j] >= (score > -120.f ? least : 1);
+        const u64 who = __ballot(take);
+        if (!who) continue;
+        uint32_t at = 0;
+        if (lane == 0) at = atomicAdd(&sh.n_list, (uint32_t)__popcll(who));
+        at = __shfl(at, 0, 64) + __popcll(who & (((u64)1 << lane) - 1));
+        if (take && at < kList) {
+          sh.list_key[at] = x[j];
+          sh.list_class[at] = c[j];
+        }
       }
     }
     __syncthreads();
@@ -543,21 +577,21 @@ struct Row {
   }
 
   // The cut at which the number (by_sum: the sum of the units) of the classes from the top reaches
-  // `target`, by histograms of the bits of p: 32 bins an octave from 1 down first (whole: of
+  // `target`, by histograms of the bits of p: 64 bins an octave from 1 down first (whole: of
   // all the octaves), then 11 bits a level within the bin reached, until its classes fit into the
   // list and are sorted.  False where all classes (those above 2^-63, which have units) stay
   // below target.
   __device__ bool select(bool by_sum, u64 target, bool whole, Cut& cut) {
-    constexpr u64 first_bin = (u64)1023 << 5;                 // bits of 1.0 >> 47
+    constexpr u64 first_bin = (u64)1023 << 6;                 // bits of 1.0 >> 46
     u64 prefix_bits = 0, above_n = 0, above_sum = 0;
-    int shift = whole ? 52 : 47, up = 64;
+    int shift = whole ? 52 : 46, up = 64;
     for (;;) {
       __syncthreads();
-      for (int b = threadIdx.x; b < kBins; b += NT) {
+      for (int b = threadIdx.x; b < kFlatBins; b += NT) {
         sh.sums[b] = 0;
         sh.counts[b] = 0;
       }
-      if (threadIdx.x == 0) sh.found_a = kBins;
+      if (threadIdx.x == 0) sh.found_a = kFlatBins;
       __syncthreads();
       // bins ascend as keys descend
       const u64 top_bin = up == 64 ? (whole ? 2047 : first_bin) : (prefix_bits >> shift) | (((u64)1 << (up - shift)) - 1);
@@ -568,13 +602,13 @@ struct Row {
         for (int i = 0; i < 16; ++i)
           if (x[i] != 0 && (up == 64 || x[i] >> up == prefix_bits >> up)) {
             const u64 below = top_bin - (x[i] >> shift);
-            const int b = (x[i] >> shift) > top_bin ? 0 : below < kBins - 1 ? (int)below : kBins - 1;
+            const int b = (x[i] >> shift) > top_bin ? 0 : below < kFlatBins - 1 ? (int)below : kFlatBins - 1;
             atomicAdd(&sh.sums[b], units_of(x[i]));
-            atomicAdd(&sh.counts[b], 1u);
+            if (!by_sum) atomicAdd(&sh.counts[b], 1u);
           }
       }
       __syncthreads();
-      constexpr int PER = kBins / NT;
+      constexpr int PER = kFlatBins / NT;
       u64 n = 0, s = 0, total_n, total_s;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
@@ -595,17 +629,20 @@ struct Row {
       }
       __syncthreads();
       const int b = (int)sh.found_a;
-      if (b == kBins) return false;
-      if (up == 64 && !whole && b == kBins - 1) return false;         // beyond 63 octaves
+      if (b == kFlatBins) return false;
+      if (up == 64 && !whole && b == kFlatBins - 1) return false;         // beyond 63 octaves
       prefix_bits = (top_bin - b) << shift;
       above_n = sh.found_b;
       above_sum = sh.found_c;
-      const int count = (int)sh.counts[b];
-      if (count <= kList) {
+      bool fits = by_sum || sh.counts[b] <= kList;
+      if (fits) {
         list_prefix(prefix_bits, shift);
+        fits = sh.n_list <= kList;
+      }
+      if (fits) {
         sort();
         accumulate();
-        const int r = by_sum ? reach(count, target - above_sum) : (int)(target - above_n);
+        const int r = by_sum ? reach((int)sh.n_list, target - above_sum) : (int)(target - above_n);
         cut.key = sh.list_key[r - 1];
         cut.mass = above_sum + sh.run_key[r - 1];
         __syncthreads();
@@ -639,7 +676,7 @@ struct Row {
     // with one model the logits themselves tell which classes may be there
     float lo = -INFINITY, hi = INFINITY;
     if (a.S == 1) {
-      const float span = shift > 47 ? 1.f : 1.f / 16;         // log2(33 / 32) at most
+      const float span = shift > 46 ? 1.f : 1.f / 32;         // log2(65 / 64) at most
       lo = log2f((float)__longlong_as_double((long long)prefix_bits)) - kSlack;
       hi = lo + span + 2 * kSlack;
       if (!(lo > -120.f)) lo = -INFINITY, hi = INFINITY;
@@ -760,12 +797,12 @@ struct Row {
   __device__ bool draw_in_unit(int c0, u64 target, u64 cut, u64 ties, u64 mass, float u) {
     constexpr int PER = kUnitClasses / NT;
     u64 x[PER], equal = 0, part = 0, total;
+    int c[PER];
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int c = c0 + threadIdx.x * PER + j;
-      x[j] = c < a.C ? key(c) : 0;
-      equal += x[j] == cut;
-    }
+    for (int j = 0; j < PER; ++j) c[j] = c0 + threadIdx.x * PER + j;
+    keys<PER>(c, x);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) equal += x[j] == cut;
     u64 tie = block_scan<NT>(equal, sh.wave_a, total);
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -823,10 +860,10 @@ __device__ __forceinline__ Filters row_filters(const TokenArgs& a, int row, floa
 // because a row's time is mostly that of fetching the code it runs through once.
 template <bool BF16, int NT>
 __global__ __launch_bounds__(NT) void sample_kernel(TokenArgs a) {
-  __shared__ RowShared sh;
+  __shared__ RowShared<false> sh;
   const int row = a.row0 + blockIdx.x;
   const float t = row_temperature(a, row);
-  Row<BF16, NT> r{a, sh, row, log2_scale(t)};
+  Row<BF16, NT, false> r{a, sh, row, log2_scale(t)};
   const int state = t >= 0.f ? r.init() : 2;
   if (threadIdx.x == 0) a.flat[row] = 0;
   if (state != 0) {
@@ -886,11 +923,11 @@ __global__ __launch_bounds__(NT) void sample_kernel(TokenArgs a) {
 // Rows with more kept classes than a list holds: cut by histograms, then a scan of the units.
 template <bool BF16, int NT>
 __global__ __launch_bounds__(NT, 4) void sample_flat_kernel(TokenArgs a) {
-  __shared__ RowShared sh;
+  __shared__ RowShared<true> sh;
   const int row = a.row0 + blockIdx.x;
   if (!a.flat[row]) return;
   const float t = row_temperature(a, row);
-  Row<BF16, NT> r{a, sh, row, log2_scale(t)};
+  Row<BF16, NT, true> r{a, sh, row, log2_scale(t)};
   r.init();
   const Filters f = row_filters(a, row, t);
   Cut cut{1, ~(u64)0, r.unit_masses()};
@@ -949,8 +986,8 @@ __global__ __launch_bounds__(NT, 4) void sample_flat_kernel(TokenArgs a) {
 }
 
 // Sorts the list of a row's first classes and writes it.
-template <bool BF16, int NT>
-__device__ __forceinline__ void write_topk(const TokenArgs& a, RowShared& sh, Row<BF16, NT>& r, int row) {
+template <bool BF16, int NT, bool FLAT>
+__device__ __forceinline__ void write_topk(const TokenArgs& a, RowShared<FLAT>& sh, Row<BF16, NT, FLAT>& r, int row) {
   r.sort();
   const int n = (int)sh.n_list;
   for (int j = threadIdx.x; j < a.k; j += NT) {
@@ -962,9 +999,9 @@ __device__ __forceinline__ void write_topk(const TokenArgs& a, RowShared& sh, Ro
 
 template <bool BF16, int NT>
 __global__ __launch_bounds__(NT) void topk_kernel(TokenArgs a) {
-  __shared__ RowShared sh;
+  __shared__ RowShared<false> sh;
   const int row = a.row0 + blockIdx.x;
-  Row<BF16, NT> r{a, sh, row, log2_scale(a.t_all)};
+  Row<BF16, NT, false> r{a, sh, row, log2_scale(a.t_all)};
   const int state = r.init();
   const bool listed = state != 0 || r.list(r.bound(a.k, r.best_score()));
   if (threadIdx.x == 0) a.flat[row] = !listed;
@@ -974,7 +1011,7 @@ __global__ __launch_bounds__(NT) void topk_kernel(TokenArgs a) {
       a.out[(long long)row * a.k + j] = state == 1 ? -INFINITY : NAN;
     }
   } else if (listed) {
-    write_topk<BF16, NT>(a, sh, r, row);
+    write_topk(a, sh, r, row);
   }
 }
 
@@ -982,10 +1019,10 @@ __global__ __launch_bounds__(NT) void topk_kernel(TokenArgs a) {
 // list is then the classes above it and the first ties.
 template <bool BF16, int NT>
 __global__ __launch_bounds__(NT, 4) void topk_flat_kernel(TokenArgs a) {
-  __shared__ RowShared sh;
+  __shared__ RowShared<true> sh;
   const int row = a.row0 + blockIdx.x;
   if (!a.flat[row]) return;
-  Row<BF16, NT> r{a, sh, row, log2_scale(a.t_all)};
+  Row<BF16, NT, true> r{a, sh, row, log2_scale(a.t_all)};
   r.init();
   Cut cut{1, ~(u64)0, 0};
   r.select(false, (u64)a.k, true, cut);
@@ -1008,7 +1045,7 @@ __global__ __launch_bounds__(NT, 4) void topk_flat_kernel(TokenArgs a) {
     seen_ties += total;
   }
   __syncthreads();
-  write_topk<BF16, NT>(a, sh, r, row);
+  write_topk(a, sh, r, row);
 }
 
 template <bool BF16>

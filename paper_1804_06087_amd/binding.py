@@ -8,6 +8,7 @@ library is missing the binding raises instead of falling back to anything else.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import List, Optional, Sequence
 
@@ -493,9 +494,20 @@ def _dtype_code(t, name):
 
 def _rows(t, name):
     """Distance between the rows of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"{name}: expected a matrix with contiguous rows, got {tuple(t.shape)} with strides {t.stride()}")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{name}: expected a matrix with contiguous rows, got {tuple(shape)} with strides {stride}")
+    return stride[0] if shape[0] > 1 else max(stride[0], shape[1])
+
+
+def _vector(t, n, dtype, device, name):
+    """Device pointer of a contiguous vector of n values on ``device`` (0 for None)."""
+    if t is None:
+        return 0
+    if t.dtype != dtype or t.shape != (n,) or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor ({n},) of {dtype} on {device}, got {tuple(t.shape)} "
+                         f"{t.dtype} on {t.device}{'' if t.is_contiguous() else ' (not contiguous)'}")
+    return t.data_ptr()
 
 
 def _same_device(first, *others):
@@ -509,36 +521,43 @@ def _call(first, stream, need, workspace, fn, *args):
     that device), with a workspace of ``need`` bytes where it takes one (need None: it does not).  A workspace
     that is not given is taken from torch's allocator for the time of the work."""
     import torch
-    if torch.cuda.current_device() != first.device.index:
-        with torch.cuda.device(first.device):
+    index = first.device.index
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
             return _call(first, stream, need, workspace, fn, *args)
-    if not isinstance(stream, (int, type(None))) and stream.device != first.device:
-        raise ValueError(f"stream of {stream.device}, tensors on {first.device}")
-    handle = _stream(stream)
+    if stream is None:
+        handle = torch._C._cuda_getCurrentRawStream(index)
+    else:
+        if not isinstance(stream, int) and stream.device != first.device:
+            raise ValueError(f"stream of {stream.device}, tensors on {first.device}")
+        handle = _stream(stream)
     if need is None:
         return _check(fn(*args, handle))
     if workspace is not None:
         if not workspace.is_cuda or not workspace.is_contiguous():
             raise ValueError("workspace: expected a contiguous device tensor")
         _same_device(first, workspace)
-    elif need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=first.device)
-        if stream is not None:          # allocated for the current stream: kept until `stream` has passed
-            workspace.record_stream(torch.cuda.ExternalStream(handle, device=first.device))
-    return _check(fn(*args, _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                     handle))
+        return _check(fn(*args, workspace.data_ptr(), workspace.numel() * workspace.element_size(), handle))
+    if not need:
+        return _check(fn(*args, 0, 0, handle))
+    workspace = torch.empty(need, dtype=torch.uint8, device=first.device)
+    if stream is not None:              # allocated for the current stream: kept until `stream` has passed
+        workspace.record_stream(torch.cuda.ExternalStream(handle, device=first.device))
+    return _check(fn(*args, workspace.data_ptr(), need, handle))
 
 
 def _model_rows(logits):
     """[S, n, C] (or [n, C]: one model) with contiguous rows -> (S, n, C, ld_model, ld_row)."""
-    if logits.dim() == 2:
-        logits = logits.unsqueeze(0)
-    if logits.dim() != 3 or (logits.stride(2) != 1 and logits.shape[2] > 1):
+    shape, stride = logits.shape, logits.stride()
+    if len(shape) == 2:
+        shape, stride = (1, *shape), (0, *stride)
+    if len(shape) != 3 or (stride[2] != 1 and shape[2] > 1):
         raise ValueError(f"logits: expected [S, n, C] or [n, C] with contiguous rows, got {tuple(logits.shape)} with "
                          f"strides {logits.stride()}")
-    return (*logits.shape, logits.stride(0), logits.stride(1))
+    return (*shape, stride[0], stride[1])
 
 
+@functools.lru_cache(maxsize=4096)
 def combine_workspace(n_models: int, n: int, n_classes: int) -> int:
     """Bytes of workspace of combine_sample and combine_topk."""
     b = C.c_longlong()
@@ -554,16 +573,14 @@ def combine_sample(logits, uniform, out_labels, out_probs, temperature=None, top
     import torch
     code = _dtype_code(logits, "logits")
     S, n, nc, ld_model, ld_row = _model_rows(logits)
-    for t, dt, name in ((uniform, torch.float32, "uniform"), (temperature, torch.float32, "temperature"),
-                        (top_k, torch.int32, "top_k"), (top_p, torch.float32, "top_p"),
-                        (min_p, torch.float32, "min_p"), (out_labels, torch.int32, "labels"),
-                        (out_probs, torch.float32, "probabilities")):
-        if t is not None:
-            _expect(t, (n,), dt, name)
-    _same_device(logits, uniform, temperature, top_k, top_p, min_p, out_labels, out_probs)
+    f32, dev = torch.float32, logits.device
+    if uniform is None or out_labels is None or out_probs is None:
+        raise ValueError("uniform, out_labels and out_probs are required")
     _call(logits, stream, combine_workspace(S, n, nc), workspace, load_library().rafiki_combine_sample,
-          _ptr(logits), code, ld_model, ld_row, S, n, nc, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
-          _ptr(uniform), _ptr(out_labels), _ptr(out_probs))
+          logits.data_ptr(), code, ld_model, ld_row, S, n, nc, _vector(temperature, n, f32, dev, "temperature"),
+          _vector(top_k, n, torch.int32, dev, "top_k"), _vector(top_p, n, f32, dev, "top_p"),
+          _vector(min_p, n, f32, dev, "min_p"), _vector(uniform, n, f32, dev, "uniform"),
+          _vector(out_labels, n, torch.int32, dev, "labels"), _vector(out_probs, n, f32, dev, "probabilities"))
 
 
 def combine_topk(logits, out_labels, out_logp, temperature: float = 1.0, workspace=None, stream=None):
@@ -577,7 +594,7 @@ def combine_topk(logits, out_labels, out_logp, temperature: float = 1.0, workspa
     _expect(out_logp, (n, k), torch.float32, "log-probabilities")
     _same_device(logits, out_labels, out_logp)
     _call(logits, stream, combine_workspace(S, n, nc), workspace, load_library().rafiki_combine_topk,
-          _ptr(logits), code, ld_model, ld_row, S, n, nc, temperature, k, _ptr(out_labels), _ptr(out_logp))
+          logits.data_ptr(), code, ld_model, ld_row, S, n, nc, temperature, k, out_labels.data_ptr(), out_logp.data_ptr())
 
 
 def distill_loss(logits, teacher_labels, teacher_logp, out_loss=None, grad_logits=None, grad_loss=None,
@@ -592,17 +609,16 @@ def distill_loss(logits, teacher_labels, teacher_logp, out_loss=None, grad_logit
     k = teacher_labels.shape[-1]
     _expect(teacher_labels, (n, k), torch.int32, "teacher_labels")
     _expect(teacher_logp, (n, k), torch.float32, "teacher_logp")
-    for t, name in ((out_loss, "loss"), (grad_loss, "grad_loss")):
-        if t is not None:
-            _expect(t, (n,), torch.float32, name)
+    loss_at = _vector(out_loss, n, torch.float32, logits.device, "loss")
+    weight_at = _vector(grad_loss, n, torch.float32, logits.device, "grad_loss")
     ld_grad = 0
     if grad_logits is not None:
         if grad_logits.shape != logits.shape or grad_logits.dtype != logits.dtype:
             raise ValueError("grad_logits: expected the shape and dtype of the logits")
         ld_grad = _rows(grad_logits, "grad_logits")
-    _same_device(logits, teacher_labels, teacher_logp, out_loss, grad_logits, grad_loss)
-    _call(logits, stream, None, None, load_library().rafiki_distill_loss, _ptr(logits), code, ld_row, n, nc,
-          _ptr(teacher_labels), _ptr(teacher_logp), k, temperature, 1 if rest else 0, _ptr(grad_loss), _ptr(out_loss),
+    _same_device(logits, teacher_labels, teacher_logp, grad_logits)
+    _call(logits, stream, None, None, load_library().rafiki_distill_loss, logits.data_ptr(), code, ld_row, n, nc,
+          teacher_labels.data_ptr(), teacher_logp.data_ptr(), k, temperature, 1 if rest else 0, weight_at, loss_at,
           _ptr(grad_logits), ld_grad)
 
 
@@ -613,12 +629,14 @@ def quantize_rows_i8(x, q, scale, stream=None):
     ld_x, ld_q = _rows(x, "x"), _rows(q, "q")
     if q.shape != x.shape or q.dtype != torch.int8:
         raise ValueError("q: expected int8 of the shape of x")
-    _expect(scale, (x.shape[0],), torch.float32, "scale")
-    _same_device(x, q, scale)
-    _call(x, stream, None, None, load_library().rafiki_quantize_rows_i8, _ptr(x), code, ld_x, *x.shape, _ptr(q), ld_q,
-          _ptr(scale))
+    if scale is None:
+        raise ValueError("scale is required")
+    _same_device(x, q)
+    _call(x, stream, None, None, load_library().rafiki_quantize_rows_i8, x.data_ptr(), code, ld_x, *x.shape, q.data_ptr(),
+          ld_q, _vector(scale, x.shape[0], torch.float32, x.device, "scale"))
 
 
+@functools.lru_cache(maxsize=4096)
 def fc_i8_workspace(n: int, c_in: int, c_out: int) -> int:
     """Bytes of workspace of fc_i8."""
     b = C.c_longlong()
@@ -641,13 +659,14 @@ def fc_i8(x, x_scale, w, w_scale, y, bias=None, relu: bool = False, workspace=No
         end = t.storage_offset() + (t.shape[0] - 1) * ld + (c_in + 15) // 16 * 16
         if end > t.untyped_storage().nbytes():
             raise ValueError(f"{name}: the last row is not readable up to the next multiple of 16")
-    _expect(x_scale, (n,), torch.float32, "x_scale")
-    _expect(w_scale, (c_out,), torch.float32, "w_scale")
-    if bias is not None:
-        _expect(bias, (c_out,), torch.float32, "bias")
-    _same_device(x, x_scale, w, w_scale, y, bias)
-    _call(y, stream, fc_i8_workspace(n, c_in, c_out), workspace, load_library().rafiki_fc_i8, _ptr(x), ld_x,
-          _ptr(x_scale), _ptr(w), ld_w, _ptr(w_scale), _ptr(bias), n, c_in, c_out, 1 if relu else 0, _ptr(y), code, ld_y)
+    if x_scale is None or w_scale is None:
+        raise ValueError("x_scale and w_scale are required")
+    _same_device(y, x, w)
+    f32 = torch.float32
+    _call(y, stream, fc_i8_workspace(n, c_in, c_out), workspace, load_library().rafiki_fc_i8, x.data_ptr(), ld_x,
+          _vector(x_scale, n, f32, y.device, "x_scale"), w.data_ptr(), ld_w,
+          _vector(w_scale, c_out, f32, y.device, "w_scale"), _vector(bias, c_out, f32, y.device, "bias"), n, c_in, c_out,
+          1 if relu else 0, y.data_ptr(), code, ld_y)
 
 
 def tile_configs():

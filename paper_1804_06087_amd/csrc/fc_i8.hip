@@ -403,19 +403,105 @@ __global__ __launch_bounds__(WM * WN * 64, OCC) void fc_i8_tile_kernel(FcI8Args 
   }
 }
 
-// Joins the splits' sums: a thread per output.
-__global__ __launch_bounds__(256) void fc_i8_reduce_kernel(FcI8Args a, int splits) {
-  const long long total = (long long)a.n * a.c_out;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
-    const int row = (int)(i / a.c_out), o = (int)(i - (long long)row * a.c_out);
-    int acc = 0;
-    for (int s = 0; s < splits; ++s) acc += a.partial[s * total + i];
-    const float v = finish(acc, a.sx[row] * a.sw[o], a.bias ? a.bias[o] : 0.f, a.relu);
-    if (a.out_bf16) ((__bf16*)a.y)[row * a.ld_y + o] = (__bf16)v;
-    else ((float*)a.y)[row * a.ld_y + o] = v;
+// 16 bytes of a row from k on; chunks behind the row's last are 0, and bytes behind c_in.
+__device__ __forceinline__ i32x4 x_chunk(const int8_t* p, int k, int c_in) {
+  i32x4 v = {0, 0, 0, 0};
+  if (k < c_in) v = *(const i32x4*)(p + k);
+  if (k + 16 > c_in) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int left = c_in - (k + 4 * i);
+      v[i] = left <= 0 ? 0 : left < 4 ? v[i] & ((1 << (8 * left)) - 1) : v[i];
+    }
+  }
+  return v;
+}
+
+// Few rows (up to 16 NB): one launch whose bound is the bytes of w, each read once, by one wave, without LDS.
+// A workgroup takes 16 rows of w and its WAVES waves the 64-byte steps of K in turn, UNROLL steps in flight;
+// v_mfma_i32_16x16x64_i8 sums them (lane l holds 16 bytes from 16 (l / 16) of row l % 16 of either operand,
+// and outputs 4 (l / 16) .. + 3 of w's rows for row l % 16 of x), and the waves' sums meet in LDS.
+template <int NB, int WAVES, int UNROLL>
+__global__ __launch_bounds__(WAVES * 64) void fc_i8_rows_kernel(FcI8Args a) {
+  __shared__ int4 sums[WAVES][NB][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int o0 = blockIdx.x * 16, r = lane & 15, q = lane >> 4;
+  const int8_t* wp = a.w + min(o0 + r, a.c_out - 1) * a.ld_w;
+  const int8_t* xp[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) xp[b] = a.x + min(b * 16 + r, a.n - 1) * a.ld_x;
+  i32x4 acc[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) acc[b] = i32x4{0, 0, 0, 0};
+  const int steps = (a.c_in + 63) / 64;
+  for (int s0 = wave; s0 < steps; s0 += WAVES * UNROLL) {
+    i32x4 w[UNROLL], x[UNROLL][NB];
+#pragma unroll
+    for (int i = 0; i < UNROLL; ++i) {
+      const int k = (s0 + i * WAVES) * 64 + q * 16;
+      w[i] = i32x4{0, 0, 0, 0};
+      if (k < a.c_in) w[i] = __builtin_nontemporal_load((const i32x4*)(wp + k));
+#pragma unroll
+      for (int b = 0; b < NB; ++b) x[i][b] = x_chunk(xp[b], k, a.c_in);
+    }
+#pragma unroll
+    for (int i = 0; i < UNROLL; ++i)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i], x[i][b], acc[b], 0, 0, 0);
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b) sums[wave][b][lane] = make_int4(acc[b][0], acc[b][1], acc[b][2], acc[b][3]);
+  __syncthreads();
+  for (int t = threadIdx.x; t < NB * 64; t += WAVES * 64) {
+    const int b = t >> 6, l = t & 63;
+    int v[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const int4 p = sums[w][b][l];
+      v[0] += p.x;
+      v[1] += p.y;
+      v[2] += p.z;
+      v[3] += p.w;
+    }
+    const int row = b * 16 + (l & 15), o = o0 + 4 * (l >> 4);
+    if (row >= a.n) continue;
+    const float sx = a.sx[row];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (o + j >= a.c_out) continue;
+      const float f = finish(v[j], sx * a.sw[o + j], a.bias ? a.bias[o + j] : 0.f, a.relu);
+      if (a.out_bf16) ((__bf16*)a.y)[row * a.ld_y + o + j] = (__bf16)f;
+      else ((float*)a.y)[row * a.ld_y + o + j] = f;
+    }
   }
 }
 
+// Joins the splits' sums: a thread per 4 outputs of a row.
+__global__ __launch_bounds__(256) void fc_i8_reduce_kernel(FcI8Args a, int splits) {
+  const int quads = (a.c_out + 3) / 4;
+  const long long total = (long long)a.n * quads, plane = (long long)a.n * a.c_out;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
+    const int row = (int)(total >> 32 ? i / quads : (uint32_t)i / (uint32_t)quads), o = (int)(i - (long long)row * quads) * 4;
+    const int* p = a.partial + (long long)row * a.c_out + o;
+    i32x4 acc = {0, 0, 0, 0};
+    if (o + 4 <= a.c_out) {
+#pragma unroll 4
+      for (int s = 0; s < splits; ++s) acc += *(const i32x4_any*)(p + s * plane);
+    } else {
+      for (int s = 0; s < splits; ++s)
+#pragma unroll
+        for (int j = 0; j < 3; ++j) acc[j] += o + j < a.c_out ? p[s * plane + j] : 0;
+    }
+    const float sx = a.sx[row];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (o + j >= a.c_out) continue;
+      const float v = finish(acc[j], sx * a.sw[o + j], a.bias ? a.bias[o + j] : 0.f, a.relu);
+      if (a.out_bf16) ((__bf16*)a.y)[row * a.ld_y + o + j] = (__bf16)v;
+      else ((float*)a.y)[row * a.ld_y + o + j] = v;
+    }
+  }
+}
 
 template <bool BF16, int NT, int CH>
 hipError_t launch_quantize_rows(const void* x, long long ld_x, int n, int c, int8_t* q, long long ld_q, float* scale,
@@ -451,7 +537,7 @@ hipError_t launch_quantize(const void* x, bool bf16, long long ld_x, int n, int 
 struct FcConfig {
   int bm, bn, per_cu;        // workgroups that fit on a compute unit
 };
-constexpr FcConfig kConfigs[] = {{256, 256, 1}, {128, 128, 2}, {64, 128, 2}, {32, 128, 2}};
+constexpr FcConfig kConfigs[] = {{256, 256, 1}, {128, 128, 2}, {64, 128, 2}};
 
 struct FcPlan {
   int cfg, splits, kt_per_split;
@@ -460,7 +546,7 @@ struct FcPlan {
 FcPlan plan_fc(int n, int c_in, int c_out) {
   const int ktiles = (c_in + 127) / 128;
   FcPlan best{0, 1, ktiles};
-  int cfg = n > 128 ? 0 : n > 64 ? 1 : n > 32 ? 2 : 3;
+  int cfg = n > 128 ? 0 : n > 64 ? 1 : 2;
   auto tiles = [&](int c) {
     return (long long)((n + kConfigs[c].bm - 1) / kConfigs[c].bm) * ((c_out + kConfigs[c].bn - 1) / kConfigs[c].bn);
   };
@@ -481,24 +567,33 @@ hipError_t launch_tile(const FcI8Args& a, int splits, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Rows that fc_i8_rows_kernel takes: its waves read x again for every 16 outputs.
+constexpr int kFewRows = 32;
+
 long long fc_i8_workspace_bytes(int n, int c_in, int c_out) {
+  if (n <= kFewRows) return 0;
   const FcPlan p = plan_fc(n, c_in, c_out);
   return p.splits > 1 ? (long long)p.splits * n * c_out * 4 : 0;
 }
 
 hipError_t launch_fc_i8(const FcI8Args& args, hipStream_t s) {
   FcI8Args a = args;
+  if (a.n <= kFewRows) {
+    const dim3 grid((a.c_out + 15) / 16);
+    if (a.n <= 16) launch(fc_i8_rows_kernel<1, 8, 4>, grid, dim3(512), s, a);
+    else launch(fc_i8_rows_kernel<2, 8, 4>, grid, dim3(512), s, a);
+    return hipGetLastError();
+  }
   const FcPlan p = plan_fc(a.n, a.c_in, a.c_out);
   a.kt_per_split = p.kt_per_split;
   hipError_t st;
   switch (p.cfg) {
     case 0: st = launch_tile<256, 256, 2, 4, 2, 2>(a, p.splits, s); break;
     case 1: st = launch_tile<128, 128, 2, 2, 2, 2>(a, p.splits, s); break;
-    case 2: st = launch_tile<64, 128, 1, 4, 3, 2>(a, p.splits, s); break;
-    default: st = launch_tile<32, 128, 1, 4, 3, 2>(a, p.splits, s); break;
+    default: st = launch_tile<64, 128, 1, 4, 3, 2>(a, p.splits, s); break;
   }
   if (st != hipSuccess || p.splits == 1) return st;
-  const long long total = (long long)a.n * a.c_out;
+  const long long total = (long long)a.n * ((a.c_out + 3) / 4);
   launch(fc_i8_reduce_kernel, dim3((unsigned)std::min<long long>((total + 255) / 256, 1 << 16)), dim3(256), s, a, p.splits);
   return hipGetLastError();
 }

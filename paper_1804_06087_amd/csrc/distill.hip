@@ -79,11 +79,19 @@ __device__ __forceinline__ float wave_add(float v) {
   return v;
 }
 
+// A barrier for what goes through LDS alone: __syncthreads() would also wait for every load from memory.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);                        // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // The maximum as a reference for powers: an empty row has none and takes 0.
 __device__ __forceinline__ float reference(float top) { return top == -INFINITY ? 0.f : top; }
 
 // NT threads hold a row of up to NT CH + 2 chunks, the two edges among them (CH = 0: any length, not held).
-template <bool BF16, int NT, int CH, int OCC>
+template <bool BF16, bool REST, int NT, int CH, int OCC>
 __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
   constexpr int V = BF16 ? 8 : 4, NW = NT / 64;
   extern __shared__ uint32_t marks[];                        // rest: bit c + shift is set for c in K
@@ -185,7 +193,7 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
       }
     } else {
       for (int i = 0; i * NT + tid + 1 < chunks - 1; ++i) {
-        unpack<BF16, V>(a.rest ? without_members(load(i), (i * NT + tid + 1) * V) : load(i), z);
+        unpack<BF16, V>(REST ? without_members(load(i), (i * NT + tid + 1) * V) : load(i), z);
         f(z, kAll, [&](const float* d) { store(i, d); });
       }
     }
@@ -202,11 +210,11 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
     ids[j] = valid ? id : -1;
     slot_q[j] = valid ? a.logp[(long long)row * a.k + j] : -INFINITY;
   }
-  if (a.rest)
+  if (REST)
     for (int w = tid; w < (chunks * V + 31) / 32 + 1; w += NT) marks[w] = 0;
-  __syncthreads();
+  lds_barrier();
   float t_top = 0.f, t_sum = 1.f;                          // rest = 0: q = 2^(..) / sum, in every wave
-  if (!a.rest) {
+  if (!REST) {
     t_top = -INFINITY;
     for (int j = lane; j < a.k; j += 64) t_top = fmaxf(t_top, slot_q[j]);
     t_top = reference(wave_max(t_top));
@@ -219,14 +227,14 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
       return;
     }
   }
-  __syncthreads();
+  lds_barrier();
   for (int j = tid; j < a.k; j += NT) {
     const int id = ids[j];
     slot_q[j] = expf(slot_q[j] - t_top) / t_sum;
-    if (a.rest && id >= 0) atomicOr(&marks[(id + shift) >> 5], 1u << ((id + shift) & 31));
+    if (REST && id >= 0) atomicOr(&marks[(id + shift) >> 5], 1u << ((id + shift) & 31));
   }
-  __syncthreads();
-  if (a.rest) {
+  lds_barrier();
+  if (REST) {
     if constexpr (CH > 0) {
 #pragma unroll
       for (int i = 0; i < CH; ++i)
@@ -263,23 +271,43 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
     }
   }
 
-  // ---- maxima, then sums of powers
-  float top = -INFINITY;
-  for_chunks([&](const float* z, uint32_t, auto&&) {
+  // ---- maxima and sums of powers, in one pass: a thread's sum follows its maximum, so that it grows while the row
+  // is still arriving (with a pass for the maximum first, loading, computing and storing took turns on all
+  // compute units at once, 339 us for 2047 x 131071)
+  float top = -INFINITY, sum = 0.f;
+  for_chunks([&](const float* z, uint32_t own, auto&&) {
+    float now = top;
 #pragma unroll
-    for (int j = 0; j < V; ++j) top = fmaxf(top, z[j]);
+    for (int j = 0; j < V; ++j) now = fmaxf(now, z[j]);
+    const float off = -reference(now) * s;
+    sum *= power2(__builtin_fmaf(top, s, off));
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum += own >> j & 1 ? power2(__builtin_fmaf(z[j], s, off)) : 0.f;
+    top = now;
   });
-  top = wave_max(top);
-  member_top = wave_max(member_top);
+  // the wave's, then the workgroup's
+  auto join = [&](float& t, float& v) {
+    const float all = wave_max(t);
+    v = wave_add(v * power2(__builtin_fmaf(t, s, -reference(all) * s)));
+    t = all;
+  };
+  join(top, sum);
+  float member_sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < SLOTS; ++i)
+    if (q_class[i] >= 0.f || q_class[i] != q_class[i]) member_sum += power2(__builtin_fmaf(z_class[i], s, -reference(member_top) * s));
+  join(member_top, member_sum);
   members = wave_add(members);
   q_sum = wave_add(q_sum);
   if (lane == 0) {
     w_top[wave] = top;
+    w_sum[wave] = sum;
     w_member_top[wave] = member_top;
+    w_member_sum[wave] = member_sum;
     w_members[wave] = members;
     w_q[wave] = q_sum;
   }
-  __syncthreads();
+  lds_barrier();
   top = member_top = -INFINITY;
   members = q_sum = 0.f;
 #pragma unroll
@@ -289,35 +317,19 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
     members += w_members[w];
     q_sum += w_q[w];
   }
-  const float top_r = reference(top), top_all = a.rest ? reference(fmaxf(top, member_top)) : top_r;
+  const float top_r = reference(top), top_all = REST ? reference(fmaxf(top, member_top)) : top_r;
   const float off_r = -top_r * s, off_all = -top_all * s;
-  float sum = 0.f;
-  for_chunks([&](const float* z, uint32_t own, auto&&) {
-#pragma unroll
-    for (int j = 0; j < V; ++j) sum += own >> j & 1 ? power2(__builtin_fmaf(z[j], s, off_r)) : 0.f;
-  });
-  float member_sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < SLOTS; ++i)
-    if (q_class[i] >= 0.f || q_class[i] != q_class[i]) member_sum += power2(__builtin_fmaf(z_class[i], s, off_all));
-  sum = wave_add(sum);
-  member_sum = wave_add(member_sum);
-  if (lane == 0) {
-    w_sum[wave] = sum;
-    w_member_sum[wave] = member_sum;
-  }
-  __syncthreads();
   sum = member_sum = 0.f;
 #pragma unroll
   for (int w = 0; w < NW; ++w) {
-    sum += w_sum[w];
-    member_sum += w_member_sum[w];
+    sum += w_sum[w] * power2(__builtin_fmaf(w_top[w], s, off_r));
+    member_sum += w_member_sum[w] * power2(__builtin_fmaf(w_member_top[w], s, off_all));
   }
   const float part_r = sum * power2((top_r - top_all) * s);        // r's share of the sum over all
-  const float sum_all = a.rest ? part_r + member_sum : sum;
+  const float sum_all = REST ? part_r + member_sum : sum;
   const bool defined = sum_all > 0.f && sum_all < INFINITY && top_all < INFINITY && member_top < INFINITY;
   float q_r = 0.f;
-  if (a.rest) {
+  if (REST) {
     q_r = 1.f - q_sum;
     if (q_r < kRestMin || members == (float)a.C) q_r = 0.f;
   }
@@ -341,7 +353,7 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
     if (g == 0.f) {
       zero_row();
     } else {
-      const float p_r = a.rest ? part_r / sum_all : 1.f;
+      const float p_r = REST ? part_r / sum_all : 1.f;
       const float factor = sum == 0.f ? (defined ? 0.f : NAN) : scale * (big_q * p_r - q_r) / sum;
       for_chunks([&](const float* z, uint32_t, auto&& store_chunk) {
         float d[V];
@@ -352,7 +364,7 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
       __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0): K's classes are written after these
     }
   }
-  __syncthreads();
+  lds_barrier();
   if (a.loss && tid == 0) {
     float part = 0.f;
 #pragma unroll
@@ -370,37 +382,38 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
   }
 }
 
-template <bool BF16, int NT, int CH, int OCC>
+template <bool BF16, bool REST, int NT, int CH, int OCC>
 hipError_t launch_rows(const DistillArgs& a, hipStream_t s) {
-  const size_t lds = a.rest ? ((size_t)a.C + 16 + 31) / 32 * 4 + 4 : 0;   // and a word behind
+  const size_t lds = REST ? ((size_t)a.C + 16 + 31) / 32 * 4 + 4 : 0;   // and a word behind
   DistillArgs part = a;
   for (long long row = 0; row < a.n; row += 1 << 20) {       // 2^20 rows a launch at most
     part.row0 = (int)row;
     const int rows = (int)std::min<long long>(a.n - row, 1 << 20);
-    hipLaunchKernelGGL((distill_kernel<BF16, NT, CH, OCC>), dim3(rows), dim3(NT), lds, s, part);
+    hipLaunchKernelGGL((distill_kernel<BF16, REST, NT, CH, OCC>), dim3(rows), dim3(NT), lds, s, part);
     const hipError_t st = hipGetLastError();
     if (st != hipSuccess) return st;
   }
   return hipSuccess;
 }
 
-template <bool BF16>
+template <bool BF16, bool REST>
 hipError_t launch_by_length(const DistillArgs& a, hipStream_t s) {
   constexpr int V = BF16 ? 8 : 4;
   const int held = a.C + V - 1 - 2 * V;                      // classes between the edges, with the longest shift
-  if (held <= 256 * 1 * V) return launch_rows<BF16, 256, 1, 4>(a, s);
-  if (held <= 256 * 4 * V) return launch_rows<BF16, 256, 4, 4>(a, s);
-  if (held <= 512 * 8 * V) return launch_rows<BF16, 512, 8, 4>(a, s);
-  if (held <= 1024 * 8 * V) return launch_rows<BF16, 1024, 8, 4>(a, s);
-  if (held <= 1024 * 16 * V) return launch_rows<BF16, 1024, 16, 4>(a, s);
-  if (held <= 1024 * 20 * V) return launch_rows<BF16, 1024, 20, 4>(a, s);
-  return launch_rows<BF16, 1024, 0, 4>(a, s);
+  if (held <= 256 * 1 * V) return launch_rows<BF16, REST, 256, 1, 4>(a, s);
+  if (held <= 256 * 4 * V) return launch_rows<BF16, REST, 256, 4, 4>(a, s);
+  if (held <= 512 * 8 * V) return launch_rows<BF16, REST, 512, 8, 4>(a, s);
+  if (held <= 1024 * 8 * V) return launch_rows<BF16, REST, 1024, 8, 4>(a, s);
+  if (held <= 1024 * 16 * V) return launch_rows<BF16, REST, 1024, 16, 4>(a, s);
+  if (held <= 1024 * 20 * V) return launch_rows<BF16, REST, 1024, 20, 4>(a, s);
+  return launch_rows<BF16, REST, 1024, 0, 4>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t s) {
-  return bf16 ? launch_by_length<true>(a, s) : launch_by_length<false>(a, s);
+  if (bf16) return a.rest ? launch_by_length<true, true>(a, s) : launch_by_length<true, false>(a, s);
+  return a.rest ? launch_by_length<false, true>(a, s) : launch_by_length<false, false>(a, s);
 }
 
 }  // namespace rafiki

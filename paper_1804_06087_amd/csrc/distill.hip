@@ -121,7 +121,7 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
     return __builtin_nontemporal_load((const u32x4*)(x_row + (long long)i * NT * 16 + (unsigned)(tid + 1) * 16u));
   };
   auto store = [&](int i, const float d[V]) {
-    *(u32x4_any*)(d_row + (long long)i * NT * 16 + (unsigned)(tid + 1) * 16u) = pack<BF16, V>(d);
+    __builtin_nontemporal_store(pack<BF16, V>(d), (u32x4_any*)(d_row + (long long)i * NT * 16 + (unsigned)(tid + 1) * 16u));
   };
   auto load_edge = [&]() {
     u32x4 q = {kMasked, kMasked, kMasked, kMasked};
@@ -400,10 +400,13 @@ template <bool BF16, bool REST>
 hipError_t launch_by_length(const DistillArgs& a, hipStream_t s) {
   constexpr int V = BF16 ? 8 : 4;
   const int held = a.C + V - 1 - 2 * V;                      // classes between the edges, with the longest shift
-  if (held <= 256 * 1 * V) return launch_rows<BF16, REST, 256, 1, 4>(a, s);
-  if (held <= 256 * 4 * V) return launch_rows<BF16, REST, 256, 4, 4>(a, s);
-  if (held <= 512 * 8 * V) return launch_rows<BF16, REST, 512, 8, 4>(a, s);
-  if (held <= 1024 * 8 * V) return launch_rows<BF16, REST, 1024, 8, 4>(a, s);
+  // Few threads with many chunks each: more rows share a compute unit, and one's loads run beside another's
+  // arithmetic (30000 bf16 classes: 151 us in 512 threads of 8 chunks, 129 us in 256 of 16).
+  if (held <= 128 * 2 * V) return launch_rows<BF16, REST, 128, 2, 4>(a, s);
+  if (held <= 128 * 8 * V) return launch_rows<BF16, REST, 128, 8, 4>(a, s);
+  if (held <= 256 * 8 * V) return launch_rows<BF16, REST, 256, 8, 4>(a, s);
+  if (held <= 256 * 16 * V) return launch_rows<BF16, REST, 256, 16, 4>(a, s);
+  if (held <= 512 * 16 * V) return launch_rows<BF16, REST, 512, 16, 4>(a, s);
   if (held <= 1024 * 16 * V) return launch_rows<BF16, REST, 1024, 16, 4>(a, s);
   if (held <= 1024 * 20 * V) return launch_rows<BF16, REST, 1024, 20, 4>(a, s);
   return launch_rows<BF16, REST, 1024, 0, 4>(a, s);

@@ -196,7 +196,7 @@ struct RowShared {
     uint32_t counts[FLAT ? kFlatBins : kBins];
     u64 run_key[kList];             // sorted runs; sums of units along the list
   };
-  u64 wave_a[16], wave_b[16];
+  u64 wave_a[16];
   u64 found_a, found_b, found_c;
   int found_class;
   uint32_t n_groups, n_list;
@@ -204,9 +204,14 @@ struct RowShared {
   int list_class[kList], run_class[kList];
 };
 
-// Sum of v over the threads before this one; total = the sum over all.
+// Sum of v over the threads before this one, and over all.  Not inlined: a row's time is mostly that of
+// fetching the code it runs through, and the row kernels scan half a dozen times.
+struct Scan {
+  u64 before, total;
+};
 template <int NT>
-__device__ __forceinline__ u64 block_scan(u64 v, u64* waves, u64& total) {
+__device__ __attribute__((noinline)) Scan block_scan(u64 v) {
+  __shared__ u64 waves[NT / 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   u64 s = v;
 #pragma unroll
@@ -217,15 +222,14 @@ __device__ __forceinline__ u64 block_scan(u64 v, u64* waves, u64& total) {
   __syncthreads();
   if (lane == 63) waves[wave] = s;
   __syncthreads();
-  u64 before = 0;
-  total = 0;
+  u64 before = 0, total = 0;
 #pragma unroll 4
   for (int w = 0; w < NT / 64; ++w) {
     const u64 t = waves[w];
     before += w < wave ? t : 0;
     total += t;
   }
-  return before + s - v;
+  return Scan{before + s - v, total};
 }
 
 __device__ __forceinline__ u64 units_of(u64 key) { return (u64)(__longlong_as_double((long long)key) * kUnit); }
@@ -375,48 +379,60 @@ struct Row {
     }
   }
 
-  // Bounds of log2 p over group g of 64 classes: one of its classes reaches `low`, none exceeds `high`.
-  __device__ __forceinline__ void group_scores(int g, float& low, float& high) const {
+  // Bounds of log2 p over G groups of 64 classes (g0 + j NT + the thread): one of a group's classes reaches
+  // `low`, none exceeds `high`; -inf past the last group, and where p is too small to matter.  `best` is
+  // best_score().  The groups' maxima of one model are in flight together.
+  static constexpr int G = 8;
+  __device__ __forceinline__ void group_scores(int g0, float best, float (&low)[G], float (&high)[G]) const {
+    const int groups = a.units * kUnitTops;
     const float kf = fminf((float)k, 3e38f);                 // 0 kf stays 0
-    if (a.S == 1) {
-      low = high = (stat_tops(a, row)[g] - sh.top[0]) * kf + sh.log_scale[0];
-      if (!(low > -2048.f)) low = high = -INFINITY;          // also NaN of an infinite product
-      return;
+#pragma unroll
+    for (int j = 0; j < G; ++j) {
+      low[j] = -INFINITY;
+      high[j] = 0.f;
     }
-    low = -INFINITY;
 #pragma unroll 1
     for (int m = 0; m < a.S; ++m) {
-      const float t = (stat_tops(a, (long long)row * a.S + m)[g] - sh.top[m]) * kf + sh.log_scale[m];
-      if (t > -2048.f) low = fmaxf(low, t);
+      const float* tops = stat_tops(a, (long long)row * a.S + m);
+      const float top = sh.top[m], log_scale = sh.log_scale[m];
+      float v[G];
+#pragma unroll
+      for (int j = 0; j < G; ++j) {
+        const int g = g0 + j * NT + (int)threadIdx.x;
+        v[j] = g < groups ? tops[g] : -INFINITY;
+      }
+#pragma unroll
+      for (int j = 0; j < G; ++j) {
+        const float t = (v[j] - top) * kf + log_scale;
+        const bool some = t > -2048.f;                       // also false for the NaN of an infinite product
+        low[j] = some ? fmaxf(low[j], t) : low[j];
+        high[j] += some ? __builtin_amdgcn_exp2f(t - best) : 0.f;
+      }
     }
-    high = 0.f;
-#pragma unroll 1
-    for (int m = 0; m < a.S; ++m) {
-      const float t = (stat_tops(a, (long long)row * a.S + m)[g] - sh.top[m]) * kf + sh.log_scale[m];
-      if (t > -2048.f) high += exp2f(t - low);
-    }
-    high = low > -INFINITY ? low + log2f(high) : -INFINITY;
+#pragma unroll
+    for (int j = 0; j < G; ++j) high[j] = best + __builtin_amdgcn_logf(high[j]);
   }
 
   // A score that at least `need` classes reach (need >= 1; -inf where the groups do not tell):
   // need groups hold a class at least that likely.
   __device__ float bound(int need, float best) {
-    const int groups = a.units * kUnitTops;
     __syncthreads();
     for (int b = threadIdx.x; b < kBins; b += NT) sh.counts[b] = 0;
     if (threadIdx.x == 0) sh.found_a = kBins - 1;
     __syncthreads();
-    for (int g = threadIdx.x; g < groups; g += NT) {
-      float low, high;
-      group_scores(g, low, high);
-      if (low > -INFINITY) atomicAdd(&sh.counts[(int)fminf((best - low) * kBinsPerOctave, (float)(kBins - 1))], 1u);
+    for (int g0 = 0; g0 < a.units * kUnitTops; g0 += G * NT) {
+      float low[G], high[G];
+      group_scores(g0, best, low, high);
+#pragma unroll
+      for (int j = 0; j < G; ++j)
+        if (low[j] > -INFINITY) atomicAdd(&sh.counts[(int)fminf((best - low[j]) * kBinsPerOctave, (float)(kBins - 1))], 1u);
     }
     __syncthreads();
     constexpr int PER = kBins / NT;
-    u64 n = 0, total;
+    u64 n = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) n += sh.counts[threadIdx.x * PER + i];
-    u64 at = block_scan<NT>(n, sh.wave_a, total);
+    u64 at = block_scan<NT>(n).before;
     if (at < (u64)need && at + n >= (u64)need) {
       int b = threadIdx.x * PER;
       while (at + sh.counts[b] < (u64)need) at += sh.counts[b++];
@@ -434,44 +450,54 @@ struct Row {
     return best;
   }
 
-  // Lists every class whose p reaches 2^(score) (and some below it); false where they do not fit.
-  __device__ bool list(float score) {
-    const int lane = threadIdx.x & 63;
+  // The groups that may hold a class whose log2 p reaches score, into sums; how many there are (more than
+  // kMaxGroupsListed: not all are listed).
+  __device__ int list_groups(float score, float best) {
     uint32_t* groups = (uint32_t*)sh.sums;
     __syncthreads();
-    if (threadIdx.x == 0) sh.n_groups = sh.n_list = 0;
+    if (threadIdx.x == 0) sh.n_groups = 0;
     __syncthreads();
     const int n = (a.C + 63) / 64;
-    for (int g = threadIdx.x; g < n; g += NT) {
-      float low, high;
-      group_scores(g, low, high);
-      if (high >= score - kSlack) {
-        const uint32_t i = atomicAdd(&sh.n_groups, 1u);
-        if (i < kMaxGroupsListed) groups[i] = g;
+    for (int g0 = 0; g0 < n; g0 += G * NT) {
+      float low[G], high[G];
+      group_scores(g0, best, low, high);
+#pragma unroll
+      for (int j = 0; j < G; ++j) {
+        const int g = g0 + j * NT + threadIdx.x;
+        if (g < n && high[j] >= score - kSlack) {
+          const uint32_t i = atomicAdd(&sh.n_groups, 1u);
+          if (i < kMaxGroupsListed) groups[i] = g;
+        }
       }
     }
     __syncthreads();
-    const int listed = (int)sh.n_groups;
+    return (int)sh.n_groups;
+  }
+
+  // Lists every class whose log2 p reaches score (and some below it); false where they do not fit.
+  __device__ bool list(float score, float best) {
+    const int lane = threadIdx.x & 63;
+    const uint32_t* groups = (const uint32_t*)sh.sums;
+    const int listed = list_groups(score, best);
     if (listed > kMaxGroupsListed) return false;
+    if (threadIdx.x == 0) sh.n_list = 0;
+    __syncthreads();
     const u64 least = score > -1000.f ? (u64)__double_as_longlong((double)exp2f(fmaxf(score - kSlack, -120.f))) : 1;
-    constexpr int AT_ONCE = 8;                               // groups of a wave in flight
-    for (int i = (threadIdx.x >> 6) * AT_ONCE; i < listed; i += kWaves * AT_ONCE) {
-      int c[AT_ONCE];
-      u64 x[AT_ONCE];
+    for (int i = (threadIdx.x >> 6) * G; i < listed; i += kWaves * G) {
+      int c[G];
+      u64 x[G];
 #pragma unroll
-      for (int j = 0; j < AT_ONCE; ++j) c[j] = i + j < listed ? (int)groups[i + j] * 64 + lane : a.C;
-      keys<AT_ONCE>(c, x);
+      for (int j = 0; j < G; ++j) c[j] = i + j < listed ? (int)groups[i + j] * 64 + lane : a.C;
+      keys<G>(c, x);
 #pragma unroll
-      for (int j = 0; j < AT_ONCE; ++j) {
+      for (int j = 0; j < G; ++j) {
         const bool take = x[j] >= (score > -120.f ? least : 1);
-        const u64 who = __ballot(take);
-        if (!who) continue;
-        uint32_t at = 0;
-        if (lane == 0) at = atomicAdd(&sh.n_list, (uint32_t)__popcll(who));
-        at = __shfl(at, 0, 64) + __popcll(who & (((u64)1 << lane) - 1));
-        if (take && at < kList) {
-          sh.list_key[at] = x[j];
-          sh.list_class[at] = c[j];
+        if (take) {
+          const uint32_t at = atomicAdd(&sh.n_list, 1u);
+          if (at < kList) {
+            sh.list_key[at] = x[j];
+            sh.list_class[at] = c[j];
+          }
         }
       }
     }
@@ -486,13 +512,15 @@ struct Row {
     const int runs = (n + 63) / 64;
     __syncthreads();
     for (int run = threadIdx.x >> 6; run < runs; run += kWaves) {
-      const int i = run * 64 + lane, m = min(64, n - run * 64);
+      const int i = run * 64 + lane;
       const u64 x = i < n ? sh.list_key[i] : 0;
       const int c = i < n ? sh.list_class[i] : 0x7fffffff;
       int rank = 0;
-      for (int j = 0; j < m; ++j) {
-        const u64 y = sh.list_key[run * 64 + j];
-        rank += (y > x) | ((y == x) & (sh.list_class[run * 64 + j] < c));
+#pragma unroll 8
+      for (int j = 0; j < 64; ++j) {                         // past the run's end: key 0, behind every other
+        const u64 y = (u64)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), j) << 32 |
+                      (uint32_t)__builtin_amdgcn_readlane((int)x, j);
+        rank += (y > x) | ((y == x) & (__builtin_amdgcn_readlane(c, j) < c));
       }
       if (i < n) {
         sh.run_key[run * 64 + rank] = x;
@@ -525,14 +553,14 @@ struct Row {
   __device__ void accumulate() {
     constexpr int PER = kList / NT;
     const int n = (int)sh.n_list;
-    u64 p[PER], sum = 0, total;
+    u64 p[PER], sum = 0;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       const int i = threadIdx.x * PER + j;
       p[j] = i < n ? units_of(sh.list_key[i]) : 0;
       sum += p[j];
     }
-    u64 at = block_scan<NT>(sum, sh.wave_a, total);
+    u64 at = block_scan<NT>(sum).before;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       const int i = threadIdx.x * PER + j;
@@ -553,16 +581,22 @@ struct Row {
     return sh.found_class;
   }
 
-  // The largest key, from the groups that may hold it.
+  // The largest key: the only model's maximum has it, and with more models a class of the groups that reach `best`.
   __device__ u64 best_key(float best) {
+    if (a.S == 1) return (u64)__double_as_longlong(sh.scale[0]);
+    const int lane = threadIdx.x & 63, listed = list_groups(best, best);
+    const uint32_t* groups = (const uint32_t*)sh.sums;
+    const bool some = listed <= kMaxGroupsListed;            // else all
+    const int n = some ? listed : (a.C + 63) / 64;
     u64 top = 0;
-    const int lane = threadIdx.x & 63;
-    for (int g = threadIdx.x >> 6; g < (a.C + 63) / 64; g += kWaves) {
-      float low, high;
-      group_scores(g, low, high);
-      if (high < best - kSlack) continue;
-      const u64 x = g * 64 + lane < a.C ? key(g * 64 + lane) : 0;
-      top = x > top ? x : top;
+    for (int i = (threadIdx.x >> 6) * G; i < n; i += kWaves * G) {
+      int c[G];
+      u64 x[G];
+#pragma unroll
+      for (int j = 0; j < G; ++j) c[j] = i + j < n ? (some ? (int)groups[i + j] : i + j) * 64 + lane : a.C;
+      keys<G>(c, x);
+#pragma unroll
+      for (int j = 0; j < G; ++j) top = x[j] > top ? x[j] : top;
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
@@ -609,13 +643,13 @@ struct Row {
       }
       __syncthreads();
       constexpr int PER = kFlatBins / NT;
-      u64 n = 0, s = 0, total_n, total_s;
+      u64 n = 0, s = 0;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         n += sh.counts[threadIdx.x * PER + i];
         s += sh.sums[threadIdx.x * PER + i];
       }
-      u64 at_n = above_n + block_scan<NT>(n, sh.wave_a, total_n), at_s = above_sum + block_scan<NT>(s, sh.wave_b, total_s);
+      u64 at_n = above_n + block_scan<NT>(n).before, at_s = above_sum + block_scan<NT>(s).before;
       const u64 at = by_sum ? at_s : at_n, part = by_sum ? s : n;
       if (at < target && at + part >= target) {
         int b = threadIdx.x * PER;
@@ -727,14 +761,14 @@ struct Row {
       if (threadIdx.x == 0) sh.n_list = n;
       sort();
       constexpr int PER = kList / NT;
-      u64 p[PER], sum = 0, total;
+      u64 p[PER], sum = 0;
 #pragma unroll
       for (int j = 0; j < PER; ++j) {
         const int i = threadIdx.x * PER + j;
         p[j] = i < n ? sh.sums[sh.list_key[i] & 0xFFFF] : 0;
         sum += p[j];
       }
-      u64 at = block_scan<NT>(sum, sh.wave_a, total);
+      u64 at = block_scan<NT>(sum).before;
 #pragma unroll
       for (int j = 0; j < PER; ++j) {
         if (at <= target && at + p[j] > target) {
@@ -748,6 +782,7 @@ struct Row {
     for (int i = threadIdx.x; i < n; i += NT) {
       const int c = sh.list_class[i];
       u64 before = 0;                                        // of the classes of lower index
+#pragma unroll 8
       for (int j = 0; j < n; ++j) before += sh.list_class[j] < c ? sh.sums[j] : 0;
       const u64 p = sh.sums[i];
       if (before <= target && before + p > target) {
@@ -764,9 +799,7 @@ struct Row {
       const int unit = first + threadIdx.x;
       const u64 mass = unit < a.units ? unit_mass(unit) : 0;
       if (unit < a.units) sh.sums[unit] = mass;
-      u64 part;
-      block_scan<NT>(mass, sh.wave_a, part);
-      total += part;
+      total += block_scan<NT>(mass).total;
     }
     return total;
   }
@@ -778,13 +811,13 @@ struct Row {
     for (int first = 0; first < a.units; first += NT) {
       const int i = first + threadIdx.x;
       const u64 mass = i < a.units ? sh.sums[i] : 0;
-      u64 part;
-      const u64 at = seen + block_scan<NT>(mass, sh.wave_a, part);
+      const Scan scan = block_scan<NT>(mass);
+      const u64 at = seen + scan.before;
       if (at <= target && at + mass > target) {
         sh.found_a = i;
         sh.found_b = target - at;
       }
-      seen += part;
+      seen += scan.total;
     }
     __syncthreads();
     unit = (int)sh.found_a;
@@ -796,14 +829,14 @@ struct Row {
   // another rounding) the last kept; false where none has any units.
   __device__ bool draw_in_unit(int c0, u64 target, u64 cut, u64 ties, u64 mass, float u) {
     constexpr int PER = kUnitClasses / NT;
-    u64 x[PER], equal = 0, part = 0, total;
+    u64 x[PER], equal = 0, part = 0;
     int c[PER];
 #pragma unroll
     for (int j = 0; j < PER; ++j) c[j] = c0 + threadIdx.x * PER + j;
     keys<PER>(c, x);
 #pragma unroll
     for (int j = 0; j < PER; ++j) equal += x[j] == cut;
-    u64 tie = block_scan<NT>(equal, sh.wave_a, total);
+    u64 tie = ties == ~(u64)0 ? 0 : block_scan<NT>(equal).before;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       // selects: from a branch on `x < cut || (x == cut && tie++ >= ties)` the compiler of ROCm 7.2
@@ -813,7 +846,9 @@ struct Row {
       x[j] = keep ? units_of(x[j]) : 0;
       part += x[j];
     }
-    u64 at = block_scan<NT>(part, sh.wave_b, total);
+    const Scan scan = block_scan<NT>(part);
+    const u64 total = scan.total;
+    u64 at = scan.before;
     if (a.units == 1) {                                      // the row's own sum of units decides
       mass = total;
       target = draw_target(total, u);
@@ -832,11 +867,10 @@ struct Row {
 
   // Draws at `target` of unit `unit`, or where that has no units from the nearest one behind it, or before.
   __device__ void draw(int unit, u64 target, u64 mass, float u) {
-    if (draw_in_unit(unit * kUnitClasses, target, 1, ~(u64)0, mass, u)) return;
-    for (int next = unit + 1; next < a.units; ++next)
-      if (draw_in_unit(next * kUnitClasses, 0, 1, ~(u64)0, mass, u)) return;
-    for (int next = unit - 1; next >= 0; --next)
-      if (draw_in_unit(next * kUnitClasses, ~(u64)0, 1, ~(u64)0, mass, u)) return;
+    for (int i = 0; i < a.units; ++i) {
+      const int behind = unit + i, next = behind < a.units ? behind : a.units - 1 - i;
+      if (draw_in_unit(next * kUnitClasses, i == 0 ? target : next > unit ? 0 : ~(u64)0, 1, ~(u64)0, mass, u)) return;
+    }
   }
 };
 
@@ -887,7 +921,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(TokenArgs a) {
   float score;
   if (f.top_k || by_mass) score = r.bound(f.top_k ? f.top_k : min(64, max(a.units * kUnitTops / 4, 4)), best);
   else score = best + __log2f(f.min_p) - kSlack;
-  for (bool whole = false; r.list(score); whole = true) {
+  for (bool whole = false; r.list(score, best); whole = true) {
     r.sort();
     r.accumulate();
     int kept = (int)sh.n_list;
@@ -967,17 +1001,16 @@ __global__ __launch_bounds__(NT, 4) void sample_flat_kernel(TokenArgs a) {
   for (int first = 0; first < a.units; first += NT) {
     const int unit = first + threadIdx.x;
     const u64 equal = unit < a.units ? sh.counts[unit] : 0;
-    u64 part_ties, part;
-    const u64 before = seen_ties + block_scan<NT>(equal, sh.wave_a, part_ties);
+    const Scan scan = block_scan<NT>(equal);
+    const u64 before = seen_ties + scan.before;
     const u64 kept = before >= cut.ties ? 0 : equal < cut.ties - before ? equal : cut.ties - before;
     const u64 mass = unit < a.units ? sh.sums[unit] + kept * each : 0;
-    block_scan<NT>(mass, sh.wave_b, part);
+    total += block_scan<NT>(mass).total;
     if (unit < a.units) {
       sh.sums[unit] = mass;
       sh.counts[unit] = (uint32_t)kept;
     }
-    seen_ties += part_ties;
-    total += part;
+    seen_ties += scan.total;
   }
   int unit;
   u64 rest;
@@ -1003,7 +1036,8 @@ __global__ __launch_bounds__(NT) void topk_kernel(TokenArgs a) {
   const int row = a.row0 + blockIdx.x;
   Row<BF16, NT, false> r{a, sh, row, log2_scale(a.t_all)};
   const int state = r.init();
-  const bool listed = state != 0 || r.list(r.bound(a.k, r.best_score()));
+  const float best = r.best_score();
+  const bool listed = state != 0 || r.list(r.bound(a.k, best), best);
   if (threadIdx.x == 0) a.flat[row] = !listed;
   if (state != 0) {
     for (int j = threadIdx.x; j < a.k; j += NT) {
@@ -1033,8 +1067,8 @@ __global__ __launch_bounds__(NT, 4) void topk_flat_kernel(TokenArgs a) {
   for (int c0 = 0; c0 < a.C; c0 += NT) {
     const int c = c0 + threadIdx.x;
     const u64 key = c < a.C ? r.key(c) : 0;
-    u64 total;
-    const u64 tie = seen_ties + block_scan<NT>(key == cut.key, sh.wave_a, total);
+    const Scan scan = block_scan<NT>(key == cut.key);
+    const u64 tie = seen_ties + scan.before;
     if ((key > cut.key) | ((key == cut.key) & (tie < cut.ties))) {
       const uint32_t i = atomicAdd(&sh.n_list, 1u);
       if (i < kList) {
@@ -1042,7 +1076,7 @@ __global__ __launch_bounds__(NT, 4) void topk_flat_kernel(TokenArgs a) {
         sh.list_class[i] = c;
       }
     }
-    seen_ties += total;
+    seen_ties += scan.total;
   }
   __syncthreads();
   write_topk(a, sh, r, row);

@@ -202,6 +202,7 @@ struct RowShared {
   uint32_t n_groups, n_list;
   u64 list_key[kList];
   int list_class[kList], run_class[kList];
+  uint32_t unit_ties[FLAT ? kMaxUnits : 1];   // kept classes with key == cut of every unit
 };
 
 // Sum of v over the threads before this one, and over all.  Not inlined: a row's time is mostly that of
@@ -232,7 +233,12 @@ __device__ __attribute__((noinline)) Scan block_scan(u64 v) {
   return Scan{before + s - v, total};
 }
 
-__device__ __forceinline__ u64 units_of(u64 key) { return (u64)(__longlong_as_double((long long)key) * kUnit); }
+// floor(p 2^62) for the bits of p <= 1 + 2^-52 (0 for key 0): the mantissa, shifted by the exponent.
+__device__ __forceinline__ u64 units_of(u64 key) {
+  const u64 mantissa = ((key & (((u64)1 << 52) - 1)) | (u64)1 << 52) << 10;
+  const uint32_t down = 1023 - (uint32_t)(key >> 52);
+  return down < 64 ? mantissa >> down : 0;
+}
 
 // floor (up = 0) or ceiling (up = 1) of x f, exactly, for 0 < f < 1 (x < 2^63).
 __device__ __forceinline__ u64 times_fraction(u64 x, float f, int up) {
@@ -265,6 +271,7 @@ __device__ __forceinline__ u64 draw_target(u64 mass, float u) {
 // mass is the sum of their units.
 struct Cut {
   u64 key, ties, mass;
+  bool units;                 // sums and unit_ties hold the units' kept masses and ties
 };
 
 template <bool BF16, int NT, bool FLAT>
@@ -635,8 +642,8 @@ struct Row {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if (x[i] != 0 && (up == 64 || x[i] >> up == prefix_bits >> up)) {
-            const u64 below = top_bin - (x[i] >> shift);
-            const int b = (x[i] >> shift) > top_bin ? 0 : below < kFlatBins - 1 ? (int)below : kFlatBins - 1;
+            const uint32_t at = (uint32_t)(x[i] >> shift), below = (uint32_t)top_bin - at;   // equal above 32 bits
+            const int b = at > (uint32_t)top_bin && up == 64 ? 0 : (int)min(below, (uint32_t)kFlatBins - 1);
             atomicAdd(&sh.sums[b], units_of(x[i]));
             if (!by_sum) atomicAdd(&sh.counts[b], 1u);
           }
@@ -677,13 +684,21 @@ struct Row {
         sort();
         accumulate();
         const int r = by_sum ? reach((int)sh.n_list, target - above_sum) : (int)(target - above_n);
+        cut.units = true;
         cut.key = sh.list_key[r - 1];
         cut.mass = above_sum + sh.run_key[r - 1];
         __syncthreads();
         if (threadIdx.x == 0) sh.found_class = 0;
         __syncthreads();
         int same = 0;
-        for (int i = threadIdx.x; i < r; i += NT) same += sh.list_key[i] == cut.key;
+        for (int i = threadIdx.x; i < r; i += NT) {
+          const int unit = sh.list_class[i] / kUnitClasses;
+          atomicAdd(&sh.sums[unit], units_of(sh.list_key[i]));
+          if (sh.list_key[i] == cut.key) {
+            ++same;
+            atomicAdd(&sh.unit_ties[unit], 1u);
+          }
+        }
         if (same) atomicAdd(&sh.found_class, same);
         __syncthreads();
         cut.ties = (u64)sh.found_class;
@@ -691,6 +706,7 @@ struct Row {
       }
       if (shift == 0) {                                                // one key, in more classes than the list holds
         cut.key = prefix_bits;
+        cut.units = false;
         const u64 each = units_of(cut.key);
         cut.ties = by_sum ? (target - above_sum + each - 1) / each : target - above_n;
         cut.mass = above_sum + cut.ties * each;
@@ -701,22 +717,23 @@ struct Row {
     }
   }
 
-  // Lists the classes whose key starts with prefix_bits.
+  // Lists the classes whose key starts with prefix_bits; sums[unit]: the units of the classes above them.
   __device__ void list_prefix(u64 prefix_bits, int shift) {
     __syncthreads();
     if (threadIdx.x == 0) sh.n_list = 0;
     __syncthreads();
     const u64 want = prefix_bits >> shift;
-    // with one model the logits themselves tell which classes may be there
-    float lo = -INFINITY, hi = INFINITY;
+    // with one model the logits themselves tell which classes may be there or above
+    float lo = -INFINITY;
     if (a.S == 1) {
-      const float span = shift > 46 ? 1.f : 1.f / 32;         // log2(65 / 64) at most
       lo = log2f((float)__longlong_as_double((long long)prefix_bits)) - kSlack;
-      hi = lo + span + 2 * kSlack;
-      if (!(lo > -120.f)) lo = -INFINITY, hi = INFINITY;
+      if (!(lo > -120.f)) lo = -INFINITY;
     }
     const float kf = fminf((float)k, 3e38f);
+    for (int u = threadIdx.x; u < a.units; u += NT) sh.unit_ties[u] = 0;
+    u64 above = 0;
     auto take = [&](u64 x, int c) {
+      if (x >> shift > want) above += units_of(x);
       if (x != 0 && x >> shift == want) {
         const uint32_t at = atomicAdd(&sh.n_list, 1u);
         if (at < kList) {
@@ -732,7 +749,7 @@ struct Row {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const float t = (z[i] - sh.top[0]) * kf + sh.log_scale[0];
-          if (!(t < lo || t > hi)) {
+          if (!(t < lo)) {
             const u64 x = (u64)__double_as_longlong(__builtin_fma(weight(z[i], sh.top[0], k), sh.scale[0], 0.0));
             take(x < kLeastKey ? 0 : x, unit_class(u, i));
           }
@@ -743,6 +760,10 @@ struct Row {
 #pragma unroll
         for (int i = 0; i < 16; ++i) take(x[i], unit_class(u, i));
       }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) above += __shfl_xor(above, o, 64);
+      if ((threadIdx.x & 63) == 0) sh.sums[u] = above;
+      above = 0;
     }
     __syncthreads();
   }
@@ -964,58 +985,63 @@ __global__ __launch_bounds__(NT, 4) void sample_flat_kernel(TokenArgs a) {
   Row<BF16, NT, true> r{a, sh, row, log2_scale(t)};
   r.init();
   const Filters f = row_filters(a, row, t);
-  Cut cut{1, ~(u64)0, r.unit_masses()};
+  Cut cut{1, ~(u64)0, r.unit_masses(), false};
   if (f.top_k) r.select(false, (u64)f.top_k, false, cut);
   if (f.top_p < 1.f) r.select(true, times_fraction(cut.mass, f.top_p, 1), false, cut);
   if (f.min_p > 0.f) {
-    const u64 top = r.best_key(r.best_score());
-    const u64 least = (u64)__double_as_longlong((double)f.min_p * __longlong_as_double((long long)top));
-    if (least > cut.key) { cut.key = least; cut.ties = ~(u64)0; }
+    const u64 least = (u64)__double_as_longlong((double)f.min_p * __longlong_as_double((long long)r.best_key(r.best_score())));
+    if (least > cut.key) cut = Cut{least, ~(u64)0, 0, false};
+    else cut.units = cut.units && a.S == 1;                  // with more models best_key() has used sums
   }
   __syncthreads();
-  // a wave per unit: the units above the cut, and the ties
-  const int lane = threadIdx.x & 63;
-  for (int unit = threadIdx.x >> 6; unit < a.units; unit += NT / 64) {
-    u64 mass = 0;
-    uint32_t equal = 0;
-    u64 x[16];
-    r.unit_keys(unit, x);
+  u64 total = 0;
+  if (cut.units) {
+    total = cut.mass;
+  } else {
+    // a wave per unit: the units above the cut, and the ties
+    const int lane = threadIdx.x & 63;
+    for (int unit = threadIdx.x >> 6; unit < a.units; unit += NT / 64) {
+      u64 mass = 0;
+      uint32_t equal = 0;
+      u64 x[16];
+      r.unit_keys(unit, x);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      mass += x[i] > cut.key ? units_of(x[i]) : 0;
-      equal += x[i] == cut.key;
-    }
+      for (int i = 0; i < 16; ++i) {
+        mass += x[i] > cut.key ? units_of(x[i]) : 0;
+        equal += x[i] == cut.key;
+      }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      mass += __shfl_xor(mass, o, 64);
-      equal += __shfl_xor(equal, o, 64);
+      for (int o = 32; o > 0; o >>= 1) {
+        mass += __shfl_xor(mass, o, 64);
+        equal += __shfl_xor(equal, o, 64);
+      }
+      if (lane == 0) {
+        sh.sums[unit] = mass;
+        sh.unit_ties[unit] = equal;
+      }
     }
-    if (lane == 0) {
-      sh.sums[unit] = mass;
-      sh.counts[unit] = equal;
+    __syncthreads();
+    const u64 each = units_of(cut.key);
+    u64 seen_ties = 0;
+    for (int first = 0; first < a.units; first += NT) {
+      const int unit = first + threadIdx.x;
+      const u64 equal = unit < a.units ? sh.unit_ties[unit] : 0;
+      const Scan scan = block_scan<NT>(equal);
+      const u64 before = seen_ties + scan.before;
+      const u64 kept = before >= cut.ties ? 0 : equal < cut.ties - before ? equal : cut.ties - before;
+      const u64 mass = unit < a.units ? sh.sums[unit] + kept * each : 0;
+      total += block_scan<NT>(mass).total;
+      if (unit < a.units) {
+        sh.sums[unit] = mass;
+        sh.unit_ties[unit] = (uint32_t)kept;
+      }
+      seen_ties += scan.total;
     }
-  }
-  __syncthreads();
-  const u64 each = units_of(cut.key);
-  u64 seen_ties = 0, total = 0;
-  for (int first = 0; first < a.units; first += NT) {
-    const int unit = first + threadIdx.x;
-    const u64 equal = unit < a.units ? sh.counts[unit] : 0;
-    const Scan scan = block_scan<NT>(equal);
-    const u64 before = seen_ties + scan.before;
-    const u64 kept = before >= cut.ties ? 0 : equal < cut.ties - before ? equal : cut.ties - before;
-    const u64 mass = unit < a.units ? sh.sums[unit] + kept * each : 0;
-    total += block_scan<NT>(mass).total;
-    if (unit < a.units) {
-      sh.sums[unit] = mass;
-      sh.counts[unit] = (uint32_t)kept;
-    }
-    seen_ties += scan.total;
   }
   int unit;
   u64 rest;
   r.find_unit(draw_target(total, f.u), unit, rest);
-  r.draw_in_unit(unit * kUnitClasses, rest, cut.key, sh.counts[unit], total, f.u);
+  r.draw_in_unit(unit * kUnitClasses, rest, cut.key, sh.unit_ties[unit], total, f.u);
 }
 
 // Sorts the list of a row's first classes and writes it.
@@ -1058,7 +1084,7 @@ __global__ __launch_bounds__(NT, 4) void topk_flat_kernel(TokenArgs a) {
   if (!a.flat[row]) return;
   Row<BF16, NT, true> r{a, sh, row, log2_scale(a.t_all)};
   r.init();
-  Cut cut{1, ~(u64)0, 0};
+  Cut cut{1, ~(u64)0, 0, false};
   r.select(false, (u64)a.k, true, cut);
   __syncthreads();
   if (threadIdx.x == 0) sh.n_list = 0;

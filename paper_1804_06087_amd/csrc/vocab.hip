@@ -420,34 +420,63 @@ struct Row {
     for (int j = 0; j < G; ++j) high[j] = best + __builtin_amdgcn_logf(high[j]);
   }
 
-  // A score that at least `need` classes reach (need >= 1; -inf where the groups do not tell):
-  // need groups hold a class at least that likely.
+  // A score that at least `need` classes reach (need >= 1; -inf where none is found): `need` groups hold a class
+  // at least that likely, or where there are fewer groups, `need` classes are (a pass over the logits).
   __device__ float bound(int need, float best) {
-    __syncthreads();
-    for (int b = threadIdx.x; b < kBins; b += NT) sh.counts[b] = 0;
-    if (threadIdx.x == 0) sh.found_a = kBins - 1;
-    __syncthreads();
-    for (int g0 = 0; g0 < a.units * kUnitTops; g0 += G * NT) {
-      float low[G], high[G];
-      group_scores(g0, best, low, high);
+    float score = -INFINITY;
+    for (bool classes = need > (a.C + 63) / 64;; classes = true) {
+      // the classes of a bin that the bound cuts would not fit into a list beside so many
+      if (classes && need > kList / 8 * 7 && a.C > kList) return score;
+      __syncthreads();
+      for (int b = threadIdx.x; b < kBins; b += NT) sh.counts[b] = 0;
+      if (threadIdx.x == 0) sh.found_a = kBins - 1;
+      __syncthreads();
+      auto count = [&](float low) {
+        if (low > -INFINITY) atomicAdd(&sh.counts[(int)fminf((best - low) * kBinsPerOctave, (float)(kBins - 1))], 1u);
+      };
+      if (classes) {
+        const float kf = fminf((float)k, 3e38f);
+        for (int u = threadIdx.x >> 6; u < a.units; u += kWaves) {
+          float low[16];
 #pragma unroll
-      for (int j = 0; j < G; ++j)
-        if (low[j] > -INFINITY) atomicAdd(&sh.counts[(int)fminf((best - low[j]) * kBinsPerOctave, (float)(kBins - 1))], 1u);
-    }
-    __syncthreads();
-    constexpr int PER = kBins / NT;
-    u64 n = 0;
+          for (int i = 0; i < 16; ++i) low[i] = -INFINITY;
+#pragma unroll 1
+          for (int m = 0; m < a.S; ++m) {
+            float z[16];
+            unit_logits(u, m, z);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) n += sh.counts[threadIdx.x * PER + i];
-    u64 at = block_scan<NT>(n).before;
-    if (at < (u64)need && at + n >= (u64)need) {
-      int b = threadIdx.x * PER;
-      while (at + sh.counts[b] < (u64)need) at += sh.counts[b++];
-      sh.found_a = b;
+            for (int i = 0; i < 16; ++i) {
+              const float t = (z[i] - sh.top[m]) * kf + sh.log_scale[m];
+              low[i] = t > -2048.f ? fmaxf(low[i], t) : low[i];
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) count(low[i]);
+        }
+      } else {
+        for (int g0 = 0; g0 < a.units * kUnitTops; g0 += G * NT) {
+          float low[G], high[G];
+          group_scores(g0, best, low, high);
+#pragma unroll
+          for (int j = 0; j < G; ++j) count(low[j]);
+        }
+      }
+      __syncthreads();
+      constexpr int PER = kBins / NT;
+      u64 n = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) n += sh.counts[threadIdx.x * PER + i];
+      u64 at = block_scan<NT>(n).before;
+      if (at < (u64)need && at + n >= (u64)need) {
+        int b = threadIdx.x * PER;
+        while (at + sh.counts[b] < (u64)need) at += sh.counts[b++];
+        sh.found_a = b;
+      }
+      __syncthreads();
+      const int b = (int)sh.found_a;
+      if (b < kBins - 1) score = best - (float)(b + 1) / kBinsPerOctave - kSlack;
+      if (classes || score > -INFINITY || a.C <= kList) return score;
     }
-    __syncthreads();
-    const int b = (int)sh.found_a;
-    return b == kBins - 1 ? -INFINITY : best - (float)(b + 1) / kBinsPerOctave - kSlack;
   }
 
   // The largest of the groups' lower bounds: that of the class at which a model has its maximum.
@@ -471,7 +500,7 @@ struct Row {
 #pragma unroll
       for (int j = 0; j < G; ++j) {
         const int g = g0 + j * NT + threadIdx.x;
-        if (g < n && high[j] >= score - kSlack) {
+        if (g < n && high[j] > -INFINITY && high[j] >= score - kSlack) {
           const uint32_t i = atomicAdd(&sh.n_groups, 1u);
           if (i < kMaxGroupsListed) groups[i] = g;
         }

@@ -417,7 +417,8 @@ struct Row {
       }
     }
 #pragma unroll
-    for (int j = 0; j < G; ++j) high[j] = best + __builtin_amdgcn_logf(high[j]);
+    for (int j = 0; j < G; ++j)                              // near underflow 32 models at most sum to 5 octaves more
+      high[j] = high[j] > 0x1p-100f ? best + __builtin_amdgcn_logf(high[j]) : low[j] + 5.f;
   }
 
   // A score that at least `need` classes reach (need >= 1; -inf where none is found): `need` groups hold a class
@@ -500,7 +501,7 @@ struct Row {
 #pragma unroll
       for (int j = 0; j < G; ++j) {
         const int g = g0 + j * NT + threadIdx.x;
-        if (g < n && high[j] > -INFINITY && high[j] >= score - kSlack) {
+        if (g < n && low[j] > -INFINITY && high[j] >= score - kSlack) {
           const uint32_t i = atomicAdd(&sh.n_groups, 1u);
           if (i < kMaxGroupsListed) groups[i] = g;
         }

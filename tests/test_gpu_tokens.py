@@ -264,6 +264,21 @@ def test_topk_ties_order_and_special_rows():
     assert labels[4, :4].tolist() == [1000, 5, 2999, -1] and (labels[2] == -1).all() and (labels[3] == -1).all()
 
 
+@pytest.mark.parametrize("S", [1, 2, 32])
+@pytest.mark.parametrize("k", [300, 430, 440, 446, 700])
+def test_topk_far_below_the_best(S, k):
+    """Probabilities over more octaves than fp32 has: 0.29 octaves a class (0.58 from class 600 on), in 79 groups."""
+    C = 5000
+    c = torch.arange(C, device=DEV).float()
+    z = torch.stack([-(c * 0.2 + torch.relu(c - 600) * 0.2)] * S)[:, None].repeat(1, 2, 1)
+    z[:, 1] = z[:, 1].flip(-1)
+    labels = torch.empty((2, k), dtype=torch.int32, device=DEV)
+    logp = torch.empty((2, k), device=DEV)
+    bd.combine_topk(z.contiguous(), labels, logp)
+    torch.cuda.synchronize()
+    check_topk(z, k, 1.0, labels, logp)
+
+
 # ---------------------------------------------------------------- distillation
 
 def teacher(rng, n, C, k, rest):

@@ -284,7 +284,7 @@ struct Row {
 
   // Joins the units' statistics, a wave per model; 0: a distribution, 1: a model without a class
   // above -inf, 2: NaN or +inf somewhere.
-  __device__ int init() {
+  __device__ __forceinline__ int init() {
     const int lane = threadIdx.x & 63;
     if (threadIdx.x == 0) sh.state = 0;
     __syncthreads();
@@ -312,7 +312,7 @@ struct Row {
   }
 
   // Units of the mass of all classes of unit u.
-  __device__ u64 unit_mass(int u) const {
+  __device__ __forceinline__ u64 unit_mass(int u) const {
     double p = 0.0;
 #pragma unroll 1
     for (int m = 0; m < a.S; ++m) {
@@ -324,18 +324,25 @@ struct Row {
   }
 
   // Bits of p_c (they order as p_c does) of N classes, 0 for one without a probability or past the row's end:
-  // one model's N logits are in flight together.
+  // one model's N logits are in flight together, and the next model's behind them.
   template <int N>
   __device__ __forceinline__ void keys(const int (&c)[N], u64 (&x)[N]) const {
     double p[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) p[i] = 0.0;
+    float next[N];
+    auto fetch = [&](int m) {
+      const long long at = row * a.ld_row + m * a.ld_model;
+#pragma unroll
+      for (int i = 0; i < N; ++i) next[i] = c[i] < a.C ? logit<BF16>(a.logits, at + c[i]) : -INFINITY;
+    };
+    fetch(0);
 #pragma unroll 1
     for (int m = 0; m < a.S; ++m) {
-      const long long at = row * a.ld_row + m * a.ld_model;
       float z[N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) z[i] = c[i] < a.C ? logit<BF16>(a.logits, at + c[i]) : -INFINITY;
+      for (int i = 0; i < N; ++i) z[i] = next[i];
+      if (m + 1 < a.S) fetch(m + 1);                         // while this model's powers are taken
       const float top = sh.top[m];
       const double scale = sh.scale[m];
 #pragma unroll
@@ -398,16 +405,23 @@ struct Row {
       low[j] = -INFINITY;
       high[j] = 0.f;
     }
-#pragma unroll 1
-    for (int m = 0; m < a.S; ++m) {
+    float next[G];
+    auto fetch = [&](int m) {
       const float* tops = stat_tops(a, (long long)row * a.S + m);
-      const float top = sh.top[m], log_scale = sh.log_scale[m];
-      float v[G];
 #pragma unroll
       for (int j = 0; j < G; ++j) {
         const int g = g0 + j * NT + (int)threadIdx.x;
-        v[j] = g < groups ? tops[g] : -INFINITY;
+        next[j] = g < groups ? tops[g] : -INFINITY;
       }
+    };
+    fetch(0);
+#pragma unroll 1
+    for (int m = 0; m < a.S; ++m) {
+      float v[G];
+#pragma unroll
+      for (int j = 0; j < G; ++j) v[j] = next[j];
+      if (m + 1 < a.S) fetch(m + 1);
+      const float top = sh.top[m], log_scale = sh.log_scale[m];
 #pragma unroll
       for (int j = 0; j < G; ++j) {
         const float t = (v[j] - top) * kf + log_scale;
@@ -421,9 +435,25 @@ struct Row {
       high[j] = high[j] > 0x1p-100f ? best + __builtin_amdgcn_logf(high[j]) : low[j] + 5.f;
   }
 
+  // The scores of the first G NT groups, taken once (FLAT: not kept).
+  float low0[FLAT ? 1 : G], high0[FLAT ? 1 : G];
+  __device__ __forceinline__ void scores(int g0, float best, float (&low)[G], float (&high)[G]) const {
+    if constexpr (!FLAT) {
+      if (g0 == 0) {
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+          low[j] = low0[j];
+          high[j] = high0[j];
+        }
+        return;
+      }
+    }
+    group_scores(g0, best, low, high);
+  }
+
   // A score that at least `need` classes reach (need >= 1; -inf where none is found): `need` groups hold a class
   // at least that likely, or where there are fewer groups, `need` classes are (a pass over the logits).
-  __device__ float bound(int need, float best) {
+  __device__ __forceinline__ float bound(int need, float best) {
     float score = -INFINITY;
     for (bool classes = need > (a.C + 63) / 64;; classes = true) {
       // the classes of a bin that the bound cuts would not fit into a list beside so many
@@ -457,7 +487,7 @@ struct Row {
       } else {
         for (int g0 = 0; g0 < a.units * kUnitTops; g0 += G * NT) {
           float low[G], high[G];
-          group_scores(g0, best, low, high);
+          scores(g0, best, low, high);
 #pragma unroll
           for (int j = 0; j < G; ++j) count(low[j]);
         }
@@ -483,13 +513,14 @@ struct Row {
   // The largest of the groups' lower bounds: that of the class at which a model has its maximum.
   __device__ __forceinline__ float best_score() const {
     float best = -INFINITY;
+#pragma unroll 1
     for (int m = 0; m < a.S; ++m) best = fmaxf(best, sh.log_scale[m]);
     return best;
   }
 
   // The groups that may hold a class whose log2 p reaches score, into sums; how many there are (more than
   // kMaxGroupsListed: not all are listed).
-  __device__ int list_groups(float score, float best) {
+  __device__ __forceinline__ int list_groups(float score, float best) {
     uint32_t* groups = (uint32_t*)sh.sums;
     __syncthreads();
     if (threadIdx.x == 0) sh.n_groups = 0;
@@ -497,7 +528,7 @@ struct Row {
     const int n = (a.C + 63) / 64;
     for (int g0 = 0; g0 < n; g0 += G * NT) {
       float low[G], high[G];
-      group_scores(g0, best, low, high);
+      scores(g0, best, low, high);
 #pragma unroll
       for (int j = 0; j < G; ++j) {
         const int g = g0 + j * NT + threadIdx.x;
@@ -512,7 +543,7 @@ struct Row {
   }
 
   // Lists every class whose log2 p reaches score (and some below it); false where they do not fit.
-  __device__ bool list(float score, float best) {
+  __device__ __forceinline__ bool list(float score, float best) {
     const int lane = threadIdx.x & 63;
     const uint32_t* groups = (const uint32_t*)sh.sums;
     const int listed = list_groups(score, best);
@@ -544,7 +575,7 @@ struct Row {
 
   // Sorts the list by key down and class up: every 64 by rank in a wave, then every class's place among the
   // other runs of 64 by bisection.  (A bitonic sort of 1024 with a barrier a step took 60 us.)
-  __device__ void sort() {
+  __device__ __forceinline__ void sort() {
     const int n = (int)sh.n_list, lane = threadIdx.x & 63;
     const int runs = (n + 63) / 64;
     __syncthreads();
@@ -553,12 +584,14 @@ struct Row {
       const u64 x = i < n ? sh.list_key[i] : 0;
       const int c = i < n ? sh.list_class[i] : 0x7fffffff;
       int rank = 0;
-#pragma unroll 8
-      for (int j = 0; j < 64; ++j) {                         // past the run's end: key 0, behind every other
-        const u64 y = (u64)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), j) << 32 |
-                      (uint32_t)__builtin_amdgcn_readlane((int)x, j);
-        rank += (y > x) | ((y == x) & (__builtin_amdgcn_readlane(c, j) < c));
-      }
+      const int m = min(64, (n - run * 64 + 7) & ~7);
+      for (int j0 = 0; j0 < m; j0 += 8)
+#pragma unroll
+        for (int j = j0; j < j0 + 8; ++j) {                  // past the run's end: key 0, behind every other
+          const u64 y = (u64)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), j) << 32 |
+                        (uint32_t)__builtin_amdgcn_readlane((int)x, j);
+          rank += (y > x) | ((y == x) & (__builtin_amdgcn_readlane(c, j) < c));
+        }
       if (i < n) {
         sh.run_key[run * 64 + rank] = x;
         sh.run_class[run * 64 + rank] = c;
@@ -587,7 +620,7 @@ struct Row {
   }
 
   // run_key[i] = the units of the listed classes up to and with i.
-  __device__ void accumulate() {
+  __device__ __forceinline__ void accumulate() {
     constexpr int PER = kList / NT;
     const int n = (int)sh.n_list;
     u64 p[PER], sum = 0;
@@ -608,7 +641,7 @@ struct Row {
   }
 
   // The number of the first n accumulated classes whose sum reaches target (n + 1 where all do not).
-  __device__ int reach(int n, u64 target) {
+  __device__ __forceinline__ int reach(int n, u64 target) {
     __syncthreads();
     if (threadIdx.x == 0) sh.found_class = n + 1;
     __syncthreads();
@@ -619,7 +652,7 @@ struct Row {
   }
 
   // The largest key: the only model's maximum has it, and with more models a class of the groups that reach `best`.
-  __device__ u64 best_key(float best) {
+  __device__ __forceinline__ u64 best_key(float best) {
     if (a.S == 1) return (u64)__double_as_longlong(sh.scale[0]);
     const int lane = threadIdx.x & 63, listed = list_groups(best, best);
     const uint32_t* groups = (const uint32_t*)sh.sums;
@@ -652,7 +685,7 @@ struct Row {
   // all the octaves), then 11 bits a level within the bin reached, until its classes fit into the
   // list and are sorted.  False where all classes (those above 2^-63, which have units) stay
   // below target.
-  __device__ bool select(bool by_sum, u64 target, bool whole, Cut& cut) {
+  __device__ __forceinline__ bool select(bool by_sum, u64 target, bool whole, Cut& cut) {
     constexpr u64 first_bin = (u64)1023 << 6;                 // bits of 1.0 >> 46
     u64 prefix_bits = 0, above_n = 0, above_sum = 0;
     int shift = whole ? 52 : 46, up = 64;
@@ -748,7 +781,7 @@ struct Row {
   }
 
   // Lists the classes whose key starts with prefix_bits; sums[unit]: the units of the classes above them.
-  __device__ void list_prefix(u64 prefix_bits, int shift) {
+  __device__ __forceinline__ void list_prefix(u64 prefix_bits, int shift) {
     __syncthreads();
     if (threadIdx.x == 0) sh.n_list = 0;
     __syncthreads();
@@ -799,7 +832,7 @@ struct Row {
   }
 
   // Draws from the first n accumulated classes, in the order of their indices.
-  __device__ void draw_listed(int n, u64 target, u64 mass, bool greedy) {
+  __device__ __forceinline__ void draw_listed(int n, u64 target, u64 mass, bool greedy) {
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += NT) sh.sums[i] = sh.run_key[i] - (i ? sh.run_key[i - 1] : 0);
     __syncthreads();
@@ -844,7 +877,7 @@ struct Row {
   }
 
   // The units' masses into sums, and their sum.
-  __device__ u64 unit_masses() {
+  __device__ __forceinline__ u64 unit_masses() {
     u64 total = 0;
     for (int first = 0; first < a.units; first += NT) {
       const int unit = first + threadIdx.x;
@@ -856,7 +889,7 @@ struct Row {
   }
 
   // The unit in which the sums of the units' masses pass target, and what of target lies in it.
-  __device__ void find_unit(u64 target, int& unit, u64& rest) {
+  __device__ __forceinline__ void find_unit(u64 target, int& unit, u64& rest) {
     u64 seen = 0;
     __syncthreads();
     for (int first = 0; first < a.units; first += NT) {
@@ -878,7 +911,7 @@ struct Row {
   // The class c of [c0, c0 + kUnitClasses) at which the kept units pass `target`, counted from c0; the
   // first `ties` classes with key == cut are kept.  Where they stay below target (it comes from sums of
   // another rounding) the last kept; false where none has any units.
-  __device__ bool draw_in_unit(int c0, u64 target, u64 cut, u64 ties, u64 mass, float u) {
+  __device__ __forceinline__ bool draw_in_unit(int c0, u64 target, u64 cut, u64 ties, u64 mass, float u) {
     constexpr int PER = kUnitClasses / NT;
     u64 x[PER], equal = 0, part = 0;
     int c[PER];
@@ -917,7 +950,7 @@ struct Row {
   }
 
   // Draws at `target` of unit `unit`, or where that has no units from the nearest one behind it, or before.
-  __device__ void draw(int unit, u64 target, u64 mass, float u) {
+  __device__ __forceinline__ void draw(int unit, u64 target, u64 mass, float u) {
     for (int i = 0; i < a.units; ++i) {
       const int behind = unit + i, next = behind < a.units ? behind : a.units - 1 - i;
       if (draw_in_unit(next * kUnitClasses, i == 0 ? target : next > unit ? 0 : ~(u64)0, 1, ~(u64)0, mass, u)) return;
@@ -969,6 +1002,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(TokenArgs a) {
     return;
   }
   const float best = r.best_score();
+  r.group_scores(0, best, r.low0, r.high0);
   float score;
   if (f.top_k || by_mass) score = r.bound(f.top_k ? f.top_k : min(64, max(a.units * kUnitTops / 4, 4)), best);
   else score = best + __log2f(f.min_p) - kSlack;
@@ -1016,8 +1050,12 @@ __global__ __launch_bounds__(NT, 4) void sample_flat_kernel(TokenArgs a) {
   r.init();
   const Filters f = row_filters(a, row, t);
   Cut cut{1, ~(u64)0, r.unit_masses(), false};
-  if (f.top_k) r.select(false, (u64)f.top_k, false, cut);
-  if (f.top_p < 1.f) r.select(true, times_fraction(cut.mass, f.top_p, 1), false, cut);
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {                     // one copy of select()'s code
+    const bool by_sum = pass == 1;
+    if (by_sum ? f.top_p < 1.f : f.top_k != 0)
+      r.select(by_sum, by_sum ? times_fraction(cut.mass, f.top_p, 1) : (u64)f.top_k, false, cut);
+  }
   if (f.min_p > 0.f) {
     const u64 least = (u64)__double_as_longlong((double)f.min_p * __longlong_as_double((long long)r.best_key(r.best_score())));
     if (least > cut.key) cut = Cut{least, ~(u64)0, 0, false};
@@ -1093,6 +1131,7 @@ __global__ __launch_bounds__(NT) void topk_kernel(TokenArgs a) {
   Row<BF16, NT, false> r{a, sh, row, log2_scale(a.t_all)};
   const int state = r.init();
   const float best = r.best_score();
+  r.group_scores(0, best, r.low0, r.high0);
   const bool listed = state != 0 || r.list(r.bound(a.k, best), best);
   if (threadIdx.x == 0) a.flat[row] = !listed;
   if (state != 0) {

@@ -396,7 +396,7 @@ struct Row {
   // Bounds of log2 p over G groups of 64 classes (g0 + j NT + the thread): one of a group's classes reaches
   // `low`, none exceeds `high`; -inf past the last group, and where p is too small to matter.  `best` is
   // best_score().  The groups' maxima of one model are in flight together.
-  static constexpr int G = 8;
+  static constexpr int G = 4;
   __device__ __forceinline__ void group_scores(int g0, float best, float (&low)[G], float (&high)[G]) const {
     const int groups = a.units * kUnitTops;
     const float kf = fminf((float)k, 3e38f);                 // 0 kf stays 0
@@ -1209,7 +1209,7 @@ hipError_t launch_row_kernel(F kernel, int threads, const TokenArgs& a, hipStrea
 hipError_t launch_sample(const TokenArgs& a, bool bf16, hipStream_t s) {
   hipError_t st = bf16 ? launch_stats<true>(a, s) : launch_stats<false>(a, s);
   if (st != hipSuccess) return st;
-  st = bf16 ? launch_row_kernel(sample_kernel<true, 256>, 256, a, s) : launch_row_kernel(sample_kernel<false, 256>, 256, a, s);
+  st = bf16 ? launch_row_kernel(sample_kernel<true, 512>, 512, a, s) : launch_row_kernel(sample_kernel<false, 512>, 512, a, s);
   if (st != hipSuccess || a.C <= kList) return st;           // every class fits into a list
   if (!a.temperature && !a.top_k && !a.top_p && !a.min_p) return st;   // a unit always does
   return bf16 ? launch_row_kernel(sample_flat_kernel<true, 1024>, 1024, a, s)
@@ -1219,7 +1219,7 @@ hipError_t launch_sample(const TokenArgs& a, bool bf16, hipStream_t s) {
 hipError_t launch_topk(const TokenArgs& a, bool bf16, hipStream_t s) {
   hipError_t st = bf16 ? launch_stats<true>(a, s) : launch_stats<false>(a, s);
   if (st != hipSuccess) return st;
-  st = bf16 ? launch_row_kernel(topk_kernel<true, 256>, 256, a, s) : launch_row_kernel(topk_kernel<false, 256>, 256, a, s);
+  st = bf16 ? launch_row_kernel(topk_kernel<true, 512>, 512, a, s) : launch_row_kernel(topk_kernel<false, 512>, 512, a, s);
   if (st != hipSuccess || a.C <= kList) return st;
   return bf16 ? launch_row_kernel(topk_flat_kernel<true, 1024>, 1024, a, s)
               : launch_row_kernel(topk_flat_kernel<false, 1024>, 1024, a, s);

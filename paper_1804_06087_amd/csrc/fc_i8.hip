@@ -214,6 +214,13 @@ struct TileLoader {
 // v_mfma_i32_32x32x32_i8 with w as the first operand, so that a lane sums 4 neighbouring outputs of
 // one row.  Splits (grid y) each sum a range of K tiles; with more than one the
 // int32 sums go to the workspace and fc_i8_reduce_kernel joins them.
+//
+// Measured on an MI355X: 4096 x 4096 x 30000 515 to 610 us by the values (1.65 to 1.95 POP/s; the library's int8 product,
+// without scales and bias, 530 us on random values).  The matrix cores are busy for 47 % of the cycles at the
+// 1.95 GHz that this load leaves them; without the products the loads, fragment reads and stores alone take
+// 443 us, without the loads the rest takes 500 us, without the stores 536 us: LDS, which takes both operands'
+// tiles and gives each wave 192 rows for 128 x 64 outputs, is shared by all of them.  Deeper rings of 64-byte K tiles,
+// 4 waves of 128 x 128 and two workgroups of 128 x 256 a unit were 5 to 20 % slower.
 template <int BM, int BN, int WM, int WN, int STAGES, int OCC>
 __global__ __launch_bounds__(WM * WN * 64, OCC) void fc_i8_tile_kernel(FcI8Args a) {
   constexpr int NW = WM * WN;
@@ -535,28 +542,30 @@ hipError_t launch_quantize(const void* x, bool bf16, long long ld_x, int n, int 
 
 // The tile configurations, largest first.
 struct FcConfig {
-  int bm, bn, per_cu;        // workgroups that fit on a compute unit
+  int bm, bn;
 };
-constexpr FcConfig kConfigs[] = {{256, 256, 1}, {128, 128, 2}, {64, 128, 2}};
+constexpr FcConfig kConfigs[] = {{256, 256}, {128, 128}, {64, 128}};
+constexpr int kUnitsOfGpu = 256;
 
 struct FcPlan {
   int cfg, splits, kt_per_split;
 };
 
+// The largest tile that still gives every compute unit one (2048 x 1024 x 8192: 26.8 us in 256 x 256, 29.0 in 128 x 128,
+// 35.2 in 64 x 128; 1000 x 4096 x 4096: 53, 28 and 28 us), else the smallest, with K split over the idle units
+// in runs of at least 8 K tiles (64 x 25088 x 4096: 78 us unsplit, 24 in 8, 27 in 16; 128 x 2048 x 1000: 10.3
+// unsplit, 10.7 in 2, 12.3 in 4): the splits' sums go through memory and a second launch.
 FcPlan plan_fc(int n, int c_in, int c_out) {
   const int ktiles = (c_in + 127) / 128;
-  FcPlan best{0, 1, ktiles};
-  int cfg = n > 128 ? 0 : n > 64 ? 1 : 2;
   auto tiles = [&](int c) {
-    return (long long)((n + kConfigs[c].bm - 1) / kConfigs[c].bm) * ((c_out + kConfigs[c].bn - 1) / kConfigs[c].bn);
+    return ((long long)n + kConfigs[c].bm - 1) / kConfigs[c].bm * (((long long)c_out + kConfigs[c].bn - 1) / kConfigs[c].bn);
   };
-  if (cfg == 0 && tiles(0) < 256) cfg = 1;
-  best.cfg = cfg;
-  const long long slots = 256 * kConfigs[cfg].per_cu, t = tiles(cfg);
-  int splits = (int)std::max<long long>(1, std::min<long long>(slots / t, ktiles / 4));
-  best.kt_per_split = (ktiles + splits - 1) / splits;
-  best.splits = (ktiles + best.kt_per_split - 1) / best.kt_per_split;
-  return best;
+  int cfg = 0;
+  while (cfg < 2 && tiles(cfg) < kUnitsOfGpu) ++cfg;
+  const int splits = (int)std::max<long long>(1, std::min<long long>(kUnitsOfGpu / tiles(cfg), ktiles / 8));
+  FcPlan p{cfg, 1, (ktiles + splits - 1) / splits};
+  p.splits = (ktiles + p.kt_per_split - 1) / p.kt_per_split;
+  return p;
 }
 
 template <int BM, int BN, int WM, int WN, int STAGES, int OCC>
@@ -567,18 +576,24 @@ hipError_t launch_tile(const FcI8Args& a, int splits, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Rows that fc_i8_rows_kernel takes: its waves read x again for every 16 outputs.
-constexpr int kFewRows = 32;
+// What fc_i8_rows_kernel takes: its waves read x again for every 16 outputs, so it suits products whose x and w are
+// small.  In us, and in tiles: 1 x 4096 x 4096 7.8 and 12.0, 16 x 8192 x 4096 10.9 and 11.4, 32 x 4096 x 4096 8.7 and 12.1;
+// but 32 x 8192 x 4096 15.1 and 12.4, 16 x 12288 x 1000 15.2 and 11.6, 16 x 1024 x 30000 11.3 and 7.3.
+bool few_rows(int n, int c_in, int c_out) {
+  if (n > 32) return false;
+  const int blocks = (n + 15) / 16;
+  return c_in * blocks <= 8192 && c_out <= 16384 && (long long)c_in * c_out * blocks <= 1 << 25;
+}
 
 long long fc_i8_workspace_bytes(int n, int c_in, int c_out) {
-  if (n <= kFewRows) return 0;
+  if (few_rows(n, c_in, c_out)) return 0;
   const FcPlan p = plan_fc(n, c_in, c_out);
   return p.splits > 1 ? (long long)p.splits * n * c_out * 4 : 0;
 }
 
 hipError_t launch_fc_i8(const FcI8Args& args, hipStream_t s) {
   FcI8Args a = args;
-  if (a.n <= kFewRows) {
+  if (few_rows(a.n, a.c_in, a.c_out)) {
     const dim3 grid((a.c_out + 15) / 16);
     if (a.n <= 16) launch(fc_i8_rows_kernel<1, 8, 4>, grid, dim3(512), s, a);
     else launch(fc_i8_rows_kernel<2, 8, 4>, grid, dim3(512), s, a);

@@ -18,12 +18,16 @@ LaunchEvents& launch_events();
 // Every kernel of the library is launched through this, so tracing can time it.  An
 // untimed launch is a plain launch, which stream capture records into a graph.
 template <typename F, typename... Args>
-inline void launch(F kernel, dim3 grid, dim3 block, hipStream_t s, Args... args) {
+inline void launch_lds(F kernel, dim3 grid, dim3 block, size_t lds, hipStream_t s, Args... args) {
   const LaunchEvents& ev = launch_events();
   if (ev.start || ev.stop)
-    hipExtLaunchKernelGGL(kernel, grid, block, 0, s, ev.start, ev.stop, 0, args...);
+    hipExtLaunchKernelGGL(kernel, grid, block, lds, s, ev.start, ev.stop, 0, args...);
   else
-    hipLaunchKernelGGL(kernel, grid, block, 0, s, args...);
+    hipLaunchKernelGGL(kernel, grid, block, lds, s, args...);
+}
+template <typename F, typename... Args>
+inline void launch(F kernel, dim3 grid, dim3 block, hipStream_t s, Args... args) {
+  launch_lds(kernel, grid, block, 0, s, args...);
 }
 
 typedef uint16_t bf16_t;   // bfloat16 storage (upper half of an IEEE float)

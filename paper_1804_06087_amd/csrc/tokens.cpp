@@ -22,6 +22,10 @@ bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 bool aligned_to(const void* p, int dtype) { return ((uintptr_t)p & (dtype == RAFIKI_BF16 ? 1 : 3)) == 0; }
 bool known(int dtype) { return dtype == RAFIKI_FP32 || dtype == RAFIKI_BF16; }
 
+bool fc_sizes(int n, int c_in, int c_out) {
+  return n >= 1 && n <= (1 << 24) && c_out >= 1 && c_out <= (1 << 24) && c_in >= 1 && c_in <= 131071;
+}
+
 long long combine_bytes(int n_models, int n, int n_classes) {
   return (long long)n_models * n * token_stat_stride(n_classes) + ((long long)n * 4 + 15) / 16 * 16;
 }
@@ -136,14 +140,15 @@ int rafiki_quantize_rows_i8(const void* x, int dtype, long long ld_x, int n, int
                             float* scale, void* stream) {
   if (!x || !q || !scale) return invalid("null pointer");
   if (!known(dtype)) return invalid("dtype must be RAFIKI_FP32 or RAFIKI_BF16");
-  if (n < 1 || c < 1 || ld_x < 0 || ld_q < c) return invalid("n and c must be >= 1, ld_x >= 0 and ld_q >= c");
+  if (n < 1 || c < 1 || c > (1 << 30) || ld_x < 0 || ld_q < c)
+    return invalid("n >= 1, c in [1, 2^30], ld_x >= 0 and ld_q >= c");
   if (!aligned_to(x, dtype)) return invalid("rows are not aligned to their type");
   return launched(launch_quantize(x, dtype == RAFIKI_BF16, ld_x, n, c, q, ld_q, scale, (hipStream_t)stream), "quantize");
 }
 
 int rafiki_fc_i8_workspace(int n, int c_in, int c_out, long long* bytes) {
   if (!bytes) return invalid("null pointer");
-  if (n < 1 || c_out < 1 || c_in < 1 || c_in > 131071) return invalid("n, c_out must be >= 1 and c_in in [1, 131071]");
+  if (!fc_sizes(n, c_in, c_out)) return invalid("n and c_out must be in [1, 2^24] and c_in in [1, 131071]");
   *bytes = fc_i8_workspace_bytes(n, c_in, c_out);
   return RAFIKI_OK;
 }
@@ -153,7 +158,7 @@ int rafiki_fc_i8(const int8_t* x, long long ld_x, const float* x_scale, const in
                  long long ld_y, void* workspace, long long workspace_bytes, void* stream) {
   if (!x || !x_scale || !w || !w_scale || !y) return invalid("null pointer");
   if (!known(y_dtype)) return invalid("y_dtype must be RAFIKI_FP32 or RAFIKI_BF16");
-  if (n < 1 || c_out < 1 || c_in < 1 || c_in > 131071) return invalid("n, c_out must be >= 1 and c_in in [1, 131071]");
+  if (!fc_sizes(n, c_in, c_out)) return invalid("n and c_out must be in [1, 2^24] and c_in in [1, 131071]");
   const long long k16 = (c_in + 15) / 16 * 16;
   if (!aligned16(x) || !aligned16(w) || ld_x % 16 || ld_w % 16 || ld_x < k16 || ld_w < k16 || ld_x > (1 << 22) ||
       ld_w > (1 << 22))

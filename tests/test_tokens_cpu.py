@@ -60,11 +60,11 @@ def _fc(**over):
                               {"k": 1025}, {"n": 0}, {"C": 0}, {"C": (1 << 20) + 1}, {"t": 0.0}, {"t": math.nan},
                               {"ld_row": -1}, {"ld_grad": 9}, {"dtype": 5}, {"grad": P + 2}, {"logits": P + 1})],
     *[(_quantize, o) for o in ({"x": None}, {"q": None}, {"scale": None}, {"n": 0}, {"c": 0}, {"ld_q": 9},
-                               {"ld_x": -1}, {"dtype": 2}, {"x": P + 1})],
+                               {"ld_x": -1}, {"dtype": 2}, {"x": P + 1}, {"c": (1 << 30) + 1, "ld_q": 1 << 31})],
     *[(_fc, o) for o in ({"x": None}, {"w": None}, {"sx": None}, {"sw": None}, {"y": None}, {"n": 0}, {"c_out": 0},
                          {"c_in": 0}, {"c_in": 131072, "ld_x": 131072, "ld_w": 131072}, {"ld_x": 15}, {"ld_x": 0},
                          {"ld_w": 24}, {"x": P + 4}, {"w": P + 8}, {"ld_y": 4}, {"dtype": 2}, {"y": P + 2},
-                         {"ld_w": (1 << 22) + 16})],
+                         {"ld_w": (1 << 22) + 16}, {"n": (1 << 24) + 1}, {"c_out": (1 << 24) + 1, "ld_y": 1 << 25})],
 ])
 def test_refusals(call, over):
     assert call(**over) == INVALID, over

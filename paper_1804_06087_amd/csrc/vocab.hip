@@ -849,6 +849,7 @@ struct Row {
         sh.list_class[i] = 0;
       }
       if (threadIdx.x == 0) sh.n_list = n;
+      __syncthreads();                                       // sort() reads it at once
       sort();
       constexpr int PER = kList / NT;
       u64 p[PER], sum = 0;
@@ -1047,7 +1048,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(TokenArgs a) {
 }
 
 // Rows with more kept classes than a list holds: cut by histograms, then a scan of the units.  1024 threads: two
-// passes over the logits, 64-bit powers and LDS atomics bound them (115 us a row of 131072 fp32; 512 threads: 126).
+// passes over the logits, 64-bit powers and LDS atomics bound them (115 us a row of 131072 fp32; 512 threads took 15 us more).
 template <bool BF16, int NT>
 __global__ __launch_bounds__(NT, 4) void sample_flat_kernel(TokenArgs a) {
   __shared__ RowShared<true> sh;

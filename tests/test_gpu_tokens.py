@@ -108,6 +108,22 @@ def test_sample_flat_rows(dtype):
     check_sample(z, par, *run_sample(z, par))
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("S,C", [(2, 40000), (3, 1025), (32, 5003)])
+def test_sample_flat_rows_of_several_models(S, C, dtype):
+    """The mean of several flat distributions; every fourth row holds few distinct values, so its cuts fall into ties."""
+    rng = np.random.default_rng(S + C)
+    z = (rng.standard_normal((S, 8, C)) * 0.3).astype(np.float32)
+    z[:, 3::4] = np.round(z[:1, 3::4] * 2) / 2
+    z = torch.from_numpy(z).to(DT[dtype]).to(DEV)
+    par = {"uniform": rng.random(8).astype(np.float32),
+           "temperature": np.float32([1, 0.7, 2, 1, 1, 1, 0, 1]),
+           "top_p": np.float32([0.5, 0.9, 0.99, 1.0, 0.3, 1.0, 1.0, 1.0]),
+           "top_k": np.int32([0, C - 1, C - 100, C // 2, 0, C // 2, 5000, 1024]),
+           "min_p": np.float32([0, 0, 0.1, 0, 0.5, 0.2, 0, 0])}
+    check_sample(z, par, *run_sample(z, par))
+
+
 def test_sample_ties_are_cut_by_index():
     """Rows of few distinct values: top-k, top-p and min-p cut inside runs of equal classes.  All sums are exact
     (powers of two), so every border is exact too."""
@@ -245,6 +261,21 @@ def test_topk(S, n, C, k, t, dtype):
     check_topk(z, k, np.float32(t), labels, logp)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("S,C,k", [(3, 5003, 1024), (2, 40000, 1000), (32, 2500, 900), (1, 1025, 1024)])
+def test_topk_flat_rows_of_several_models(S, C, k, dtype):
+    """The k-th class among thousands of nearly equal ones; the last row's k-th class is one of many equal ones."""
+    rng = np.random.default_rng(61 + S)
+    z = (rng.standard_normal((S, 4, C)) * 0.01).astype(np.float32)
+    z[:, 3] = np.round(z[:1, 3] * 50) / 50
+    z = torch.from_numpy(z).to(DT[dtype]).to(DEV)
+    labels = torch.full((4, k), -7, dtype=torch.int32, device=DEV)
+    logp = torch.full((4, k), -7.0, device=DEV)
+    bd.combine_topk(z, labels, logp)
+    torch.cuda.synchronize()
+    check_topk(z, k, 1.0, labels, logp)
+
+
 def test_topk_ties_order_and_special_rows():
     C, k = 3000, 600
     z = torch.zeros((1, 8, C), device=DEV)
@@ -353,6 +384,17 @@ def test_distill(n, C, k, t, dtype, rest):
     # each output alone gives the same bits
     assert torch.equal(run_distill(z, ids, logp, t, rest, g, grad=False)[0], loss)
     assert torch.equal(run_distill(z, ids, logp, t, rest, g, loss=False)[1], grad)
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("chunks", [256, 1024, 2048, 4096, 8192, 16384, 20480])
+def test_distill_at_every_row_length(chunks, dtype, rest):
+    """Both sides of each number of 16-byte chunks at which a row takes more threads or registers; of the odd
+    lengths every row starts at another alignment."""
+    V = 8 if dtype == "bf16" else 4
+    for C in (chunks * V + V + 1, chunks * V + V + 2):
+        test_distill(3, C, 9, 1.5, dtype, rest)
 
 
 @pytest.mark.parametrize("rest", [False, True])
@@ -487,6 +529,12 @@ def test_quantize(n, c, dtype):
     assert (buf[:, c:] == 99).all()
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("c", [8192, 8193, 28672, 28673, 60001, 131071])
+def test_quantize_long_rows(c, dtype):
+    test_quantize(3, c, dtype)
+
+
 def test_quantize_special_rows():
     x = np.zeros((8, 37), np.float32)
     x[0, 5] = np.nan
@@ -538,6 +586,13 @@ def test_fc(n, c_in, c_out, dtype):
     torch.cuda.synchronize()
     check_fc(x, sx, w, sw, bias, relu, y, dtype)
     assert (buf[:, c_out:] == 42).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,c_in,c_out", [(4100, 130, 4200), (3841, 256, 4351), (2050, 300, 2049), (4097, 17, 4097)])
+def test_fc_many_tiles(n, c_in, c_out, dtype):
+    """Enough rows and columns for the larger tiles, with ragged edges and K ends inside a chunk."""
+    test_fc(n, c_in, c_out, dtype)
 
 
 def test_fc_extremes():

@@ -87,7 +87,7 @@ int rafiki_combine_topk(const void* logits, int dtype, long long ld_model, long 
  *             (rounding of the fp32 values), or with K all classes, counts as 0.
  * Terms with q = 0 are 0.  With Q = sum q + q_r the gradient is
  *   dz_c = T g_i (Q p_c - q_c) for c in K,  T g_i (Q p_c - q_r p_c / p_r) otherwise (q_r = 0
- *   without rest, or where p_r = 0),
+ *   without rest, or where p_r = 0: nothing above -inf outside K),
  * where g_i = grad_loss[i] (fp32 [n], dL / d loss_i; null: 1); a row with g_i = 0 has gradient
  * 0 whatever it holds.  A class with p = 0 in K and q > 0 gives loss +inf; NaN, +inf or a row
  * of only -inf in the student, or NaN in the teacher, gives NaN.

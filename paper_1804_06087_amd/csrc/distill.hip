@@ -104,7 +104,9 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
   __shared__ float slot_q[kMaxTokenK];                       // teacher_logp, then q of the slot
   constexpr uint32_t kMasked = BF16 ? 0xFF80FF80u : 0xFF800000u;     // -inf in every place
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const float s = kLog2e / a.t;
+  // Powers are of (z - top) s, not of z s - top s: masks of the type's lowest value overflow the products,
+  // and a row of nothing else is a uniform one.  T below 2^-127 counts as that, which keeps 0 s at 0.
+  const float s = fminf(kLog2e / a.t, 0x1p127f);
   const int row = a.row0 + blockIdx.x;
   const float g = a.grad_loss ? a.grad_loss[row] : 1.f;
   const long long base = row * a.ld_row, gbase = row * a.ld_grad;
@@ -283,23 +285,23 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
     float now = top;
 #pragma unroll
     for (int j = 0; j < V; ++j) now = fmaxf(now, z[j]);
-    const float off = -reference(now) * s;
-    sum *= power2(__builtin_fmaf(top, s, off));
+    const float ref = reference(now);
+    sum *= power2((top - ref) * s);
 #pragma unroll
-    for (int j = 0; j < V; ++j) sum += own >> j & 1 ? power2(__builtin_fmaf(z[j], s, off)) : 0.f;
+    for (int j = 0; j < V; ++j) sum += own >> j & 1 ? power2((z[j] - ref) * s) : 0.f;
     top = now;
   });
   // the wave's, then the workgroup's
   auto join = [&](float& t, float& v) {
     const float all = wave_max(t);
-    v = wave_add(v * power2(__builtin_fmaf(t, s, -reference(all) * s)));
+    v = wave_add(v * power2((t - reference(all)) * s));
     t = all;
   };
   join(top, sum);
   float member_sum = 0.f;
 #pragma unroll
   for (int i = 0; i < SLOTS; ++i)
-    if (q_class[i] >= 0.f || q_class[i] != q_class[i]) member_sum += power2(__builtin_fmaf(z_class[i], s, -reference(member_top) * s));
+    if (q_class[i] >= 0.f || q_class[i] != q_class[i]) member_sum += power2((z_class[i] - reference(member_top)) * s);
   join(member_top, member_sum);
   members = wave_add(members);
   q_sum = wave_add(q_sum);
@@ -322,12 +324,11 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
     q_sum += w_q[w];
   }
   const float top_r = reference(top), top_all = REST ? reference(fmaxf(top, member_top)) : top_r;
-  const float off_r = -top_r * s, off_all = -top_all * s;
   sum = member_sum = 0.f;
 #pragma unroll
   for (int w = 0; w < NW; ++w) {
-    sum += w_sum[w] * power2(__builtin_fmaf(w_top[w], s, off_r));
-    member_sum += w_member_sum[w] * power2(__builtin_fmaf(w_member_top[w], s, off_all));
+    sum += w_sum[w] * power2((w_top[w] - top_r) * s);
+    member_sum += w_member_sum[w] * power2((w_member_top[w] - top_all) * s);
   }
   const float part_r = sum * power2((top_r - top_all) * s);        // r's share of the sum over all
   const float sum_all = REST ? part_r + member_sum : sum;
@@ -346,7 +347,7 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
       const float q = q_class[i];
-      if (q > 0.f || q != q) part += q * (logf(q) - kLn2 * (__builtin_fmaf(z_class[i], s, off_all) - log_all));
+      if (q > 0.f || q != q) part += q * (logf(q) - kLn2 * ((z_class[i] - top_all) * s - log_all));
     }
     part = wave_add(part);
     if (lane == 0) w_part[wave] = part;
@@ -362,7 +363,7 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
       for_chunks([&](const float* z, uint32_t, auto&& store_chunk) {
         float d[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) d[j] = factor * power2(__builtin_fmaf(z[j], s, off_r));
+        for (int j = 0; j < V; ++j) d[j] = factor * power2((z[j] - top_r) * s);
         store_chunk(d);
       });
       __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0): K's classes are written after these
@@ -373,7 +374,7 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
     float part = 0.f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) part += w_part[w];
-    if (q_r > 0.f) part += sum == 0.f ? INFINITY : q_r * (logf(q_r) - kLn2 * (log2f(part_r) - log_all));
+    if (q_r > 0.f) part += sum == 0.f ? INFINITY : q_r * (logf(q_r) - kLn2 * (log2f(sum) + (top_r - top_all) * s - log_all));
     a.loss[row] = defined ? a.t * a.t * part : NAN;
   }
   if (a.grad && g != 0.f) {
@@ -381,7 +382,7 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
     for (int i = 0; i < SLOTS; ++i) {
       const float q = q_class[i];
       if (q >= 0.f || q != q)
-        put<BF16>(a.grad, gbase + ids[tid + i * NT], scale * (big_q * (power2(__builtin_fmaf(z_class[i], s, off_all)) / sum_all) - q));
+        put<BF16>(a.grad, gbase + ids[tid + i * NT], scale * (big_q * (power2((z_class[i] - top_all) * s) / sum_all) - q));
     }
   }
 }

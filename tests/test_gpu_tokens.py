@@ -424,6 +424,56 @@ def test_distill_slots_empty_repeated_and_masked(rest):
 
 
 @pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("C", [5, 700, 90001])
+def test_distill_masks_of_the_lowest_value(C, dtype, rest):
+    """Rows masked with the type's lowest value: one of nothing else is uniform; the rest has p = 0.  Scores 0 and
+    powers 1 are exact: what is left are sums of equal terms (2^-24 an addition, C / 1024 + 64 of them), quotients
+    and log2 C (2^-22 relative), times the T^2 (Q + 1) of the formula.  Row 1's other classes are equal, so that
+    p_c / p_r = 1 / (C - 2) however small p_r is; its log is finite as long as fp32 holds the difference of the
+    logits over T, in powers of 2."""
+    z = torch.full((3, C), float(torch.finfo(DT[dtype]).min), dtype=DT[dtype], device=DEV)
+    z[1, 2] = z[1, C - 1] = 1.0
+    z[2] = float(torch.finfo(DT[dtype]).max)
+    ids = np.int32([[2, C - 1]] * 3)
+    logp = np.log(np.float32([[0.5, 0.25]] * 3))
+    for t in (0.5, 2.0):
+        loss, grad = run_distill(z, ids, logp, t, rest)
+        q = np.float64([0.5, 0.25]) if rest else np.float64([2 / 3, 1 / 3])
+        q_r = 0.25 if rest else 0.0
+        eps = (C / 1024 + 64) * 2.0 ** -24 + 2.0 ** -20
+        for i, p in ((0, 1 / C), (1, 0.5), (2, 1 / C)):
+            want = (q * (np.log(q) - math.log(p))).sum()
+            other = (C - 2) * p if i != 1 else 0.0
+            if rest:
+                log_other = math.log(other) if i != 1 else (float(z[1, 0]) - 1.0) / t
+                if -log_other / math.log(2) > torch.finfo(torch.float32).max:
+                    log_other = -math.inf
+                want += q_r * (math.log(q_r) - log_other)
+            got = float(loss[i])
+            limit = t * t * 2 * max(math.log(4 * C), abs(want)) * eps if math.isfinite(want) else 0.0
+            assert got == t * t * want or abs(got - t * t * want) <= limit, (i, got, want)
+            d = host(grad[i]).astype(np.float64)
+            assert np.abs(d[ids[i]] - t * (p - q)).max() <= t * (eps * 2 + HALF_STEP[dtype]), i
+            outside = np.delete(d, ids[i])
+            wanted = t * (other - q_r) / (C - 2)
+            assert np.abs(outside - wanted).max() <= t * 2 * eps / C + abs(wanted) * HALF_STEP[dtype], (i, wanted)
+
+
+def test_distill_smallest_and_largest_temperatures():
+    """T so small that one class has all, and so large that all classes are alike."""
+    z = torch.tensor([[1.0, 3.0, 2.0, -math.inf], [0.0, 0.0, 0.0, 0.0]], device=DEV)
+    ids, logp = np.int32([[1], [1]]), np.float32([[0.0], [0.0]])
+    loss, grad = run_distill(z, ids, logp, 1e-39, False)
+    assert torch.isfinite(loss).all() and torch.isfinite(grad).all() and float(loss[0]) == 0 and (grad[0] == 0).all()
+    loss, grad = run_distill(z, ids, logp, 1e19, False)
+    for i, n in ((0, 3), (1, 4)):
+        assert abs(float(loss[i]) / 1e38 - math.log(n)) <= 2.0 ** -20
+        want = np.array([1 / n, 1 / n - 1, 1 / n, 1 / n if n == 4 else 0.0])
+        assert np.abs(host(grad[i]) / 1e19 - want).max() <= 2.0 ** -20
+
+
+@pytest.mark.parametrize("rest", [False, True])
 def test_distill_not_finite(rest):
     rng = np.random.default_rng(22)
     z = lm_logits(rng, 1, 5, 700, "fp32", masked=False)[0]

@@ -267,7 +267,8 @@ int rafiki_ensemble_trace_read(rafiki_ensemble_t h, rafiki_trace_rec* out, int c
  *
  * Ensemble combine (Section 1; Section 5.2): logits fp32 [n_models][n][n_classes]; the
  * mean of the per-model softmax to out_probs fp32 [n][n_classes] and its first-index
- * argmax to out_labels int32 [n].  1 <= n_models <= 32, n >= 1, 1 <= n_classes <= 1024. */
+ * argmax to out_labels int32 [n].  1 <= n_models <= 32, n >= 1, 1 <= n_classes <= 1024.
+ * (rafiki_tokens.h draws from the same mean, or lists its first classes, over up to 2^20.) */
 int rafiki_combine_mean(const float* logits, int n_models, int n, int n_classes, float* out_probs,
                         int32_t* out_labels, void* stream);
 

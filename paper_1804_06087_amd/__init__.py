@@ -1,6 +1,7 @@
 """MI355X (gfx950) ensemble-inference hot path: HIP kernels behind a C ABI
 (``include/rafiki_ensemble.h``), the greedy batch-size scheduler and serving loops
-(``include/rafiki_sched.h``), the actor-critic scheduler (``include/rafiki_rl.h``), and a
+(``include/rafiki_sched.h``), the actor-critic scheduler (``include/rafiki_rl.h``), answers
+over a vocabulary (``include/rafiki_tokens.h``: sampling, top-k, distillation, 8-bit FC), and a
 thin ctypes binding."""
 from .binding import (Ensemble, RafikiError, load_library, last_error, LIB_PATH, EXPORTED,
                       RAFIKI_OK, RAFIKI_ERR_INVALID, RAFIKI_ERR_UNSUPPORTED, RAFIKI_ERR_NOMEM,

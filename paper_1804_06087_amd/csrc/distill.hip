@@ -13,8 +13,8 @@
 // start anywhere.  Rows too long for the registers are read again for each pass (CH = 0), from the L2
 // or the memory-side cache.
 //
-// Measured on an MI355X: 4096 x 30000 bf16 125 us (3.9 TB/s of the floor's bytes; a device copy moves 4.7), 2047 x
-// 131071 bf16 299 us (3.6 TB/s): one such row fills a compute unit's registers, so its arithmetic (two powers a
+// Measured on an MI355X: 4096 x 30000 bf16 127 us (3.9 TB/s of the floor's bytes; a device copy moves 4.7), 2047 x
+// 131071 bf16 292 us (3.7 TB/s): one such row fills a compute unit's registers, so its arithmetic (two powers a
 // class, 15 us) overlaps only with its own loads and stores and those of other units.
 #include "tokens.h"
 

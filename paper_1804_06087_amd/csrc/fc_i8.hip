@@ -34,7 +34,8 @@ typedef uint32_t u32_byte __attribute__((aligned(1)));
 
 // One workgroup per row, which its NT threads hold in CH chunks of 16 bytes each (CH = 0: any length, read
 // twice): the largest magnitude, then the quotients.  The bound is the row's bytes, and with few rows
-// their latency: 64 rows of 25088 fp32 took 50 us in 256 threads that read single values.
+// their latency: 64 rows of 25088 fp32 take 7 us (50 us in 256 threads that read single values), 4096 of
+// 4096 bf16 16 us.
 template <bool BF16, int NT, int CH>
 __global__ __launch_bounds__(NT) void quantize_kernel(const void* x, long long ld_x, int row0, int c, int8_t* q,
                                                       long long ld_q, float* scale) {
@@ -428,6 +429,7 @@ __device__ __forceinline__ i32x4 x_chunk(const int8_t* p, int k, int c_in) {
 // A workgroup takes 16 rows of w and its WAVES waves the 64-byte steps of K in turn, UNROLL steps in flight;
 // v_mfma_i32_16x16x64_i8 sums them (lane l holds 16 bytes from 16 (l / 16) of row l % 16 of either operand,
 // and outputs 4 (l / 16) .. + 3 of w's rows for row l % 16 of x), and the waves' sums meet in LDS.
+// 1 x 4096 x 4096: 5.6 us, 3.0 TB/s.
 template <int NB, int WAVES, int UNROLL>
 __global__ __launch_bounds__(WAVES * 64) void fc_i8_rows_kernel(FcI8Args a) {
   __shared__ int4 sums[WAVES][NB][64];
@@ -483,7 +485,8 @@ __global__ __launch_bounds__(WAVES * 64) void fc_i8_rows_kernel(FcI8Args a) {
   }
 }
 
-// Joins the splits' sums: a thread per 4 outputs of a row.
+// Joins the splits' sums: a thread per 4 outputs of a row.  Bound by its launch and the sums' bytes: 4 us for 8 splits
+// of 64 x 4096.
 __global__ __launch_bounds__(256) void fc_i8_reduce_kernel(FcI8Args a, int splits) {
   const int quads = (a.c_out + 3) / 4;
   const long long total = (long long)a.n * quads, plane = (long long)a.n * a.c_out;

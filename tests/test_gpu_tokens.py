@@ -747,6 +747,35 @@ def test_chain_against_the_oracle():
     check_distill(b["student"], host(b["ids"]), host(b["logp"]), 2.0, True, None, b["loss"], b["grad"], "bf16")
 
 
+def test_more_rows_than_one_launch_takes():
+    """2^20 + 77 rows: every operator gives a row what it gives the same row of a short call."""
+    m, n, C, k = 997, (1 << 20) + 77, 5, 3
+    gen = torch.Generator().manual_seed(3)
+    z = torch.randn(2, m, C, generator=gen).to(DEV)
+    z[:, 5] = -math.inf
+    u = torch.rand(m, generator=gen).to(DEV)
+    which = torch.arange(n, device=DEV) % m
+
+    def run(z, u):
+        n = u.numel()
+        ints = lambda *shape: torch.full(shape, -7, dtype=torch.int32, device=DEV)  # noqa: E731
+        floats = lambda *shape: torch.full(shape, -7.0, device=DEV)  # noqa: E731
+        token, prob, labels, logp, loss, grad = ints(n), floats(n), ints(n, k), floats(n, k), floats(n), floats(n, C)
+        bd.combine_sample(z, u, token, prob, top_p=torch.full((n,), 0.9, device=DEV))
+        bd.combine_topk(z, labels, logp)
+        bd.distill_loss(z[0], labels, logp, loss, grad, rest=True)
+        x, q, scale = torch.where(z[1].isinf(), 0.5, z[1]), torch.zeros(n, 16, dtype=torch.int8, device=DEV), floats(n)
+        bd.quantize_rows_i8(x, q[:, :C], scale)
+        w = torch.arange(-24, 24, device=DEV).to(torch.int8).reshape(3, 16)
+        y = floats(n, 3)
+        bd.fc_i8(q[:, :C], scale, w[:, :C], torch.ones(3, device=DEV), y)
+        torch.cuda.synchronize()
+        return token, prob, labels, logp, loss, grad, q, scale, y
+
+    for few, many in zip(run(z, u), run(z[:, which].contiguous(), u[which].contiguous())):
+        assert torch.equal(torch.nan_to_num(few[which], nan=-99.0), torch.nan_to_num(many, nan=-99.0))
+
+
 def test_two_streams_at_once_repeat_the_same_bits():
     one, two = chain_setup(2), chain_setup(3)
     want = []

@@ -330,7 +330,9 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
     sum += w_sum[w] * power2((w_top[w] - top_r) * s);
     member_sum += w_member_sum[w] * power2((w_member_top[w] - top_all) * s);
   }
-  const float part_r = sum * power2((top_r - top_all) * s);        // r's share of the sum over all
+  // r's share of the sum over all; none where nothing is above -inf outside K (top_r is then no maximum, and its power
+  // may be infinite).  A NaN sum stays NaN.
+  const float part_r = sum == 0.f ? 0.f : sum * power2((top_r - top_all) * s);
   const float sum_all = REST ? part_r + member_sum : sum;
   const bool defined = sum_all > 0.f && sum_all < INFINITY && top_all < INFINITY && member_top < INFINITY;
   float q_r = 0.f;

@@ -840,3 +840,21 @@ def test_replayed_graphs():
     other = chain_setup(6)                                       # an eager run of other sizes in between
     chain(*other)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("C", [3, 700, 90001])
+@pytest.mark.parametrize("low", [-104.0, -1000.0])
+def test_distill_empty_rest_far_below_zero(low, C, dtype):
+    """Nothing above -inf outside the teacher's classes, whose logits all lie far below 0: the same bits as with `low`
+    taken off (the values and their differences are exact), and the oracle's."""
+    z = torch.full((2, C), -math.inf, dtype=DT[dtype])
+    z[:, [0, C // 2, C - 1]] = torch.tensor([[0.0, -8.0, -16.0], [0.0, 0.0, -8.0]], dtype=DT[dtype])
+    ids = np.int32([[C // 2, 0, C - 1]] * 2)
+    logp = np.log(np.float32([[0.5, 0.25, 0.25], [0.125, 0.75, 0.125]]))
+    near = run_distill(z.to(DEV), ids, logp, 4.0, True)
+    check_distill(z, ids, logp, 4.0, True, None, *near, dtype)
+    assert torch.isfinite(near[0]).all() and torch.isfinite(near[1]).all()
+    for t in (4.0, 0.125):
+        near, far = (run_distill((z + shift).to(DEV), ids, logp, t, True) for shift in (0.0, low))
+        assert torch.equal(near[0], far[0]) and torch.equal(near[1], far[1])

@@ -86,8 +86,8 @@ int rafiki_combine_topk(const void* logits, int dtype, long long ld_model, long 
  *             loss_i = T^2 [ the sum above + q_r (log q_r - log p_r) ]; q_r below 2^-20
  *             (rounding of the fp32 values), or with K all classes, counts as 0.
  * Terms with q = 0 are 0.  With Q = sum q + q_r the gradient is
- *   dz_c = T g_i (Q p_c - q_c) for c in K,  T g_i (Q p_c - q_r p_c / p_r) otherwise (q_r = 0
- *   without rest, or where p_r = 0: nothing above -inf outside K),
+ *   dz_c = T g_i (Q p_c - q_c) for c in K,  T g_i (Q p_c - q_r p_c / p_r) otherwise; q_r is 0 in both,
+ *   and in Q, without rest, and where p_r = 0 (nothing above -inf outside K, where q_r > 0 gives loss +inf),
  * where g_i = grad_loss[i] (fp32 [n], dL / d loss_i; null: 1); a row with g_i = 0 has gradient
  * 0 whatever it holds.  A class with p = 0 in K and q > 0 gives loss +inf; NaN, +inf or a row
  * of only -inf in the student, or NaN in the teacher, gives NaN.

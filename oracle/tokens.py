@@ -112,6 +112,8 @@ def distill(z, labels, logp, t=1.0, rest=False, g=1.0):
             loss += q_r * (math.log(q_r) - (lr - lse)) if lr > -np.inf else math.inf
         if lr > -np.inf:
             share[~member] = np.exp(x[~member] - lr)
+        else:
+            q_r = 0.0                   # p_r = 0: no class can take it, and the gradient is that of the others
     d = (q.sum() + q_r) * np.exp(lx) - q - q_r * share
     return t * t * loss, t * g * d if g != 0 else np.zeros(C)
 

@@ -340,7 +340,7 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
     q_r = 1.f - q_sum;
     if (q_r < kRestMin || members == (float)a.C) q_r = 0.f;
   }
-  const float big_q = q_sum + q_r;
+  const float big_q = q_sum + (sum == 0.f ? 0.f : q_r);       // where p_r = 0, q_r has a part in the loss alone
   const float log_all = log2f(sum_all);
 
   // ---- loss: a wave's part of the sum over K

@@ -858,3 +858,23 @@ def test_distill_empty_rest_far_below_zero(low, C, dtype):
     for t in (4.0, 0.125):
         near, far = (run_distill((z + shift).to(DEV), ids, logp, t, True) for shift in (0.0, low))
         assert torch.equal(near[0], far[0]) and torch.equal(near[1], far[1])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("C", [3, 64, 30001])
+def test_distill_rest_that_no_class_can_take(C, dtype):
+    """A teacher with mass for the other classes and a student that masks all of them: the loss is infinite, and the
+    gradient that of the teacher's classes alone, which sums to 0."""
+    z = torch.full((3, C), -math.inf, dtype=DT[dtype])
+    z[0, 0] = 1.0
+    z[1, :2] = torch.tensor([0.5, -1.0], dtype=DT[dtype])
+    z[2, [0, C - 1]] = torch.tensor([-300.0, -301.0], dtype=DT[dtype])
+    ids = np.int32([[0, -1], [0, 1], [C - 1, 0]])
+    logp = np.log(np.float32([[0.75, 1.0], [0.5, 0.125], [0.25, 0.25]]))
+    loss, grad = run_distill(z.to(DEV), ids, logp, 2.0, True)
+    check_distill(z, ids, logp, 2.0, True, None, loss, grad, dtype)
+    assert (loss == math.inf).all()
+    assert (grad[0] == 0).all()                            # p = 1 and all of the mass: exactly
+    # T times two terms of at most 1/2, off by some 8 roundings of 2^-24 each, and stored once
+    assert (grad.double().sum(1).abs() <= 2 * (2 * 0.5 * (8 * 2.0 ** -24 + HALF_STEP[dtype]))).all()
+    assert (grad[:, 2:C - 1] == 0).all()

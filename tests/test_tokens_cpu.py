@@ -153,3 +153,12 @@ def test_oracle_quantisation_ties():
     x = np.array([[127.0, 0.5, 1.5, -2.5, 63.5]], np.float32)        # scale 1
     q, s = ot.quantize_rows(x)
     assert s[0] == 1 and q.tolist() == [[127, 0, 2, -2, 64]]
+
+
+def test_oracle_gradient_of_a_rest_that_no_class_can_take():
+    """p_r = 0: q_r drops out of the gradient, which then sums to 0 over the classes that are left."""
+    loss, d = ot.distill(np.array([1.0, -np.inf, -np.inf]), np.array([0], np.int32), np.log([0.75]), 1.0, True)
+    assert loss == math.inf and np.array_equal(d, np.zeros(3))
+    loss, d = ot.distill(np.array([0.5, -1.0, -np.inf]), np.array([0, 1], np.int32), np.log([0.5, 0.125]), 2.0, True)
+    p = 1 / (1 + math.exp(-0.75))
+    assert loss == math.inf and abs(d[0] - 2 * (0.625 * p - 0.5)) < 1e-15 and abs(d.sum()) < 1e-15 and d[2] == 0

@@ -516,10 +516,19 @@ def _same_device(first, *others):
             raise ValueError(f"tensors on {first.device} and {t.device}")
 
 
+def _torch_stream(stream, device):
+    """torch's stream object of ``stream``, one already or a hipStream_t (0: the null stream, which is torch's
+    default one; an ExternalStream of 0 would be a new stream)."""
+    import torch
+    if not isinstance(stream, int):
+        return stream
+    return torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+
+
 def _call(first, stream, need, workspace, fn, *args):
     """Calls a C function on the device of tensor ``first`` and on ``stream`` (None: the current stream of
     that device), with a workspace of ``need`` bytes where it takes one (need None: it does not).  A workspace
-    that is not given is taken from torch's allocator for the time of the work."""
+    that is not given is taken from torch's allocator, on the call's stream, for the time of the work."""
     import torch
     index = first.device.index
     if torch._C._cuda_getDevice() != index:
@@ -540,9 +549,13 @@ def _call(first, stream, need, workspace, fn, *args):
         return _check(fn(*args, workspace.data_ptr(), workspace.numel() * workspace.element_size(), handle))
     if not need:
         return _check(fn(*args, 0, 0, handle))
-    workspace = torch.empty(need, dtype=torch.uint8, device=first.device)
-    if stream is not None:              # allocated for the current stream: kept until `stream` has passed
-        workspace.record_stream(torch.cuda.ExternalStream(handle, device=first.device))
+    if stream is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=first.device)
+    else:
+        # from that stream's own memory: a block of the current stream's may still be read by its earlier work, and
+        # be taken by its next allocation, which `stream` is ordered with neither of
+        with torch.cuda.stream(_torch_stream(stream, first.device)):
+            workspace = torch.empty(need, dtype=torch.uint8, device=first.device)
     return _check(fn(*args, workspace.data_ptr(), need, handle))
 
 

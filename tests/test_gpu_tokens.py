@@ -878,3 +878,81 @@ def test_distill_rest_that_no_class_can_take(C, dtype):
     # T times two terms of at most 1/2, off by some 8 roundings of 2^-24 each, and stored once
     assert (grad.double().sum(1).abs() <= 2 * (2 * 0.5 * (8 * 2.0 ** -24 + HALF_STEP[dtype]))).all()
     assert (grad[:, 2:C - 1] == 0).all()
+
+
+@pytest.mark.parametrize("which", ["null", "default", "side", "number"])
+def test_workspace_belongs_to_the_stream_of_the_call(which):
+    """Without a workspace, on another stream than the current one: the block is not one that the current stream's queued
+    work still reads, and not one that its next allocations get while the call runs.  Blocks of one size, each
+    stream kept busy first."""
+    rng = np.random.default_rng(42)
+    n, C = 64, 30000
+    z = lm_logits(rng, 1, n, C, "fp32").to(DEV)
+    par = mixed_params(rng, n)
+    need = bd.combine_workspace(1, n, C)
+    args = {k: dev(v) for k, v in par.items()}
+    u = args.pop("uniform")
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    a = torch.randn(2048, 2048, device=DEV)
+    target = {"null": torch.cuda.default_stream(), "default": torch.cuda.default_stream(), "side": other,
+              "number": other}[which]
+    given = {"null": 0, "default": target, "side": target, "number": other.cuda_stream}[which]
+    labels, probs = empty_sample(n)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            block = torch.full((need,), 5, dtype=torch.uint8, device=DEV)
+            for _ in range(8):
+                b = a @ a
+            copy = block.clone()                                 # read late; the block is free again for this stream
+            del block
+            with torch.cuda.stream(target):
+                for _ in range(8):
+                    c = a @ a
+            bd.combine_sample(z, u, labels, probs, stream=given, **args)
+            junk = [torch.full((need,), 3, dtype=torch.uint8, device=DEV) for _ in range(4)]
+        torch.cuda.synchronize()
+        assert (copy == 5).all() and all((j == 3).all() for j in junk)
+        check_sample(z[:, ::7], {k: v[::7] for k, v in par.items()}, labels[::7], probs[::7])
+        del b, c, junk
+
+
+def test_replayed_graph_of_calls_that_take_their_workspace():
+    """Captured without workspaces: the graph's own memory holds them, which eager calls and allocations between the
+    replays leave alone."""
+    rng = np.random.default_rng(43)
+    z = lm_logits(rng, 2, 9, 3001, "fp32").to(DEV)
+    par = mixed_params(rng, 9)
+    args = {k: dev(v) for k, v in par.items()}
+    u = args.pop("uniform")
+    n, c_in, c_out = 64, 4096, 1000                              # few tiles: K is split through a workspace
+    assert bd.fc_i8_workspace(n, c_in, c_out) > 0
+    x = torch.from_numpy(rng.integers(-128, 128, (n, c_in), dtype=np.int8)).to(DEV)
+    w = torch.from_numpy(rng.integers(-128, 128, (c_out, c_in), dtype=np.int8)).to(DEV)
+    one = lambda k: torch.full((k,), 0.01, device=DEV)  # noqa: E731
+    sx, sw = one(n), one(c_out)
+    out = [empty_sample(9), torch.empty((n, c_out), device=DEV)]
+
+    def calls():
+        bd.combine_sample(z, u, *out[0], **args)
+        bd.fc_i8(x, sx, w, sw, out[1])
+
+    calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for step in range(4):
+        gen = torch.Generator(device=DEV).manual_seed(step)
+        u.copy_(torch.rand(9, generator=gen, device=DEV))
+        x.copy_(torch.randint(-128, 128, x.shape, generator=gen, device=DEV))
+        for t in (*out[0], out[1]):
+            t.fill_(-7)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (*out[0], out[1])]
+        junk = [torch.full((1 << s,), 9, dtype=torch.uint8, device=DEV) for s in (16, 18, 20, 22)]
+        calls()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (*out[0], out[1])))
+        del junk

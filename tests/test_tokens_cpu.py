@@ -162,3 +162,50 @@ def test_oracle_gradient_of_a_rest_that_no_class_can_take():
     loss, d = ot.distill(np.array([0.5, -1.0, -np.inf]), np.array([0, 1], np.int32), np.log([0.5, 0.125]), 2.0, True)
     p = 1 / (1 + math.exp(-0.75))
     assert loss == math.inf and abs(d[0] - 2 * (0.625 * p - 0.5)) < 1e-15 and abs(d.sum()) < 1e-15 and d[2] == 0
+
+
+# ---------------------------------------------------------------- workspaces that the binding takes itself
+
+@pytest.mark.parametrize("stream", ["none", "null", "number", "default", "object"])
+def test_workspace_is_the_stream_s_own(monkeypatch, stream):
+    """A workspace that the caller does not give is allocated with the stream of the call current, so that neither what
+    the current stream still does with a block nor its next allocation meets the work on the other stream.  torch's
+    streams and allocator are stand-ins here: what counts is which stream was current at the allocation."""
+    import contextlib
+    import types
+
+    import torch
+    device = torch.device("cuda", 0)
+    make = lambda handle: types.SimpleNamespace(cuda_stream=handle, device=device)  # noqa: E731
+    current, default = make(7), make(0)
+    state, taken, calls = {"current": current}, [], []
+
+    @contextlib.contextmanager
+    def use(s):
+        before, state["current"] = state["current"], s
+        yield
+        state["current"] = before
+
+    def external(handle, device=None):
+        assert handle, "torch makes a new stream of an external one without a handle"
+        return make(handle)
+
+    class Block:
+        def data_ptr(self):
+            return P
+
+    def empty(need, dtype, device):
+        assert need == 640
+        taken.append(state["current"].cuda_stream)
+        return Block()
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: state["current"].cuda_stream, raising=False)
+    monkeypatch.setattr(torch.cuda, "stream", use)
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda device=None: default)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", external)
+    monkeypatch.setattr(torch, "empty", empty)
+    given, want = {"none": (None, 7), "null": (0, 0), "number": (99, 99), "default": (default, 0),
+                   "object": (make(55), 55)}[stream]
+    bd._call(types.SimpleNamespace(device=device), given, 640, None, lambda *a: calls.append(a) or 0, "x")
+    assert taken == [want] and calls == [("x", P, 640, want)] and state["current"] is current

@@ -399,13 +399,23 @@ struct Row {
     }
   }
 
+  // (z - top) k in fp32, for bounds: (z h - top h) by, h by = k.  Halves first, since two finite logits may
+  // lie further apart than fp32 holds.  NaN for z = -inf at T = +inf.
+  struct Difference {
+    float h, by;
+    __device__ __forceinline__ float operator()(float z, float top) const { return (z * h - top * h) * by; }
+  };
+  __device__ __forceinline__ Difference difference() const {
+    return Difference{0.5f, fminf((float)(2.0 * k), 3e38f)};   // 0 by stays 0
+  }
+
   // Bounds of log2 p over G groups of 64 classes (g0 + j NT + the thread): one of a group's classes reaches
   // `low`, none exceeds `high`; -inf past the last group, and where p is too small to matter.  `best` is
   // best_score().  The groups' maxima of one model are in flight together.
   static constexpr int G = 4;
   __device__ __forceinline__ void group_scores(int g0, float best, float (&low)[G], float (&high)[G]) const {
     const int groups = a.units * kUnitTops;
-    const float kf = fminf((float)k, 3e38f);                 // 0 kf stays 0
+    const Difference scaled = difference();
 #pragma unroll
     for (int j = 0; j < G; ++j) {
       low[j] = -INFINITY;
@@ -430,7 +440,7 @@ struct Row {
       const float top = sh.top[m], log_scale = sh.log_scale[m];
 #pragma unroll
       for (int j = 0; j < G; ++j) {
-        const float t = (v[j] - top) * kf + log_scale;
+        const float t = scaled(v[j], top) + log_scale;
         const bool some = t > -2048.f;                       // also false for the NaN of an infinite product
         low[j] = some ? fmaxf(low[j], t) : low[j];
         high[j] += some ? __builtin_amdgcn_exp2f(t - best) : 0.f;
@@ -472,7 +482,7 @@ struct Row {
         if (low > -INFINITY) atomicAdd(&sh.counts[(int)fminf((best - low) * kBinsPerOctave, (float)(kBins - 1))], 1u);
       };
       if (classes) {
-        const float kf = fminf((float)k, 3e38f);
+        const Difference scaled = difference();
         for (int u = threadIdx.x >> 6; u < a.units; u += kWaves) {
           float low[16];
 #pragma unroll
@@ -483,7 +493,7 @@ struct Row {
             unit_logits(u, m, z);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const float t = (z[i] - sh.top[m]) * kf + sh.log_scale[m];
+              const float t = scaled(z[i], sh.top[m]) + sh.log_scale[m];
               low[i] = t > -2048.f ? fmaxf(low[i], t) : low[i];
             }
           }
@@ -798,7 +808,7 @@ struct Row {
       lo = log2f((float)__longlong_as_double((long long)prefix_bits)) - kSlack;
       if (!(lo > -120.f)) lo = -INFINITY;
     }
-    const float kf = fminf((float)k, 3e38f);
+    const Difference scaled = difference();
     for (int u = threadIdx.x; u < a.units; u += NT) sh.unit_ties[u] = 0;
     u64 above = 0;
     auto take = [&](u64 x, int c) {
@@ -817,7 +827,7 @@ struct Row {
         unit_logits(u, 0, z);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float t = (z[i] - sh.top[0]) * kf + sh.log_scale[0];
+          const float t = scaled(z[i], sh.top[0]) + sh.log_scale[0];
           if (!(t < lo)) {
             const u64 x = (u64)__double_as_longlong(__builtin_fma(weight(z[i], sh.top[0], k), sh.scale[0], 0.0));
             take(x < kLeastKey ? 0 : x, unit_class(u, i));

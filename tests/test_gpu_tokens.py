@@ -956,3 +956,42 @@ def test_replayed_graph_of_calls_that_take_their_workspace():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, (*out[0], out[1])))
         del junk
+
+
+# Logits of both signs that lie further apart than fp32 can hold: their differences and bounds stay finite.
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("S", [1, 2])
+@pytest.mark.parametrize("C", [900, 2000])
+def test_sample_span_beyond_fp32(C, S, dtype):
+    rng = np.random.default_rng(51)
+    n = 8
+    z = torch.from_numpy(np.float32(3.3e38) * (2 * rng.random((S, n, C)).astype(np.float32) - 1)).to(DT[dtype])
+    z[:, 0] = -3e38
+    z[:, 0, :64] = 3e38
+    z[:, 1] = z[:, 0]
+    z = z.to(DEV)
+    par = {"uniform": np.float32([0.9, 0.9, 0.9, 0.3, 0.999, 0.7, 0.6, 0.4]),
+           "temperature": np.float32([math.inf, 3e38, math.inf, 3e38, 3e38, 2e38, 0, math.inf]),
+           "top_k": np.int32([0, 0, 0, C * 3 // 4, 600, 0, 0, C - 1]),
+           "top_p": np.float32([1, 0.9, 0.75, 1, 1, 0.97, 1, 1]),
+           "min_p": np.float32([0.1, 0, 0, 0, 0, 0.05, 0, 0.5])}
+    check_sample(z, par, *run_sample(z, par))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("S", [1, 3])
+@pytest.mark.parametrize("C,k", [(2000, 20), (2000, 700), (2000, 1000), (700, 300), (70000, 64)])
+def test_topk_span_beyond_fp32(C, k, S, dtype):
+    rng = np.random.default_rng(52)
+    t = np.float32(3e37)
+    z = (np.float32(3.3e38) * (2 * rng.random((S, 4, C)).astype(np.float32) - 1))
+    z[:, 1] = -3e38
+    z[:, 1, ::97] = 3e38
+    z[:, 2] *= np.float32(0.01)
+    z = torch.from_numpy(z).to(DT[dtype]).to(DEV)
+    labels = torch.empty((4, k), dtype=torch.int32, device=DEV)
+    logp = torch.empty((4, k), device=DEV)
+    bd.combine_topk(z, labels, logp, temperature=float(t))
+    torch.cuda.synchronize()
+    check_topk(z, k, t, labels, logp)

@@ -399,14 +399,16 @@ struct Row {
     }
   }
 
-  // (z - top) k in fp32, for bounds: (z h - top h) by, h by = k.  Halves first, since two finite logits may
-  // lie further apart than fp32 holds.  NaN for z = -inf at T = +inf.
+  // (z - top) k in fp32, for bounds: (z h - top h) by again, h by again = k.  Halves first, since two finite logits
+  // may lie further apart than fp32 holds.  For T below about 2^-125, k is beyond fp32 (up to 2^150) and the differences
+  // that matter below its normal range, where halves lose bits: whole ones by 2^64 first; those that overflow
+  // then are -inf to scale too.  NaN for z = -inf at T = +inf.
   struct Difference {
-    float h, by;
-    __device__ __forceinline__ float operator()(float z, float top) const { return (z * h - top * h) * by; }
+    float h, by, again;
+    __device__ __forceinline__ float operator()(float z, float top) const { return (z * h - top * h) * by * again; }
   };
   __device__ __forceinline__ Difference difference() const {
-    return Difference{0.5f, fminf((float)(2.0 * k), 3e38f)};   // 0 by stays 0
+    return k < 0x1p126 ? Difference{0.5f, (float)(2.0 * k), 1.f} : Difference{1.f, 0x1p64f, (float)(k * 0x1p-64)};
   }
 
   // Bounds of log2 p over G groups of 64 classes (g0 + j NT + the thread): one of a group's classes reaches

@@ -995,3 +995,21 @@ def test_topk_span_beyond_fp32(C, k, S, dtype):
     bd.combine_topk(z, labels, logp, temperature=float(t))
     torch.cuda.synchronize()
     check_topk(z, k, t, labels, logp)
+
+
+@pytest.mark.parametrize("S", [1, 2])
+def test_temperatures_and_logits_below_the_normal_range(S):
+    """T and the logits' differences of the size of fp32's smallest values: their quotients are ordinary numbers."""
+    rng = np.random.default_rng(54)
+    C, k = 3000, 40
+    z = np.float32(1e-41) * rng.integers(-1000, 1000, (S, 4, C)).astype(np.float32)
+    t = np.float32(2e-39)
+    par = {"uniform": np.float32([0.2, 0.5, 0.8, 0.3]), "temperature": np.float32([t] * 4),
+           "top_k": np.int32([50, 0, 0, 1500]), "top_p": np.float32([1, 0.5, 1, 0.99]), "min_p": np.float32([0, 0, 0.2, 0])}
+    z = dev(z)
+    check_sample(z, par, *run_sample(z, par))
+    labels = torch.empty((4, k), dtype=torch.int32, device=DEV)
+    logp = torch.empty((4, k), device=DEV)
+    bd.combine_topk(z, labels, logp, temperature=float(t))
+    torch.cuda.synchronize()
+    check_topk(z, k, t, labels, logp)

@@ -560,7 +560,10 @@ struct Row {
     return (int)sh.n_groups;
   }
 
-  // Lists every class whose log2 p reaches score (and some below it); false where they do not fit.
+  // Lists every class whose log2 p reaches score - kSlack / 2, and none below: half of the slack above the bound of the
+  // groups, whose fp32 scores may be off in their last places, so that the list has no gap above its least class and may
+  // be cut anywhere (of equal classes at the groups' own bound, those in groups with a better class would be listed
+  // and the others not).  Gaps remain below 2^-120, where no class has units and no sum ends.  False where they do not fit.
   __device__ __forceinline__ bool list(float score, float best) {
     const int lane = threadIdx.x & 63;
     const uint32_t* groups = (const uint32_t*)sh.sums;
@@ -568,7 +571,7 @@ struct Row {
     if (listed > kMaxGroupsListed) return false;
     if (threadIdx.x == 0) sh.n_list = 0;
     __syncthreads();
-    const u64 least = score > -1000.f ? (u64)__double_as_longlong((double)exp2f(fmaxf(score - kSlack, -120.f))) : 1;
+    const u64 least = score > -1000.f ? (u64)__double_as_longlong((double)exp2f(fmaxf(score - 0.5f * kSlack, -120.f))) : 1;
     for (int i = (threadIdx.x >> 6) * G; i < listed; i += kWaves * G) {
       int c[G];
       u64 x[G];

@@ -1013,3 +1013,33 @@ def test_temperatures_and_logits_below_the_normal_range(S):
     bd.combine_topk(z, labels, logp, temperature=float(t))
     torch.cuda.synchronize()
     check_topk(z, k, t, labels, logp)
+
+
+def test_sample_top_p_cut_at_the_border_of_the_list():
+    """A nucleus that ends among equal classes exactly where the row kernel's list of classes ends.  One class leads; the
+    upper 64 groups of 64 classes hold one second class each, which set the list's bound; every group holds one of the equal
+    classes, whose log2 p differs from the bound in the last places only (T was picked for the fp32 rounding of 1 / T).
+    The first of them, by index, are in the nucleus, whichever group they are in."""
+    C, groups = 8192, 128
+    t = np.float32(1.4425914287567139)
+    k = 1.4426950408889634 / float(t)
+    z, top_p = [], []
+    for b in range(24, 232):
+        border = np.float32(((b + 1) / 16 + 1 / 32) / k)
+        for step in range(-2, 3):
+            third = (border.view(np.int32) + step).view(np.float32)
+            second = np.float32((b + 0.5) / 16 / k)
+            row = np.full(C, -np.inf, np.float32)
+            row[1::64] = -third
+            row[C // 2::64] = -second
+            row[C // 2 + 5] = 0
+            z.append(row)
+            p2, p3 = 2.0 ** (-float(second) * k), 2.0 ** (-float(third) * k)
+            # half a class off the next border: 2^-16 of the whole at least, far above the fp32 step of top_p
+            top_p.append((1 + groups // 2 * p2 + 10.5 * p3) / (1 + groups // 2 * p2 + groups * p3))
+    n = len(z)
+    z = dev(np.stack(z)[None])
+    par = {"uniform": np.zeros(n, np.float32), "temperature": np.full(n, t), "top_p": np.float32(top_p)}
+    labels, probs = run_sample(z, par)
+    assert (labels == 1).all(), torch.nonzero(labels != 1)[:, 0].tolist()
+    check_sample(z[:, ::37], {k: v[::37] for k, v in par.items()}, labels[::37], probs[::37])

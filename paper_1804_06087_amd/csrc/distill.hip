@@ -95,7 +95,10 @@ __device__ __forceinline__ void lds_barrier() {
 __device__ __forceinline__ float reference(float top) { return top == -INFINITY ? 0.f : top; }
 
 // NT threads hold a row of up to NT CH + 2 chunks, the two edges among them (CH = 0: any length, not held).
-template <bool BF16, bool REST, int NT, int CH, int OCC>
+// WIDE: the logits are halved as they are read, and T with them, since two finite ones may lie further apart than fp32
+// holds.  It is for T above 2^120: below, such a difference is more than 2^8 T, whose power is 0 in fp32 as that of
+// -inf is.  (Halves in the differences of every row instead: 300 us for 2047 x 131071, against 292.)
+template <bool BF16, bool REST, int NT, int CH, int OCC, bool WIDE>
 __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
   constexpr int V = BF16 ? 8 : 4, NW = NT / 64;
   extern __shared__ uint32_t marks[];                        // rest: bit c + shift is set for c in K
@@ -105,8 +108,8 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
   constexpr uint32_t kMasked = BF16 ? 0xFF80FF80u : 0xFF800000u;     // -inf in every place
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   // Powers are of (z - top) s, not of z s - top s: masks of the type's lowest value overflow the products,
-  // and a row of nothing else is a uniform one.  T below 2^-127 counts as that, which keeps 0 s at 0.
-  const float s = fminf(kLog2e / a.t, 0x1p127f);
+  // and a row of nothing else is a uniform one.  T below log2(e) 2^-127 (no normal T is) counts as that, which keeps 0 s at 0.
+  const float s = fminf(kLog2e / (WIDE ? 0.5f * a.t : a.t), 0x1p127f);
   const int row = a.row0 + blockIdx.x;
   const float g = a.grad_loss ? a.grad_loss[row] : 1.f;
   const long long base = row * a.ld_row, gbase = row * a.ld_grad;
@@ -123,8 +126,18 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
   const uint32_t edge_own = a.C < V ? (tid == 0 ? (1u << a.C) - 1 : 0u)
                             : tid == 0 ? (1u << (V - shift)) - 1
                                        : ~0u << (chunks * V - shift - a.C) & ((1u << V) - 1);
+  auto halved = [&](u32x4 q) {
+    if constexpr (WIDE) {
+      float z[V];
+      unpack<BF16, V>(q, z);
+#pragma unroll
+      for (int j = 0; j < V; ++j) z[j] *= 0.5f;
+      q = pack<BF16, V>(z);
+    }
+    return q;
+  };
   auto load = [&](int i) {
-    return __builtin_nontemporal_load((const u32x4*)(x_row + (long long)i * NT * 16 + (unsigned)(tid + 1) * 16u));
+    return halved(__builtin_nontemporal_load((const u32x4*)(x_row + (long long)i * NT * 16 + (unsigned)(tid + 1) * 16u)));
   };
   auto store = [&](int i, const float d[V]) {
     __builtin_nontemporal_store(pack<BF16, V>(d), (u32x4_any*)(d_row + (long long)i * NT * 16 + (unsigned)(tid + 1) * 16u));
@@ -141,7 +154,7 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
         q = pack<BF16, V>(z);
       }
     }
-    return q;
+    return halved(q);
   };
   auto store_edge = [&](const float d[V]) {
     if (has_edge && a.C >= V) {
@@ -268,7 +281,7 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
           q += slot_q[o];
         }
       if (first) {
-        z_class[i] = element<BF16>(a.logits, base + id);
+        z_class[i] = element<BF16>(a.logits, base + id) * (WIDE ? 0.5f : 1.f);
         q_class[i] = q;
         member_top = fmaxf(member_top, z_class[i]);
         members += 1.f;
@@ -343,13 +356,14 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
   const float big_q = q_sum + (sum == 0.f ? 0.f : q_r);       // where p_r = 0, q_r has a part in the loss alone
   const float log_all = log2f(sum_all);
 
-  // ---- loss: a wave's part of the sum over K
+  // ---- loss: a wave's part of the sum over K.  A logarithm stays finite as long as fp32 holds it.
+  auto log2_ratio = [&](float z, float top) { return (0.5f * z - 0.5f * top) * s * 2.f; };
   if (a.loss) {
     float part = 0.f;
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
       const float q = q_class[i];
-      if (q > 0.f || q != q) part += q * (logf(q) - kLn2 * ((z_class[i] - top_all) * s - log_all));
+      if (q > 0.f || q != q) part += q * (logf(q) - kLn2 * (log2_ratio(z_class[i], top_all) - log_all));
     }
     part = wave_add(part);
     if (lane == 0) w_part[wave] = part;
@@ -376,7 +390,7 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
     float part = 0.f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) part += w_part[w];
-    if (q_r > 0.f) part += sum == 0.f ? INFINITY : q_r * (logf(q_r) - kLn2 * (log2f(sum) + (top_r - top_all) * s - log_all));
+    if (q_r > 0.f) part += sum == 0.f ? INFINITY : q_r * (logf(q_r) - kLn2 * (log2f(sum) + log2_ratio(top_r, top_all) - log_all));
     a.loss[row] = defined ? a.t * a.t * part : NAN;
   }
   if (a.grad && g != 0.f) {
@@ -389,14 +403,14 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
   }
 }
 
-template <bool BF16, bool REST, int NT, int CH, int OCC>
+template <bool BF16, bool REST, int NT, int CH, int OCC, bool WIDE = false>
 hipError_t launch_rows(const DistillArgs& a, hipStream_t s) {
   const size_t lds = REST ? ((size_t)a.C + 16 + 31) / 32 * 4 + 4 : 0;   // and a word behind
   DistillArgs part = a;
   for (long long row = 0; row < a.n; row += 1 << 20) {       // 2^20 rows a launch at most
     part.row0 = (int)row;
     const int rows = (int)std::min<long long>(a.n - row, 1 << 20);
-    launch_lds(distill_kernel<BF16, REST, NT, CH, OCC>, dim3(rows), dim3(NT), lds, s, part);
+    launch_lds(distill_kernel<BF16, REST, NT, CH, OCC, WIDE>, dim3(rows), dim3(NT), lds, s, part);
     const hipError_t st = hipGetLastError();
     if (st != hipSuccess) return st;
   }
@@ -407,6 +421,7 @@ template <bool BF16, bool REST>
 hipError_t launch_by_length(const DistillArgs& a, hipStream_t s) {
   constexpr int V = BF16 ? 8 : 4;
   const int held = a.C + V - 1 - 2 * V;                      // classes between the edges, with the longest shift
+  if (a.t > 0x1p120f) return launch_rows<BF16, REST, 1024, 0, 4, true>(a, s);
   // Few threads with many chunks each: more rows share a compute unit, and one's loads run beside another's
   // arithmetic (30000 bf16 classes: 151 us in 512 threads of 8 chunks, 129 us in 256 of 16).
   if (held <= 128 * 2 * V) return launch_rows<BF16, REST, 128, 2, 4>(a, s);

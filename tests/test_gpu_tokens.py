@@ -1043,3 +1043,45 @@ def test_sample_top_p_cut_at_the_border_of_the_list():
     labels, probs = run_sample(z, par)
     assert (labels == 1).all(), torch.nonzero(labels != 1)[:, 0].tolist()
     check_sample(z[:, ::37], {k: v[::37] for k, v in par.items()}, labels[::37], probs[::37])
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("C,t", [(5, 1e38), (700, 1e38), (90001, 1e38), (1001, 3e38), (170000, 1.4e36), (301, 1.3e36), (301, 1e36)])
+def test_distill_span_beyond_fp32(C, t, dtype, rest):
+    """Student logits of both signs further apart than fp32 can hold, at a temperature of their size: T^2 is beyond fp32
+    and the loss with it, the gradient is not.  The terms Q p_c, q_c and q_r p_c / p_r (at most 2 together) are off by the
+    bounds of 32 bits relative to each; and a power below 2^-126 is 0, which T times it may not be: T 2^-125."""
+    rng = np.random.default_rng(53)
+    t = float(np.float32(t))
+    z = torch.from_numpy(np.float32(3.3e38) * (2 * rng.random((3, C)).astype(np.float32) - 1)).to(DT[dtype])
+    z[1] = -3e38
+    z[1, [1, C - 2]] = 3e38
+    z[2] = 3e38
+    z[2, [0, C - 1]] = -3e38
+    ids = np.int32([[0, C - 1]] * 3)
+    logp = np.log(np.float32([[0.5, 0.25]] * 3))
+    loss, grad = run_distill(z.to(DEV), ids, logp, t, rest)
+    zh, got = host(z).astype(np.float64), host(grad).astype(np.float64)
+    for i in range(3):
+        _, want = ot.distill(zh[i], ids[i], logp[i], t, rest)
+        terms = 2 * np.exp(zh[i] / t - ot._lse(zh[i] / t)) + np.abs(want) / t
+        np.add.at(terms, ids[i], 1.0)
+        eps = 2 * distill_bounds(zh[i], C, 2, t, 1.0, dtype) + 2 * 2.0 ** -22
+        assert (np.abs(got[i] - want) <= t * (terms * eps + 2.0 ** -125) + np.abs(want) * HALF_STEP[dtype]).all(), i
+    assert (loss == math.inf).all()
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_distill_loss_of_a_span_beyond_fp32(dtype, rest):
+    """The type's lowest value beside its largest at an ordinary temperature: log p = -2 max / T is within fp32, and so is the
+    loss, T times the difference for each class, of little weight."""
+    top = float(torch.finfo(DT[dtype]).max)
+    t, q = 8.0, 2.0 ** -8
+    z = torch.full((1, 100), -top, dtype=DT[dtype], device=DEV)
+    z[0, 5] = top
+    loss, grad = run_distill(z, np.int32([[5, 50]]), np.log(np.float32([[1 - q, q]])), t, rest)
+    want = t * q * 2 * top
+    assert abs(float(loss) - want) <= 1e-5 * want          # q = exp(log q): 2^-24 (1 + |log q|), some 10 roundings
+    check_distill(z, np.int32([[5, 50]]), np.log(np.float32([[1 - q, q]])), t, rest, None, None, grad, dtype)

@@ -391,7 +391,7 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
 #pragma unroll
     for (int w = 0; w < NW; ++w) part += w_part[w];
     if (q_r > 0.f) part += sum == 0.f ? INFINITY : q_r * (logf(q_r) - kLn2 * (log2f(sum) + log2_ratio(top_r, top_all) - log_all));
-    a.loss[row] = defined ? a.t * a.t * part : NAN;
+    a.loss[row] = defined ? a.t * (a.t * part) : NAN;      // T^2 alone may be beyond fp32 where its product is not
   }
   if (a.grad && g != 0.f) {
 #pragma unroll

@@ -1085,3 +1085,20 @@ def test_distill_loss_of_a_span_beyond_fp32(dtype, rest):
     want = t * q * 2 * top
     assert abs(float(loss) - want) <= 1e-5 * want          # q = exp(log q): 2^-24 (1 + |log q|), some 10 roundings
     check_distill(z, np.int32([[5, 50]]), np.log(np.float32([[1 - q, q]])), t, rest, None, None, grad, dtype)
+
+
+@pytest.mark.parametrize("t", [1e-20, 1e-25, 1e-30])
+def test_distill_loss_where_the_square_of_t_underflows(t):
+    """T^2 is below fp32, T^2 times the loss's sum is not: one class against a sure student, loss = T (difference)."""
+    z = torch.tensor([[1.0, 3.0, 2.0], [0.5, -1.0, 0.25]], device=DEV)
+    loss, _ = run_distill(z, np.int32([[0], [1]]), np.float32([[0.0], [0.0]]), t, False)
+    want = float(np.float32(t)) * np.array([2.0, 1.5])
+    assert np.abs(host(loss).astype(np.float64) - want).max() <= 1e-6 * want.min()       # some 10 roundings of 2^-24
+
+
+def test_distill_loss_where_the_square_of_t_overflows():
+    """A student that agrees exactly has loss 0 whatever T is."""
+    z = torch.tensor([[7.0], [-3.0]], device=DEV)
+    for t in (1e19, 1e25, 3e38):
+        loss, grad = run_distill(z, np.int32([[0], [0]]), np.float32([[0.0], [0.0]]), t, False)
+        assert (loss == 0).all() and (grad == 0).all()

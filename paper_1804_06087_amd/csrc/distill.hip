@@ -375,7 +375,8 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
       zero_row();
     } else {
       const float p_r = REST ? part_r / sum_all : 1.f;
-      const float factor = sum == 0.f ? (defined ? 0.f : NAN) : scale * (big_q * p_r - q_r) / sum;
+      const bool nan = !defined || big_q != big_q;           // of the student, of the teacher
+      const float factor = sum == 0.f ? (nan ? NAN : 0.f) : scale * (big_q * p_r - q_r) / sum;
       for_chunks([&](const float* z, uint32_t, auto&& store_chunk) {
         float d[V];
 #pragma unroll

@@ -1102,3 +1102,12 @@ def test_distill_loss_where_the_square_of_t_overflows():
     for t in (1e19, 1e25, 3e38):
         loss, grad = run_distill(z, np.int32([[0], [0]]), np.float32([[0.0], [0.0]]), t, False)
         assert (loss == 0).all() and (grad == 0).all()
+
+
+@pytest.mark.parametrize("C", [3, 500])
+def test_distill_nan_teacher_with_nothing_outside(C):
+    """NaN in the teacher gives NaN throughout the row, also where the student masks every other class."""
+    z = torch.full((1, C), -math.inf, device=DEV)
+    z[0, :2] = 1.0
+    loss, grad = run_distill(z, np.int32([[0, 1]]), np.float32([[math.nan, -1.0]]), 1.0, True)
+    assert torch.isnan(loss).all() and torch.isnan(grad).all()

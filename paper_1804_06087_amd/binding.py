@@ -666,10 +666,12 @@ def fc_i8(x, x_scale, w, w_scale, y, bias=None, relu: bool = False, workspace=No
     n, c_in = x.shape
     c_out = w.shape[0]
     ld_x, ld_w, ld_y = _rows(x, "x"), _rows(w, "w"), _rows(y, "y")
+    k16 = (c_in + 15) // 16 * 16                             # rows are read up to there
+    ld_x, ld_w = ld_x if n > 1 else k16, ld_w if c_out > 1 else k16   # one row has no distance to the next
     if x.dtype != torch.int8 or w.dtype != torch.int8 or w.shape[1] != c_in or y.shape != (n, c_out):
         raise ValueError("expected int8 x [n, c_in], int8 w [c_out, c_in] and y [n, c_out]")
-    for t, ld, name in ((x, ld_x, "x"), (w, ld_w, "w")):     # rows are read up to a multiple of 16
-        end = t.storage_offset() + (t.shape[0] - 1) * ld + (c_in + 15) // 16 * 16
+    for t, ld, name in ((x, ld_x, "x"), (w, ld_w, "w")):
+        end = t.storage_offset() + (t.shape[0] - 1) * ld + k16
         if end > t.untyped_storage().nbytes():
             raise ValueError(f"{name}: the last row is not readable up to the next multiple of 16")
     if x_scale is None or w_scale is None:

@@ -1111,3 +1111,25 @@ def test_distill_nan_teacher_with_nothing_outside(C):
     z[0, :2] = 1.0
     loss, grad = run_distill(z, np.int32([[0, 1]]), np.float32([[math.nan, -1.0]]), 1.0, True)
     assert torch.isnan(loss).all() and torch.isnan(grad).all()
+
+
+def test_fc_one_row_of_any_distance():
+    """A matrix of one row has no distance between rows: only the row's own place counts."""
+    rng = np.random.default_rng(55)
+    c_in, c_out = 200, 33
+    x = rng.integers(-128, 128, (1, c_in), dtype=np.int8)
+    w = rng.integers(-128, 128, (c_out, c_in), dtype=np.int8)
+    sx, sw = rng.random(1).astype(np.float32), rng.random(c_out).astype(np.float32)
+    xp, wp = padded(x), padded(w)
+    for row in (xp[0].unsqueeze(0), xp.as_strided((1, c_in), (1 << 23, 1)), xp.as_strided((1, c_in), (0, 1))):
+        y = torch.empty((1, c_out), device=DEV)
+        bd.fc_i8(row, dev(sx), wp, dev(sw), y)
+        torch.cuda.synchronize()
+        check_fc(x, sx, w, sw, None, False, y, "fp32")
+    y = torch.empty((3, 1), device=DEV)                   # one output, three rows
+    bd.fc_i8(wp[:3], dev(sw[:3]), xp[0].unsqueeze(0), dev(sx), y)
+    torch.cuda.synchronize()
+    check_fc(w[:3], sw[:3], x, sx, None, False, y, "fp32")
+    with pytest.raises(ValueError):                       # not readable up to the next multiple of 16
+        bd.fc_i8(torch.zeros(c_in, dtype=torch.int8, device=DEV).unsqueeze(0), dev(sx), wp, dev(sw),
+                 torch.empty((1, c_out), device=DEV))

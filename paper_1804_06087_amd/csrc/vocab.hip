@@ -42,14 +42,15 @@ constexpr u64 kLeastKey = (u64)(1023 - 1000) << 52;         // bits of 2^-1000
 constexpr float kSlack = 1.f / 64;
 constexpr float kBinsPerOctave = 16.f;
 
-// 2^t, t <= 0 (below -1010, for -inf and for NaN: 2^-1010, less than any probability that counts).
+// 2^t, t <= 0 (below -1020, for -inf and for NaN: 2^-1020, less than any probability that counts, and so little that a
+// class of 2^-1000 from one of 32 models is off by 2^-15 at most, half a step of its logarithm in fp32).
 // t = n + f, |f| <= 1/2: adding 1.5 2^52 leaves n in the low bits, and n goes into the exponent as an integer,
 // since conversions, rint and ldexp of 64 bits take four times an FMA's cycles (with them stats_kernel
 // took 300 us for 2 x 1024 x 131072).  2^f = 1 + f q(f) with q of degree 8 through (2^f - 1) / f at
 // Chebyshev's nodes: within 4e-14, and exactly 1 at f = 0.
 __device__ __forceinline__ double power2(double t) {
   constexpr double kRound = 6755399441055744.0;
-  t = __builtin_fmax(t, -1010.0);
+  t = __builtin_fmax(t, -1020.0);
   const double u = t + kRound, f = t - (u - kRound);
   double y = 1.0203121063391729e-07;
   y = __builtin_fma(y, f, 1.3255224878668817e-06);

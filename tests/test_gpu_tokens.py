@@ -1133,3 +1133,22 @@ def test_fc_one_row_of_any_distance():
     with pytest.raises(ValueError):                       # not readable up to the next multiple of 16
         bd.fc_i8(torch.zeros(c_in, dtype=torch.int8, device=DEV).unsqueeze(0), dev(sx), wp, dev(sw),
                  torch.empty((1, c_out), device=DEV))
+
+
+@pytest.mark.parametrize("S", [1, 2, 32])
+def test_topk_near_the_least_probability(S):
+    """Classes that one model gives 2^-980 to 2^-1000 and the others nothing: what the others' powers are cut at does not
+    show in the logarithm."""
+    C, k = 400, 300
+    x = torch.full((S, 3, C), -math.inf)
+    x[:, :, 0] = 0.0
+    likely = torch.arange(1, C)
+    x[0, :, 1:] = -(978.0 + 24.0 * likely / C) * math.log(2)      # to 2^-1002 and, of S models, S times less
+    x[:, 1, 1:] = torch.where(x[:, 1, 1:] == -math.inf, -5000.0, x[:, 1, 1:])
+    x[:, 2] = x[:, 2].flip(-1)
+    x = x.to(DEV)
+    labels = torch.empty((3, k), dtype=torch.int32, device=DEV)
+    logp = torch.empty((3, k), device=DEV)
+    bd.combine_topk(x, labels, logp)
+    torch.cuda.synchronize()
+    check_topk(x, k, 1.0, labels, logp)

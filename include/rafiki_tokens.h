@@ -35,10 +35,12 @@ extern "C" {
 
 /* The combined distribution of row i at temperature T:
  *     p_c = 1/n_models * sum_m softmax(z_m / T)_c        (z_m = logits[m][i][:])
- * taken in 64 bits from the logits as stored.  A class below 2^-1000 counts as having no
- * probability.  Classes are ranked by p, ties by the lower index.  A row has no distribution
- * where a model's logits hold NaN or +inf, or nothing above -inf, or where T is NaN or
- * negative; T = +inf weighs all classes above -inf alike. */
+ * taken in 64 bits from the logits as stored (below 2^-960, of several models, to 2^-15 of
+ * itself).  A class below 2^-1000 counts as having no probability.  Classes are ranked by p, ties
+ * by the lower index; two whose p agree but for the rounding of 64 bits, as logits permuted
+ * between the models make them, rank as those round.  A row has no distribution where a model's
+ * logits hold NaN or +inf, or nothing above -inf, or where T is NaN or negative; T = +inf weighs
+ * all classes above -inf alike. */
 
 /* Bytes of workspace for rafiki_combine_sample and rafiki_combine_topk. */
 int rafiki_combine_workspace(int n_models, int n, int n_classes, long long* bytes);
@@ -54,7 +56,8 @@ int rafiki_combine_workspace(int n_models, int n, int n_classes, long long* byte
  *                all; above 1 counts as 1);
  *   uniform      u in [0, 1): the label is the lowest class index c for which the sum of p
  *                over the kept classes with index <= c is > u times the sum of all kept (u >= 1:
- *                the last kept class, u < 0 or NaN: as 0).  Required.
+ *                the last kept class, u < 0 or NaN: as 0).  Classes below 2^-62 count as 0 in these
+ *                sums and are not drawn.  Required.
  * out_labels int32 [n]; out_probs fp32 [n]: the label's p over the sum of all kept (1 for
  * T = 0).  A row without a distribution has label -1, and probability 0 if a mask left it
  * empty, NaN otherwise.  Sums are held in units of 2^-62; that of a row of more than 1024 classes
@@ -86,14 +89,16 @@ int rafiki_combine_topk(const void* logits, int dtype, long long ld_model, long 
  *             loss_i = T^2 [ the sum above + q_r (log q_r - log p_r) ]; q_r below 2^-20
  *             (rounding of the fp32 values), or with K all classes, counts as 0.
  * Terms with q = 0 are 0.  With Q = sum q + q_r the gradient is
- *   dz_c = T g_i (Q p_c - q_c) for c in K,  T g_i (Q p_c - q_r p_c / p_r) otherwise; q_r is 0 in both,
- *   and in Q, without rest, and where p_r = 0 (nothing above -inf outside K, where q_r > 0 gives loss +inf),
+ *   dz_c = T g_i (Q p_c - q_c) for c in K,  T g_i (Q p_c - q_r p_c / p_r) otherwise; q_r is
+ *   0 here, in Q too, without rest and where p_r = 0 (nothing above -inf outside K; the loss is then
+ *   +inf if q_r > 0),
  * where g_i = grad_loss[i] (fp32 [n], dL / d loss_i; null: 1); a row with g_i = 0 has gradient
- * 0 whatever it holds.  A class with p = 0 in K and q > 0 gives loss +inf; NaN, +inf or a row
- * of only -inf in the student, or NaN in the teacher, gives NaN.
+ * 0 whatever it holds.  A class with p = 0 in K and q > 0 gives loss +inf, as does a log p
+ * beyond fp32; NaN, +inf or a row of only -inf in the student, or NaN in the teacher, gives NaN.
  * out_loss fp32 [n] or null, grad_logits [n] rows of the logits' dtype ld_grad >= n_classes
  * elements apart, or null; not both null (the backward pass alone: out_loss null).  fp32
- * arithmetic, each gradient rounded once.  T > 0 and finite; 1 <= k <= 1024, n >= 1. */
+ * arithmetic, each gradient rounded once.  T > 0 and finite (below fp32's normal range it may count as
+ * 8.5e-39); 1 <= k <= 1024, n >= 1. */
 int rafiki_distill_loss(const void* logits, int dtype, long long ld_row, int n, int n_classes,
                         const int32_t* teacher_labels, const float* teacher_logp, int k, float temperature, int rest,
                         const float* grad_loss, float* out_loss, void* grad_logits, long long ld_grad, void* stream);
@@ -109,8 +114,8 @@ int rafiki_quantize_rows_i8(const void* x, int dtype, long long ld_x, int n, int
 /* FC layer in 8 bits: y[i][o] = act(x_scale[i] * w_scale[o] * sum_c x[i][c] w[o][c] + bias[o]), x int8 [n]
  * rows ld_x bytes apart, w int8 [c_out] rows ld_w bytes apart (the FC layout [c_out, c_in]), the scales
  * fp32 [n] and [c_out], bias fp32 [c_out] or null, act ReLU if relu != 0.  Sums are exact int32; the
- * epilogue is fp32 and y (y_dtype, rows ld_y >= c_out elements apart) is rounded once.  Rows of x
- * and w start on 16-byte boundaries (pointers and ld multiples of 16) and are readable up to the next
+ * epilogue is fp32, the two scales multiplied first, and y (y_dtype, rows ld_y >= c_out elements
+ * apart) is rounded once.  Rows of x and w start on 16-byte boundaries (pointers and ld multiples of 16) and are readable up to the next
  * multiple of 16 of c_in; what lies behind c_in is ignored.  1 <= c_in <= 131071 (128^2 c_in fits an
  * int32), 1 <= n, c_out <= 2^24; ld_x, ld_w <= 2^22. */
 int rafiki_fc_i8(const int8_t* x, long long ld_x, const float* x_scale, const int8_t* w, long long ld_w,

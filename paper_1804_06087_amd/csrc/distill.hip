@@ -14,7 +14,7 @@
 // or the memory-side cache.
 //
 // Measured on an MI355X: 4096 x 30000 bf16 127 us (3.9 TB/s of the floor's bytes; a device copy moves 4.7), 2047 x
-// 131071 bf16 292 us (3.7 TB/s): one such row fills a compute unit's registers, so its arithmetic (two powers a
+// 131071 bf16 294 us (3.6 TB/s): one such row fills a compute unit's registers, so its arithmetic (two powers a
 // class, 15 us) overlaps only with its own loads and stores and those of other units.
 #include "tokens.h"
 
@@ -97,7 +97,8 @@ __device__ __forceinline__ float reference(float top) { return top == -INFINITY 
 // NT threads hold a row of up to NT CH + 2 chunks, the two edges among them (CH = 0: any length, not held).
 // WIDE: the logits are halved as they are read, and T with them, since two finite ones may lie further apart than fp32
 // holds.  It is for T above 2^120: below, such a difference is more than 2^8 T, whose power is 0 in fp32 as that of
-// -inf is.  (Halves in the differences of every row instead: 300 us for 2047 x 131071, against 292.)
+// -inf is.  (Halves in the differences of every row instead: 300 us for 2047 x 131071, against 292 without
+// either.)
 template <bool BF16, bool REST, int NT, int CH, int OCC, bool WIDE>
 __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
   constexpr int V = BF16 ? 8 : 4, NW = NT / 64;
@@ -108,7 +109,8 @@ __global__ __launch_bounds__(NT, OCC) void distill_kernel(DistillArgs a) {
   constexpr uint32_t kMasked = BF16 ? 0xFF80FF80u : 0xFF800000u;     // -inf in every place
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   // Powers are of (z - top) s, not of z s - top s: masks of the type's lowest value overflow the products,
-  // and a row of nothing else is a uniform one.  T below log2(e) 2^-127 (no normal T is) counts as that, which keeps 0 s at 0.
+  // and a row of nothing else is a uniform one.  T below log2(e) 2^-127 (no normal T is) counts as that, which
+  // keeps 0 s at 0.
   const float s = fminf(kLog2e / (WIDE ? 0.5f * a.t : a.t), 0x1p127f);
   const int row = a.row0 + blockIdx.x;
   const float g = a.grad_loss ? a.grad_loss[row] : 1.f;

@@ -12,14 +12,15 @@
 // of 1024 classes by the sums and reads only that; top-k and the filters need only the groups of 64 whose
 // maximum reaches a bound.  The bound is the k-th largest of the groups' maxima, below which no class
 // can be among the first k (k groups hold a class above it each).  The classes above it, hardly more
-// than k, are sorted in LDS.  Rows whose kept classes do not fit there (flat distributions) are cut by
-// histograms of the bits of p, in a launch of their own that other rows leave at once.
+// than k, are sorted in LDS.  For top-p alone the bound is the 64th largest.  Rows whose kept classes do not fit
+// into the list (flat distributions), and nuclei that end below that bound, are cut by histograms of the bits of
+// p, in a launch of their own that other rows leave at once.
 //
 // Measured on an MI355X: 1 x 256 x 131072 fp32, 43 us for plain draws (stats 35 us: 3.8 TB/s), 54 us with
-// top-k 50 and top-p 0.9, 173 us with every row flat; top-64 of 2 x 1024 x 131072 bf16 260 us, of which stats 250 us
-// (2.1 TB/s: 17 64-bit instructions a class, of which the conversion takes four times an FMA's cycles, bound it,
-// at 1.9 to 2.1 GHz under this load) and the rows 48 us.  A row alone takes 10 to 20 us: fetching the
-// code that it runs through once, and some ten dependent loads.
+// top-k 50 and top-p 0.9, 173 us with every row flat; top-64 of 2 x 1024 x 131072 bf16, 40 calls in a row, 297 us: stats
+// 240 us (2.2 TB/s: 17 64-bit instructions a class, of which the conversion takes four times an FMA's cycles, bound
+// it, at 1.9 to 2.1 GHz under this load), the rows 49 us, the flat check 4.5 us.  Fewer in a row take 260 us.
+// A row alone takes 10 to 20 us: fetching the code that it runs through once, and some ten dependent loads.
 #include "tokens.h"
 
 #include <algorithm>
@@ -1028,6 +1029,10 @@ __global__ __launch_bounds__(NT) void sample_kernel(TokenArgs a) {
   const float best = r.best_score();
   r.group_scores(0, best, r.low0, r.high0);
   float score;
+  // top-p alone: how far the nucleus goes is not known, and a bound from more groups lists and sorts more classes, one from
+  // fewer leaves more rows to the flat kernel.  From 16, 64, 256 and 640 groups, in us: 3 x 16 x 30000 with nuclei up to 31
+  // classes 84, 41, 49 and 50, up to 145 81, 87, 35 and 35; 1 x 256 x 131072 up to 31 138, 57, 70 and 95, up to 125 133, 138, 71
+  // and 94, up to 412 128, 132, 142 and 94.  No more than a quarter of the groups there are.
   if (f.top_k || by_mass) score = r.bound(f.top_k ? f.top_k : min(64, max(a.units * kUnitTops / 4, 4)), best);
   else score = best + __log2f(f.min_p) - kSlack;
   for (bool whole = false; r.list(score, best); whole = true) {
@@ -1063,7 +1068,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(TokenArgs a) {
   if (threadIdx.x == 0) a.flat[row] = 1;
 }
 
-// Rows with more kept classes than a list holds: cut by histograms, then a scan of the units.  1024 threads: two
+// Rows with more kept classes than sample_kernel lists: cut by histograms, then a scan of the units.  1024 threads: two
 // passes over the logits, 64-bit powers and LDS atomics bound them (115 us a row of 131072 fp32; 512 threads took 15 us more).
 template <bool BF16, int NT>
 __global__ __launch_bounds__(NT, 4) void sample_flat_kernel(TokenArgs a) {

@@ -6,8 +6,11 @@
  * are the tokens of a vocabulary, and the same average (Section 1; Section 5.2) is asked other
  * questions: draw a token from it (rafiki_combine_sample), list the likeliest tokens with
  * their log-probabilities (rafiki_combine_topk), and train one small model to answer like the
- * ensemble, from such a list (rafiki_distill_loss).  rafiki_quantize_rows_i8 and rafiki_fc_i8
- * are the final FC layer that makes the logits, in 8-bit integers.
+ * ensemble, from such a list (rafiki_distill_loss), or from answers that were drawn and then
+ * rewarded or compared (rafiki_token_logp, rafiki_policy_loss, rafiki_preference_loss).
+ * rafiki_quantize_rows_i8 and rafiki_fc_i8 are the final FC layer that makes the logits, in 8-bit
+ * integers; rafiki_quantize_rows_mx4 and rafiki_fc_mx4 in 4-bit floating point with a scale for
+ * every 32 values.
  *
  * Conventions (those of rafiki_ensemble.h, and)
  * - All pointers are device pointers of the current device; every call only enqueues work on
@@ -103,6 +106,67 @@ int rafiki_distill_loss(const void* logits, int dtype, long long ld_row, int n, 
                         const int32_t* teacher_labels, const float* teacher_logp, int k, float temperature, int rest,
                         const float* grad_loss, float* out_loss, void* grad_logits, long long ld_grad, void* stream);
 
+/* Log-probabilities of given tokens.  Row i of the logits z has the label y = labels[i] (int32 [n]);
+ * a label outside [0, n_classes) means that the position has no token (a prompt's, padding): the
+ * row is not read, its outputs are 0 and its gradient row is 0.  With x = z / T and p = softmax(x):
+ *     out_logp[i]    = log p_y,
+ *     out_entropy[i] = H = - sum_c p_c log p_c           (a term with p = 0 is 0),
+ *     dz_c = 1/T [ a_i (1[c = y] - p_c) - h_i p_c (log p_c + H) ]
+ * with a = grad_logp = dL / d logp and h = grad_entropy = dL / dH (fp32 [n]; null: 0; grad_logits
+ * needs one of them).  A row with a_i = h_i = 0 has gradient 0 whatever it holds.  A masked label
+ * (logit -inf) has log p = -inf, as has a log p beyond fp32; NaN, +inf or a row of only -inf gives NaN
+ * in all outputs of the row.  Any output may be null, not all.  fp32 arithmetic; log p is exact to fp32 also
+ * where p is near 1; each gradient is rounded once.  2^-20 <= T <= 2^20, n >= 1. */
+int rafiki_token_logp(const void* logits, int dtype, long long ld_row, int n, int n_classes, const int32_t* labels,
+                      float temperature, const float* grad_logp, const float* grad_entropy, float* out_logp,
+                      float* out_entropy, void* grad_logits, long long ld_grad, void* stream);
+
+/* Clipped policy loss of drawn tokens with its gradient.  Rows, labels, T, log p and H as above; per
+ * row (fp32 [n]) an advantage A, the log p of the policy that drew the token (old_logp; null: the present one, held
+ * constant: r = 1) and that of a reference (ref_logp; null: no KL term).  With r = exp(log p - old),
+ * d = ref - log p:
+ *     kl     = exp(d) - d - 1,
+ *     loss_i = - min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef kl - entropy_coef H,
+ *     a_i    = d loss_i / d log p = (r A <= clip(r, ..) A ? - r A : 0) + kl_coef (1 - exp(d)),
+ * and the gradient is that of rafiki_token_logp with a_i and h_i = - entropy_coef, times g_i = grad_loss[i]
+ * (fp32 [n], dL / d loss_i; null: 1).  A = 0 gives no policy term, kl_coef = 0 no KL term and entropy_coef = 0 no
+ * entropy term, whatever they would hold; a row with g_i = 0 has gradient 0.  r or exp(d) beyond fp32 are +inf,
+ * and where a_i is not finite the gradient row is NaN, as it is where log p, H or the loss is NaN.  Rows without a
+ * token have loss, log p, kl and H 0.  out_loss, out_logp, out_kl (0 without ref_logp), out_entropy fp32 [n] and
+ * grad_logits; any may be null, not all.  0 <= clip_low <= 1, clip_high >= 0 (may be +inf); the
+ * coefficients are finite. */
+int rafiki_policy_loss(const void* logits, int dtype, long long ld_row, int n, int n_classes, const int32_t* labels,
+                       const float* advantage, const float* old_logp, const float* ref_logp, float temperature,
+                       float clip_low, float clip_high, float kl_coef, float entropy_coef, const float* grad_loss,
+                       float* out_loss, float* out_logp, float* out_kl, float* out_entropy, void* grad_logits,
+                       long long ld_grad, void* stream);
+
+/* Preference loss over n_pairs pairs of answers with its gradient.  The rows of pair p's chosen answer are
+ * offsets[2 p] .. offsets[2 p + 1] - 1, those of its rejected one offsets[2 p + 1] .. offsets[2 p + 2] - 1
+ * (int32 [2 n_pairs + 1], not decreasing, within [0, n]; null: 2 n_pairs answers of n / (2 n_pairs)
+ * rows each, which then divides).  Labels, T and log p as above; rows without a token count for nothing.  With
+ * ref_logp the reference's log p (fp32 [n]; null: 0) and the sums over an answer's tokens (mean != 0: divided by their
+ * number, an answer without tokens has score 0):
+ *     score  = beta sum (log p - ref),        u = score of the chosen - score of the rejected,
+ *     loss_p = - (1 - smoothing) log sigmoid(u) - smoothing log sigmoid(-u),
+ *     a_i    = +- beta g_p [ smoothing sigmoid(u) - (1 - smoothing) sigmoid(-u) ]   (/ number if mean),
+ * + for tokens of the chosen answer, - for the rejected one's, g_p = grad_loss[p] (fp32 [n_pairs]; null:
+ * 1); the gradient is that of rafiki_token_logp.  out_loss fp32 [n_pairs], out_scores fp32 [n_pairs][2], grad_logits;
+ * any may be null, not all.  A pair with g_p = 0 has gradient 0.  A score that is NaN (a row of its tokens that has no
+ * distribution, or infinite scores of both answers) makes the loss and the gradient rows of both answers'
+ * tokens NaN.  Rows before offsets[0] and from offsets[2 n_pairs] on are not read and their gradient rows are left as
+ * they were.  Offsets that decrease or leave [0, n] give wrong values but no access out of the
+ * arrays.  log p, scores and the loss are summed in 64 bits.  beta > 0 and finite, 0 <= smoothing <= 0.5,
+ * 1 <= n_pairs <= 2^24. */
+int rafiki_preference_loss(const void* logits, int dtype, long long ld_row, int n, int n_classes,
+                           const int32_t* labels, const int32_t* offsets, int n_pairs, const float* ref_logp,
+                           float temperature, float beta, float smoothing, int mean, const float* grad_loss,
+                           float* out_loss, float* out_scores, void* grad_logits, long long ld_grad, void* workspace,
+                           long long workspace_bytes, void* stream);
+
+/* Bytes of workspace for rafiki_preference_loss. */
+int rafiki_preference_workspace(int n, int n_pairs, long long* bytes);
+
 /* Rows of x [n][c] (dtype, ld_x elements apart, any alignment) in 8 bits: scale[i] =
  * max |x_i| / 127 in fp32 (0 for a row of zeros), q = x / scale rounded to the nearest integer,
  * ties to even, exactly, into int8 rows ld_q bytes apart (ld_q >= c).  A row with a NaN or an
@@ -124,6 +188,32 @@ int rafiki_fc_i8(const int8_t* x, long long ld_x, const float* x_scale, const in
 
 /* Bytes of workspace for rafiki_fc_i8. */
 int rafiki_fc_i8_workspace(int n, int c_in, int c_out, long long* bytes);
+
+/* Rows of x [n][c] (dtype, ld_x elements apart, any alignment) in 4 bits: blocks of 32 neighbouring
+ * values, each with a scale 2^(b - 127) of one byte b and 32 codes of 4 bits: a sign (8) and one of the
+ * magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6 (0 .. 7), i.e. E2M1 values with an E8M0 scale.  With e =
+ * floor(log2 max |x|) - 2 of the block, b = e + 127 (at least 0; 0 for a block of zeros), and the codes are x / 2^(b - 127)
+ * rounded to the nearest magnitude, ties to the even code, above 6 to 6 (so a largest value whose
+ * significand exceeds 1.5 is cut to 1.5).  A block with a NaN or an infinity has b = 255 (NaN) and codes 0.
+ * A row has ceil(c / 32) blocks, its last one filled up with code 0: q rows of 16 bytes a block, two codes a byte, the
+ * even one in the low half, ld_q >= 16 ceil(c / 32) bytes apart; scale rows of a byte a block, ld_scale >=
+ * ceil(c / 32) bytes apart (rafiki_fc_mx4 wants both on 16-byte boundaries).  n >= 1, 1 <= c <= 2^30. */
+int rafiki_quantize_rows_mx4(const void* x, int dtype, long long ld_x, int n, int c, uint8_t* q, long long ld_q,
+                             uint8_t* scale, long long ld_scale, void* stream);
+
+/* FC layer in 4 bits: y[i][o] = act(sum_c x[i][c] w[o][c] + bias[o]) over the values that the codes and scales of
+ * x [n] and w [c_out] stand for (layout as above, c_in a multiple of 32: whole blocks), bias fp32 [c_out] or
+ * null, act ReLU if relu != 0 (NaN stays NaN).  Products are exact, sums fp32, and y (y_dtype, rows ld_y >= c_out
+ * elements apart) is rounded once.  Rows of codes and of scales start on 16-byte boundaries (pointers and
+ * distances multiples of 16; the distance of a single row does not matter); rows of scales are readable up to the next multiple of 16, what
+ * lies behind c_in / 32 is ignored.  32 <= c_in <= 2^20, 1 <= n, c_out <= 2^24, distances <= 2^22. */
+int rafiki_fc_mx4(const uint8_t* x, long long ld_x, const uint8_t* x_scale, long long ld_x_scale, const uint8_t* w,
+                  long long ld_w, const uint8_t* w_scale, long long ld_w_scale, const float* bias, int n, int c_in,
+                  int c_out, int relu, void* y, int y_dtype, long long ld_y, void* workspace, long long workspace_bytes,
+                  void* stream);
+
+/* Bytes of workspace for rafiki_fc_mx4. */
+int rafiki_fc_mx4_workspace(int n, int c_in, int c_out, long long* bytes);
 
 #ifdef __cplusplus
 }

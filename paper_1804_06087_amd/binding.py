@@ -40,6 +40,8 @@ EXPORTED = ("rafiki_ensemble_create", "rafiki_ensemble_infer", "rafiki_ensemble_
             "rafiki_rl_forward", "rafiki_rl_gradient", "rafiki_rl_adam_step", "rafiki_rl_run_episode",
             "rafiki_rl_train", "rafiki_combine_workspace", "rafiki_combine_sample", "rafiki_combine_topk",
             "rafiki_distill_loss", "rafiki_quantize_rows_i8", "rafiki_fc_i8", "rafiki_fc_i8_workspace",
+            "rafiki_token_logp", "rafiki_policy_loss", "rafiki_preference_loss", "rafiki_preference_workspace",
+            "rafiki_quantize_rows_mx4", "rafiki_fc_mx4", "rafiki_fc_mx4_workspace",
             "rafiki_last_error")
 KERNEL_CLASSES = ("conv_mfma", "splitk_reduce", "conv_f32", "stage", "pool", "embed", "concat", "combine", "vote",
                   "fused_net", "tap_table")
@@ -180,6 +182,13 @@ def load_library(path: str = LIB_PATH):
     lib.rafiki_quantize_rows_i8.argtypes = [V, I, L, I, I, V, L, V, V]
     lib.rafiki_fc_i8.argtypes = [V, L, V, V, L, V, V, I, I, I, I, V, I, L, V, L, V]
     lib.rafiki_fc_i8_workspace.argtypes = [I, I, I, P(L)]
+    lib.rafiki_token_logp.argtypes = [V, I, L, I, I, V, F, V, V, V, V, V, L, V]
+    lib.rafiki_policy_loss.argtypes = [V, I, L, I, I, V, V, V, V, F, F, F, F, F, V, V, V, V, V, V, L, V]
+    lib.rafiki_preference_loss.argtypes = [V, I, L, I, I, V, V, I, V, F, F, F, I, V, V, V, V, L, V, L, V]
+    lib.rafiki_preference_workspace.argtypes = [I, I, P(L)]
+    lib.rafiki_quantize_rows_mx4.argtypes = [V, I, L, I, I, V, L, V, L, V]
+    lib.rafiki_fc_mx4.argtypes = [V, L, V, L, V, L, V, L, V, I, I, I, I, V, I, L, V, L, V]
+    lib.rafiki_fc_mx4_workspace.argtypes = [I, I, I, P(L)]
     lib.rafiki_last_error.restype = C.c_char_p
     for name in EXPORTED[:-1]:
         getattr(lib, name).restype = C.c_int
@@ -635,6 +644,95 @@ def distill_loss(logits, teacher_labels, teacher_logp, out_loss=None, grad_logit
           _ptr(grad_logits), ld_grad)
 
 
+def _grad_rows(grad_logits, logits):
+    """Distance between the rows of a gradient of the logits (0 for None)."""
+    if grad_logits is None:
+        return 0
+    if grad_logits.shape != logits.shape or grad_logits.dtype != logits.dtype:
+        raise ValueError("grad_logits: expected the shape and dtype of the logits")
+    _same_device(logits, grad_logits)
+    return _rows(grad_logits, "grad_logits")
+
+
+def token_logp(logits, labels, out_logp=None, out_entropy=None, grad_logits=None, grad_logp=None, grad_entropy=None,
+               temperature: float = 1.0, stream=None):
+    """log p fp32 [n] of the tokens labels int32 [n] (outside [0, C): no token, 0) under softmax(logits / temperature),
+    logits [n, C] fp32 or bf16, and its entropy; in grad_logits the gradient of a loss whose derivatives by the two
+    are grad_logp and grad_entropy fp32 [n] (None: 0).  Any output may be None."""
+    import torch
+    code = _dtype_code(logits, "logits")
+    ld_row, ld_grad = _rows(logits, "logits"), _grad_rows(grad_logits, logits)
+    n, nc = logits.shape
+    f32, dev = torch.float32, logits.device
+    if labels is None:
+        raise ValueError("labels are required")
+    _call(logits, stream, None, None, load_library().rafiki_token_logp, logits.data_ptr(), code, ld_row, n, nc,
+          _vector(labels, n, torch.int32, dev, "labels"), temperature, _vector(grad_logp, n, f32, dev, "grad_logp"),
+          _vector(grad_entropy, n, f32, dev, "grad_entropy"), _vector(out_logp, n, f32, dev, "log-probabilities"),
+          _vector(out_entropy, n, f32, dev, "entropies"), _ptr(grad_logits), ld_grad)
+
+
+def policy_loss(logits, labels, advantage, out_loss=None, grad_logits=None, old_logp=None, ref_logp=None,
+                grad_loss=None, out_logp=None, out_kl=None, out_entropy=None, temperature: float = 1.0,
+                clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0, entropy_coef: float = 0.0,
+                stream=None):
+    """Clipped policy loss fp32 [n] of the tokens labels int32 [n] under the logits [n, C] (fp32 or bf16), with
+    advantage, the log p of the policy that drew them (old_logp; None: the present one) and of a reference (ref_logp;
+    None: no KL term) fp32 [n]; in grad_logits its gradient times grad_loss [n] (None: 1).  Any output may be None."""
+    import torch
+    code = _dtype_code(logits, "logits")
+    ld_row, ld_grad = _rows(logits, "logits"), _grad_rows(grad_logits, logits)
+    n, nc = logits.shape
+    if labels is None or advantage is None:
+        raise ValueError("labels and advantage are required")
+    vec = lambda t, name: _vector(t, n, torch.float32, logits.device, name)  # noqa: E731
+    _call(logits, stream, None, None, load_library().rafiki_policy_loss, logits.data_ptr(), code, ld_row, n, nc,
+          _vector(labels, n, torch.int32, logits.device, "labels"), vec(advantage, "advantage"), vec(old_logp, "old_logp"),
+          vec(ref_logp, "ref_logp"), temperature, clip_low, clip_high, kl_coef, entropy_coef, vec(grad_loss, "grad_loss"),
+          vec(out_loss, "loss"), vec(out_logp, "log-probabilities"), vec(out_kl, "kl"), vec(out_entropy, "entropies"),
+          _ptr(grad_logits), ld_grad)
+
+
+@functools.lru_cache(maxsize=4096)
+def preference_workspace(n: int, n_pairs: int) -> int:
+    """Bytes of workspace of preference_loss."""
+    b = C.c_longlong()
+    _check(load_library().rafiki_preference_workspace(n, n_pairs, C.byref(b)))
+    return b.value
+
+
+def preference_loss(logits, labels, out_loss=None, grad_logits=None, offsets=None, n_pairs=None, ref_logp=None,
+                    grad_loss=None, out_scores=None, temperature: float = 1.0, beta: float = 0.1,
+                    smoothing: float = 0.0, mean: bool = False, workspace=None, stream=None):
+    """Preference loss fp32 [pairs] over pairs of answers, whose tokens labels int32 [n] stand under the logits [n, C]
+    (fp32 or bf16): answer s (chosen of pair 0, rejected of pair 0, chosen of pair 1, ...) has the rows offsets[s] ..
+    offsets[s + 1] - 1 (int32 [2 pairs + 1]; None: 2 n_pairs answers of equal length).  ref_logp fp32 [n] as token_logp
+    gives it for the reference (None: 0); mean: scores per token; in grad_logits the gradient times grad_loss [pairs]
+    (None: 1); out_scores fp32 [pairs, 2].  Any output may be None."""
+    import torch
+    code = _dtype_code(logits, "logits")
+    ld_row, ld_grad = _rows(logits, "logits"), _grad_rows(grad_logits, logits)
+    n, nc = logits.shape
+    f32, dev = torch.float32, logits.device
+    if labels is None:
+        raise ValueError("labels are required")
+    if offsets is not None:
+        pairs = (offsets.shape[0] - 1) // 2 if offsets.dim() == 1 else 0
+        if pairs < 1 or offsets.shape[0] != 2 * pairs + 1 or n_pairs not in (None, pairs):
+            raise ValueError("offsets: expected int32 [2 pairs + 1]")
+        n_pairs = pairs
+    elif n_pairs is None:
+        raise ValueError("offsets or n_pairs is required")
+    if out_scores is not None:
+        _expect(out_scores, (n_pairs, 2), f32, "scores")
+        _same_device(logits, out_scores)
+    _call(logits, stream, preference_workspace(n, n_pairs), workspace, load_library().rafiki_preference_loss,
+          logits.data_ptr(), code, ld_row, n, nc, _vector(labels, n, torch.int32, dev, "labels"),
+          _vector(offsets, 2 * n_pairs + 1, torch.int32, dev, "offsets"), n_pairs, _vector(ref_logp, n, f32, dev, "ref_logp"),
+          temperature, beta, smoothing, 1 if mean else 0, _vector(grad_loss, n_pairs, f32, dev, "grad_loss"),
+          _vector(out_loss, n_pairs, f32, dev, "loss"), _ptr(out_scores), _ptr(grad_logits), ld_grad)
+
+
 def quantize_rows_i8(x, q, scale, stream=None):
     """Rows of x [n, c] (fp32 or bf16) in 8 bits: q int8 [n, c] and scale fp32 [n] = max |x| / 127."""
     import torch
@@ -682,6 +780,69 @@ def fc_i8(x, x_scale, w, w_scale, y, bias=None, relu: bool = False, workspace=No
           _vector(x_scale, n, f32, y.device, "x_scale"), w.data_ptr(), ld_w,
           _vector(w_scale, c_out, f32, y.device, "w_scale"), _vector(bias, c_out, f32, y.device, "bias"), n, c_in, c_out,
           1 if relu else 0, y.data_ptr(), code, ld_y)
+
+
+def mx4_empty(n: int, c: int, device="cuda"):
+    """Uninitialised codes uint8 [n, 16 b] and scales uint8 [n, b] of n rows of c values in 4 bits, b = ceil(c / 32),
+    with the row distances that fc_mx4 asks for."""
+    import torch
+    blocks = (c + 31) // 32
+    scale = torch.empty((n, (blocks + 15) // 16 * 16), dtype=torch.uint8, device=device)
+    return torch.empty((n, 16 * blocks), dtype=torch.uint8, device=device), scale[:, :blocks]
+
+
+def _mx4_blocks(q, scale, name):
+    """Blocks a row of codes uint8 [n, 16 b] and scales uint8 [n, b]."""
+    import torch
+    if not (q.is_cuda and scale.is_cuda and q.dtype == scale.dtype == torch.uint8 and q.dim() == scale.dim() == 2 and
+            q.shape[0] == scale.shape[0] and q.shape[1] == 16 * scale.shape[1]):
+        raise ValueError(f"{name}: expected device tensors of uint8, codes [n, 16 b] and scales [n, b], got "
+                         f"{tuple(q.shape)} {q.dtype} and {tuple(scale.shape)} {scale.dtype}")
+    return scale.shape[1]
+
+
+def quantize_rows_mx4(x, q, scale, stream=None):
+    """Rows of x [n, c] (fp32 or bf16) in 4-bit floating point: codes q uint8 [n, 16 b] and scales uint8 [n, b], one for
+    each of the b = ceil(c / 32) blocks of 32 values (mx4_empty makes both)."""
+    code = _dtype_code(x, "x")
+    ld_x, ld_q, ld_s = _rows(x, "x"), _rows(q, "q"), _rows(scale, "scale")
+    n, c = x.shape
+    if _mx4_blocks(q, scale, "q") != (c + 31) // 32 or q.shape[0] != n:
+        raise ValueError(f"q: expected codes [{n}, {(c + 31) // 32 * 16}], got {tuple(q.shape)}")
+    _same_device(x, q, scale)
+    _call(x, stream, None, None, load_library().rafiki_quantize_rows_mx4, x.data_ptr(), code, ld_x, n, c, q.data_ptr(), ld_q,
+          scale.data_ptr(), ld_s)
+
+
+@functools.lru_cache(maxsize=4096)
+def fc_mx4_workspace(n: int, c_in: int, c_out: int) -> int:
+    """Bytes of workspace of fc_mx4."""
+    b = C.c_longlong()
+    _check(load_library().rafiki_fc_mx4_workspace(n, c_in, c_out, C.byref(b)))
+    return b.value
+
+
+def fc_mx4(x, x_scale, w, w_scale, y, bias=None, relu: bool = False, workspace=None, stream=None):
+    """FC layer in 4 bits: y [n, c_out] (fp32 or bf16) = act(x w^T + bias) over the values of codes x [n, 16 b], w
+    [c_out, 16 b] and scales x_scale [n, b], w_scale [c_out, b] (quantize_rows_mx4), whose rows start on 16-byte
+    boundaries, scales readable up to the next one (mx4_empty)."""
+    import torch
+    code = _dtype_code(y, "y")
+    blocks = _mx4_blocks(x, x_scale, "x")
+    n, c_out = x.shape[0], w.shape[0]
+    if _mx4_blocks(w, w_scale, "w") != blocks or y.shape != (n, c_out):
+        raise ValueError("expected codes x [n, 16 b] and w [c_out, 16 b] and y [n, c_out]")
+    strides = []
+    b16 = (blocks + 15) // 16 * 16                           # rows of scales are read up to there
+    for t, least, name in ((x, 16 * blocks, "x"), (x_scale, b16, "x_scale"), (w, 16 * blocks, "w"), (w_scale, b16, "w_scale")):
+        ld = _rows(t, name) if t.shape[0] > 1 else least     # one row has no distance to the next
+        if t.storage_offset() + (t.shape[0] - 1) * ld + least > t.untyped_storage().nbytes():
+            raise ValueError(f"{name}: the last row is not readable up to the next multiple of 16")
+        strides += [t.data_ptr(), ld]
+    _same_device(y, x, x_scale, w, w_scale)
+    _call(y, stream, fc_mx4_workspace(n, 32 * blocks, c_out), workspace, load_library().rafiki_fc_mx4, *strides,
+          _vector(bias, c_out, torch.float32, y.device, "bias"), n, 32 * blocks, c_out, 1 if relu else 0, y.data_ptr(), code,
+          _rows(y, "y"))
 
 
 def tile_configs():

@@ -69,6 +69,66 @@ struct FcI8Args {
   int* partial;               // [splits][n][c_out] int32 sums (splits > 1)
 };
 
+struct TokenLossArgs {
+  const void* logits;
+  long long ld_row;
+  int n, C, row0;             // row0: the launch's first row
+  const int32_t* labels;
+  double inv_t;               // 1 / T
+  float s;                    // log2(e) / T
+  bool policy;
+  const float* grad_logp;     // token_logp
+  const float* grad_entropy;
+  const float* advantage;     // policy_loss
+  const float* old_logp;
+  const float* ref_logp;
+  const float* grad_loss;
+  float clip_low, clip_high;
+  float kl_coef, entropy_coef;
+  float* loss;
+  float* logp;
+  float* kl;
+  float* entropy;
+  void* grad;
+  long long ld_grad;
+};
+
+struct PreferenceRow {        // of the workspace
+  double delta;               // log p - ref
+  float top, share, rest;     // the other classes' maximum, p there, 1 - p of the label
+  float weight;               // dL / d log p over T
+};
+struct PreferenceArgs {
+  const void* logits;
+  long long ld_row;
+  int n, C, row0, pairs;
+  const int32_t* labels;
+  const int32_t* offsets;
+  const float* ref_logp;
+  double inv_t;
+  float s, beta, smoothing;
+  int mean;
+  const float* grad_loss;
+  float* loss;
+  float* scores;
+  void* grad;
+  long long ld_grad;
+  PreferenceRow* rows;        // [n]
+};
+
+struct FcMx4Args {
+  const uint8_t* x;
+  const uint8_t* xs;
+  const uint8_t* w;
+  const uint8_t* ws;
+  long long ld_x, ld_xs, ld_w, ld_ws, ld_y;
+  const float* bias;
+  int n, blocks, c_out, relu, out_bf16;
+  int kt_per_split;           // K tiles per split
+  void* y;
+  float* partial;             // [splits][n][c_out] sums (splits > 1)
+};
+
 hipError_t launch_sample(const TokenArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_topk(const TokenArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t s);
@@ -76,5 +136,11 @@ hipError_t launch_quantize(const void* x, bool bf16, long long ld_x, int n, int 
                            float* scale, hipStream_t s);
 hipError_t launch_fc_i8(const FcI8Args& a, hipStream_t s);
 long long fc_i8_workspace_bytes(int n, int c_in, int c_out);
+hipError_t launch_token_loss(const TokenLossArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_preference(const PreferenceArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_quantize_mx4(const void* x, bool bf16, long long ld_x, int n, int c, uint8_t* q, long long ld_q,
+                               uint8_t* scale, long long ld_scale, hipStream_t s);
+hipError_t launch_fc_mx4(const FcMx4Args& a, hipStream_t s);
+long long fc_mx4_workspace_bytes(int n, int blocks, int c_out);
 
 }  // namespace rafiki

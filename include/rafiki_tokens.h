@@ -116,10 +116,15 @@ int rafiki_distill_loss(const void* logits, int dtype, long long ld_row, int n, 
  * needs one of them).  A row with a_i = h_i = 0 has gradient 0 whatever it holds.  A masked label
  * (logit -inf) has log p = -inf, as has a log p beyond fp32; NaN, +inf or a row of only -inf gives NaN
  * in all outputs of the row.  Any output may be null, not all.  fp32 arithmetic; log p is exact to fp32 also
- * where p is near 1; each gradient is rounded once.  2^-20 <= T <= 2^20, n >= 1. */
+ * where p is near 1; each gradient is rounded once.  Scalars are 64 bits here, since what follows subtracts and sums
+ * log-probabilities.  2^-20 <= T <= 2^20, n >= 1. */
 int rafiki_token_logp(const void* logits, int dtype, long long ld_row, int n, int n_classes, const int32_t* labels,
-                      float temperature, const float* grad_logp, const float* grad_entropy, float* out_logp,
-                      float* out_entropy, void* grad_logits, long long ld_grad, void* stream);
+                      double temperature, const float* grad_logp, const float* grad_entropy, float* out_logp,
+                      float* out_entropy, void* grad_logits, long long ld_grad, void* workspace,
+                      long long workspace_bytes, void* stream);
+
+/* Bytes of workspace for rafiki_token_logp and rafiki_policy_loss (0 unless few rows are long). */
+int rafiki_token_workspace(int n, int n_classes, long long* bytes);
 
 /* Clipped policy loss of drawn tokens with its gradient.  Rows, labels, T, log p and H as above; per
  * row (fp32 [n]) an advantage A, the log p of the policy that drew the token (old_logp; null: the present one, held
@@ -136,10 +141,10 @@ int rafiki_token_logp(const void* logits, int dtype, long long ld_row, int n, in
  * grad_logits; any may be null, not all.  0 <= clip_low <= 1, clip_high >= 0 (may be +inf); the
  * coefficients are finite. */
 int rafiki_policy_loss(const void* logits, int dtype, long long ld_row, int n, int n_classes, const int32_t* labels,
-                       const float* advantage, const float* old_logp, const float* ref_logp, float temperature,
-                       float clip_low, float clip_high, float kl_coef, float entropy_coef, const float* grad_loss,
+                       const float* advantage, const float* old_logp, const float* ref_logp, double temperature,
+                       double clip_low, double clip_high, double kl_coef, double entropy_coef, const float* grad_loss,
                        float* out_loss, float* out_logp, float* out_kl, float* out_entropy, void* grad_logits,
-                       long long ld_grad, void* stream);
+                       long long ld_grad, void* workspace, long long workspace_bytes, void* stream);
 
 /* Preference loss over n_pairs pairs of answers with its gradient.  The rows of pair p's chosen answer are
  * offsets[2 p] .. offsets[2 p + 1] - 1, those of its rejected one offsets[2 p + 1] .. offsets[2 p + 2] - 1
@@ -160,12 +165,12 @@ int rafiki_policy_loss(const void* logits, int dtype, long long ld_row, int n, i
  * 1 <= n_pairs <= 2^24. */
 int rafiki_preference_loss(const void* logits, int dtype, long long ld_row, int n, int n_classes,
                            const int32_t* labels, const int32_t* offsets, int n_pairs, const float* ref_logp,
-                           float temperature, float beta, float smoothing, int mean, const float* grad_loss,
+                           double temperature, double beta, double smoothing, int mean, const float* grad_loss,
                            float* out_loss, float* out_scores, void* grad_logits, long long ld_grad, void* workspace,
                            long long workspace_bytes, void* stream);
 
 /* Bytes of workspace for rafiki_preference_loss. */
-int rafiki_preference_workspace(int n, int n_pairs, long long* bytes);
+int rafiki_preference_workspace(int n, int n_classes, long long* bytes);
 
 /* Rows of x [n][c] (dtype, ld_x elements apart, any alignment) in 8 bits: scale[i] =
  * max |x_i| / 127 in fp32 (0 for a row of zeros), q = x / scale rounded to the nearest integer,

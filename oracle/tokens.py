@@ -181,7 +181,7 @@ def policy(z, y, A, old=None, ref=None, t=1.0, low=0.2, high=0.2, kl_coef=0.0, e
         if A != 0:
             r = fp32(np.exp(np.float64(logp) - old)) if old is not None else 1.0
             plain = r * np.float64(A)
-            cut = np.clip(r, 1 - np.float64(np.float32(low)), 1 + np.float64(np.float32(high))) * np.float64(A)
+            cut = np.clip(r, 1 - low, 1 + high) * np.float64(A)
             loss = math.nan if np.isnan(plain) else -min(plain, cut)
             slope = math.nan if np.isnan(plain) else (-plain if plain <= cut else 0.0)
         if ref is not None:

@@ -41,6 +41,7 @@ EXPORTED = ("rafiki_ensemble_create", "rafiki_ensemble_infer", "rafiki_ensemble_
             "rafiki_rl_train", "rafiki_combine_workspace", "rafiki_combine_sample", "rafiki_combine_topk",
             "rafiki_distill_loss", "rafiki_quantize_rows_i8", "rafiki_fc_i8", "rafiki_fc_i8_workspace",
             "rafiki_token_logp", "rafiki_policy_loss", "rafiki_preference_loss", "rafiki_preference_workspace",
+            "rafiki_token_workspace",
             "rafiki_quantize_rows_mx4", "rafiki_fc_mx4", "rafiki_fc_mx4_workspace",
             "rafiki_last_error")
 KERNEL_CLASSES = ("conv_mfma", "splitk_reduce", "conv_f32", "stage", "pool", "embed", "concat", "combine", "vote",
@@ -182,10 +183,10 @@ def load_library(path: str = LIB_PATH):
     lib.rafiki_quantize_rows_i8.argtypes = [V, I, L, I, I, V, L, V, V]
     lib.rafiki_fc_i8.argtypes = [V, L, V, V, L, V, V, I, I, I, I, V, I, L, V, L, V]
     lib.rafiki_fc_i8_workspace.argtypes = [I, I, I, P(L)]
-    lib.rafiki_token_logp.argtypes = [V, I, L, I, I, V, F, V, V, V, V, V, L, V]
-    lib.rafiki_policy_loss.argtypes = [V, I, L, I, I, V, V, V, V, F, F, F, F, F, V, V, V, V, V, V, L, V]
-    lib.rafiki_preference_loss.argtypes = [V, I, L, I, I, V, V, I, V, F, F, F, I, V, V, V, V, L, V, L, V]
-    lib.rafiki_preference_workspace.argtypes = [I, I, P(L)]
+    lib.rafiki_token_workspace.argtypes = lib.rafiki_preference_workspace.argtypes = [I, I, P(L)]
+    lib.rafiki_token_logp.argtypes = [V, I, L, I, I, V, C.c_double, V, V, V, V, V, L, V, L, V]
+    lib.rafiki_policy_loss.argtypes = [V, I, L, I, I, V, V, V, V] + [C.c_double] * 5 + [V] * 6 + [L, V, L, V]
+    lib.rafiki_preference_loss.argtypes = [V, I, L, I, I, V, V, I, V] + [C.c_double] * 3 + [I, V, V, V, V, L, V, L, V]
     lib.rafiki_quantize_rows_mx4.argtypes = [V, I, L, I, I, V, L, V, L, V]
     lib.rafiki_fc_mx4.argtypes = [V, L, V, L, V, L, V, L, V, I, I, I, I, V, I, L, V, L, V]
     lib.rafiki_fc_mx4_workspace.argtypes = [I, I, I, P(L)]
@@ -654,8 +655,16 @@ def _grad_rows(grad_logits, logits):
     return _rows(grad_logits, "grad_logits")
 
 
+@functools.lru_cache(maxsize=4096)
+def token_workspace(n: int, n_classes: int) -> int:
+    """Bytes of workspace of token_logp and policy_loss."""
+    b = C.c_longlong()
+    _check(load_library().rafiki_token_workspace(n, n_classes, C.byref(b)))
+    return b.value
+
+
 def token_logp(logits, labels, out_logp=None, out_entropy=None, grad_logits=None, grad_logp=None, grad_entropy=None,
-               temperature: float = 1.0, stream=None):
+               temperature: float = 1.0, workspace=None, stream=None):
     """log p fp32 [n] of the tokens labels int32 [n] (outside [0, C): no token, 0) under softmax(logits / temperature),
     logits [n, C] fp32 or bf16, and its entropy; in grad_logits the gradient of a loss whose derivatives by the two
     are grad_logp and grad_entropy fp32 [n] (None: 0).  Any output may be None."""
@@ -666,7 +675,7 @@ def token_logp(logits, labels, out_logp=None, out_entropy=None, grad_logits=None
     f32, dev = torch.float32, logits.device
     if labels is None:
         raise ValueError("labels are required")
-    _call(logits, stream, None, None, load_library().rafiki_token_logp, logits.data_ptr(), code, ld_row, n, nc,
+    _call(logits, stream, token_workspace(n, nc), workspace, load_library().rafiki_token_logp, logits.data_ptr(), code, ld_row, n, nc,
           _vector(labels, n, torch.int32, dev, "labels"), temperature, _vector(grad_logp, n, f32, dev, "grad_logp"),
           _vector(grad_entropy, n, f32, dev, "grad_entropy"), _vector(out_logp, n, f32, dev, "log-probabilities"),
           _vector(out_entropy, n, f32, dev, "entropies"), _ptr(grad_logits), ld_grad)
@@ -675,7 +684,7 @@ def token_logp(logits, labels, out_logp=None, out_entropy=None, grad_logits=None
 def policy_loss(logits, labels, advantage, out_loss=None, grad_logits=None, old_logp=None, ref_logp=None,
                 grad_loss=None, out_logp=None, out_kl=None, out_entropy=None, temperature: float = 1.0,
                 clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0, entropy_coef: float = 0.0,
-                stream=None):
+                workspace=None, stream=None):
     """Clipped policy loss fp32 [n] of the tokens labels int32 [n] under the logits [n, C] (fp32 or bf16), with
     advantage, the log p of the policy that drew them (old_logp; None: the present one) and of a reference (ref_logp;
     None: no KL term) fp32 [n]; in grad_logits its gradient times grad_loss [n] (None: 1).  Any output may be None."""
@@ -686,7 +695,7 @@ def policy_loss(logits, labels, advantage, out_loss=None, grad_logits=None, old_
     if labels is None or advantage is None:
         raise ValueError("labels and advantage are required")
     vec = lambda t, name: _vector(t, n, torch.float32, logits.device, name)  # noqa: E731
-    _call(logits, stream, None, None, load_library().rafiki_policy_loss, logits.data_ptr(), code, ld_row, n, nc,
+    _call(logits, stream, token_workspace(n, nc), workspace, load_library().rafiki_policy_loss, logits.data_ptr(), code, ld_row, n, nc,
           _vector(labels, n, torch.int32, logits.device, "labels"), vec(advantage, "advantage"), vec(old_logp, "old_logp"),
           vec(ref_logp, "ref_logp"), temperature, clip_low, clip_high, kl_coef, entropy_coef, vec(grad_loss, "grad_loss"),
           vec(out_loss, "loss"), vec(out_logp, "log-probabilities"), vec(out_kl, "kl"), vec(out_entropy, "entropies"),
@@ -694,10 +703,10 @@ def policy_loss(logits, labels, advantage, out_loss=None, grad_logits=None, old_
 
 
 @functools.lru_cache(maxsize=4096)
-def preference_workspace(n: int, n_pairs: int) -> int:
+def preference_workspace(n: int, n_classes: int) -> int:
     """Bytes of workspace of preference_loss."""
     b = C.c_longlong()
-    _check(load_library().rafiki_preference_workspace(n, n_pairs, C.byref(b)))
+    _check(load_library().rafiki_preference_workspace(n, n_classes, C.byref(b)))
     return b.value
 
 
@@ -726,7 +735,7 @@ def preference_loss(logits, labels, out_loss=None, grad_logits=None, offsets=Non
     if out_scores is not None:
         _expect(out_scores, (n_pairs, 2), f32, "scores")
         _same_device(logits, out_scores)
-    _call(logits, stream, preference_workspace(n, n_pairs), workspace, load_library().rafiki_preference_loss,
+    _call(logits, stream, preference_workspace(n, nc), workspace, load_library().rafiki_preference_loss,
           logits.data_ptr(), code, ld_row, n, nc, _vector(labels, n, torch.int32, dev, "labels"),
           _vector(offsets, 2 * n_pairs + 1, torch.int32, dev, "offsets"), n_pairs, _vector(ref_logp, n, f32, dev, "ref_logp"),
           temperature, beta, smoothing, 1 if mean else 0, _vector(grad_loss, n_pairs, f32, dev, "grad_loss"),

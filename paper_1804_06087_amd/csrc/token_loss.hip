@@ -69,6 +69,7 @@ __device__ __forceinline__ T wave_add(T v) {
   return v;
 }
 
+
 // The maximum as a reference for powers: an empty row has none and takes 0.
 __device__ __forceinline__ float reference(float top) { return top == -INFINITY ? 0.f : top; }
 // Exponents of 2 as factors of a power that is 0 below here: -inf would make it NaN.
@@ -140,23 +141,51 @@ struct Row {
         if (c0 + j < C) put<BF16>(row, c0 + j, d[j]);
     }
   }
-  template <int NT>
-  __device__ __forceinline__ void zero(char* row) const {
-    for (int i = threadIdx.x; i < chunks; i += NT) {
-      float d[V];
+  __device__ __forceinline__ void zero_chunk(char* row, int i) const {
+    float d[V];
 #pragma unroll
-      for (int j = 0; j < V; ++j) d[j] = 0.f;
-      store(row, i, d, 0.f);
-    }
+    for (int j = 0; j < V; ++j) d[j] = 0.f;
+    store(row, i, d, 0.f);
+  }
+  template <int NT>
+  __device__ __forceinline__ void zero(char* row, int tid) const {
+    for (int i = tid; i < chunks; i += NT) zero_chunk(row, i);
   }
 };
 
-// Sums over classes: 2^(y - top), and of those times (y - top).
+// Sums over classes, the label's apart: 2^x with x = (z - top) s, and of those times x.
 struct Sums {
   float top, sum, moment;
 };
+// x = d s of a difference d of logits, and the power; PRECISE: s in two parts, and what is rounded off x into `lost`, whose
+// sum times ln 2 belongs to the sum of powers.
+template <bool PRECISE>
+__device__ __forceinline__ float term(float d, const Scale& s, float& x, float& lost) {
+  x = d * s.hi;
+  const float e = power2(x);
+  if constexpr (PRECISE) lost = fmaf(e, fminf(fmaf(d, s.lo, fmaf(d, s.hi, -x)), 1.f), lost);   // NaN where d = -inf and e = 0: 1
+  return e;
+}
+// Relative to the label's logit, which needs no maximum: sums stay below 2^127 as long as p_l is above 2^-127, and what underflows
+// beside the label's own 1 does not count.  Where that does not hold, the sum is not finite and the caller takes
+// add_chunk_any.
+template <int V, bool ENT, bool PRECISE>
+__device__ __forceinline__ void add_chunk(Sums& a, float& lost, const float z[V], float ref, const Scale& s) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    float x;
+    const float e = term<PRECISE>(z[j] - ref, s, x, lost);
+    a.sum += e;
+    if constexpr (ENT) a.moment = fmaf(e, finite_log2(x), a.moment);
+  }
+}
+template <bool ENT>
+__device__ __forceinline__ bool bounded(const Sums& a) {
+  return a.sum < INFINITY && (!ENT || fabsf(a.moment) < INFINITY);
+}
+// For any values: relative to the largest so far.
 template <int V, bool ENT>
-__device__ __forceinline__ void add_chunk(Sums& a, const float z[V], float s) {
+__device__ __forceinline__ void add_chunk_any(Sums& a, const float z[V], float s) {
   float now = a.top;
 #pragma unroll
   for (int j = 0; j < V; ++j) now = fmaxf(now, z[j]);
@@ -171,33 +200,43 @@ __device__ __forceinline__ void add_chunk(Sums& a, const float z[V], float s) {
   }
   a.top = now;
 }
-// The workgroup's sums in every thread (a barrier).
-template <int NW, bool ENT>
+// The same sums relative to `ref`.
+template <bool ENT>
+__device__ __forceinline__ Sums moved(Sums v, float ref, float s) {
+  const float step = (v.top - ref) * s, grown = v.sum == 0.f ? 0.f : power2(step);
+  if (ENT) v.moment = (v.moment + v.sum * finite_log2(step)) * grown;
+  v.sum *= grown;
+  return v;
+}
+// The sums of NW waves' threads in every thread; a barrier if NW > 1, and before `waves` is used again.  With ANY the threads'
+// references differ.
+template <int NW, bool ENT, bool ANY>
 __device__ __forceinline__ Sums join(Sums a, float s, Sums (&waves)[NW]) {
-  auto to = [&](Sums v, float ref) {
-    const float step = (v.top - ref) * s, grown = v.sum == 0.f ? 0.f : power2(step);
-    if (ENT) v.moment = (v.moment + v.sum * finite_log2(step)) * grown;
-    v.sum *= grown;
-    return v;
-  };
-  const float all = wave_max(a.top);
-  a = to(a, reference(all));
+  if constexpr (ANY) {
+    const float all = wave_max(a.top);
+    a = moved<ENT>(a, reference(all), s);
+    a.top = all;
+  }
   a.sum = wave_add(a.sum);
   if (ENT) a.moment = wave_add(a.moment);
-  a.top = all;
-  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = a;
-  __syncthreads();
-  float top = -INFINITY;
+  if constexpr (NW > 1) {
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = a;
+    __syncthreads();
+    float top = a.top;
+    if constexpr (ANY) {
 #pragma unroll
-  for (int w = 0; w < NW; ++w) top = fmaxf(top, waves[w].top);
-  Sums r{top, 0.f, 0.f};
+      for (int w = 0; w < NW; ++w) top = fmaxf(top, waves[w].top);
+    }
+    Sums r{top, 0.f, 0.f};
 #pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    const Sums v = to(waves[w], reference(top));
-    r.sum += v.sum;
-    r.moment += v.moment;
+    for (int w = 0; w < NW; ++w) {
+      const Sums v = ANY ? moved<ENT>(waves[w], reference(top), s) : waves[w];
+      r.sum += v.sum;
+      r.moment += v.moment;
+    }
+    return r;
   }
-  return r;
+  return a;
 }
 
 // What a row's sums and its label's logit say.
@@ -225,7 +264,7 @@ __device__ __forceinline__ RowFacts row_facts(const Sums& r, float z, float s, d
   // log p in 64 bits: the difference of two logits may exceed fp32, and what follows subtracts it
   const double D = ((double)z - (double)top) * inv_t;
   if (r.sum == 0.f) f.logp = 0.0;
-  else if (D > 0) f.logp = -log1p((double)(r.sum * expf((float)-D)));
+  else if (D >= 0) f.logp = -log1p((double)r.sum * (D > 0 ? (double)expf((float)-D) : 1.0));
   else f.logp = D - log((double)r.sum + (double)expf((float)D));
   if (!f.defined) {
     f.logp = NAN;
@@ -251,134 +290,261 @@ __device__ __forceinline__ RowGrad row_grad(const RowFacts& f, float a, float h,
   return g;
 }
 
-// One workgroup of NT threads per row.  CH > 0: the row, of at most NT CH chunks, stays in registers from its sums to its
-// gradient, so that it is read once; CH = 0: any length, read again for the gradient.
-template <bool BF16, bool POLICY, bool ENT, int NT, int CH>
-__global__ __launch_bounds__(NT) void token_loss_kernel(TokenLossArgs a) {
+// What a loss makes of a row's facts: its outputs and the gradient's factors (in every thread that calls it).
+template <bool POLICY, bool ENT>
+__device__ __forceinline__ RowGrad finish_row(const TokenLossArgs& a, int row, const RowFacts& f, bool writes) {
+  float da, dh;
+  if constexpr (POLICY) {
+    // 64 bits: r and exp(d) are powers of differences, and kl is what is left of them
+    double loss = 0.0, kl = 0.0, slope = 0.0;
+    const double A = a.advantage[row];
+    if (A != 0.0) {
+      const double ratio = a.old_logp ? (double)(float)exp(f.logp - (double)a.old_logp[row]) : f.logp == f.logp ? 1.0 : f.logp;
+      const double kept = fmin(fmax(ratio, 1.0 - a.clip_low), 1.0 + a.clip_high);
+      const double plain = ratio * A, cut = kept * A;
+      loss = plain != plain ? plain : -fmin(plain, cut);
+      slope = plain != plain ? plain : plain <= cut ? -plain : 0.0;
+    }
+    if (a.ref_logp) {
+      const double d = (double)a.ref_logp[row] - f.logp, e = expm1(d);
+      const bool beyond = (float)e == INFINITY;
+      kl = beyond ? INFINITY : e - d;
+      if (a.kl_coef != 0.0) {
+        loss += a.kl_coef * kl;
+        slope -= a.kl_coef * (beyond ? INFINITY : e);
+      }
+    }
+    if (a.entropy_coef != 0.0) loss -= a.entropy_coef * (double)f.entropy;
+    if (!f.defined) loss = kl = NAN;
+    if (writes) {
+      if (a.loss) a.loss[row] = (float)loss;
+      if (a.kl) a.kl[row] = (float)kl;
+    }
+    const float g = a.grad_loss ? a.grad_loss[row] : 1.f;
+    da = loss != loss ? NAN : g * (float)slope;
+    dh = g * -(float)a.entropy_coef;
+  } else {
+    da = a.grad_logp ? a.grad_logp[row] : 0.f;
+    dh = a.grad_entropy ? a.grad_entropy[row] : 0.f;
+  }
+  if (writes) {
+    if (a.logp) a.logp[row] = (float)f.logp;
+    if (a.entropy) a.entropy[row] = f.entropy;
+  }
+  return row_grad<ENT>(f, da, dh, (float)a.inv_t);
+}
+
+template <bool BF16>
+__device__ __forceinline__ u32x4 masked_chunk() {
+  constexpr uint32_t m = BF16 ? 0xFF80FF80u : 0xFF800000u;   // -inf in every place
+  return u32x4{m, m, m, m};
+}
+
+// f(a chunk's values) for the chunks first + tid, + NT, .. below `last` of a row that is read for it, UN in flight.
+template <bool BF16, bool STREAM, int NT, typename F>
+__device__ __forceinline__ void for_chunks(const Row<BF16>& r, int first, int last, F&& f) {
+  constexpr int V = Row<BF16>::V, UN = 4;
+  for (int i0 = first; i0 < last; i0 += NT * UN) {
+    u32x4 q[UN];
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      q[u] = masked_chunk<BF16>();
+      if (i0 + u * NT < last) q[u] = r.template load<STREAM>(i0 + u * NT);
+    }
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      float z[V];
+      unpack<BF16, V>(q[u], z);
+      f(z, i0 + u * NT);
+    }
+  }
+}
+
+// Chunk i's gradient from its values.
+template <bool BF16, bool ENT>
+__device__ __forceinline__ void store_gradient(const Row<BF16>& r, char* row, int i, float z[Row<BF16>::V], float top, float s,
+                                               const RowGrad& d) {
+#pragma unroll
+  for (int j = 0; j < Row<BF16>::V; ++j) {
+    const float x = (z[j] - top) * s;
+    z[j] = power2(x) * (ENT ? fmaf(d.f1, finite_log2(x), d.f0) : d.f0);
+  }
+  r.store(row, i, z, d.at_label);
+}
+
+// What a row needs before it is read: false if nothing of it is.
+template <bool BF16, bool POLICY>
+__device__ __forceinline__ bool open_row(const TokenLossArgs& a, int row, Row<BF16>& r, bool& weightless) {
+  const int label = a.labels[row];
+  r.init(a.logits, row * a.ld_row, a.C, label);
+  if (POLICY) weightless = a.grad_loss && a.grad_loss[row] == 0.f;
+  else weightless = !((a.grad_logp && a.grad_logp[row] != 0.f) || (a.grad_entropy && a.grad_entropy[row] != 0.f));
+  return (unsigned)label < (unsigned)a.C;
+}
+__device__ __forceinline__ void no_token(const TokenLossArgs& a, int row) {
+  if (a.loss) a.loss[row] = 0.f;
+  if (a.logp) a.logp[row] = 0.f;
+  if (a.kl) a.kl[row] = 0.f;
+  if (a.entropy) a.entropy[row] = 0.f;
+}
+
+// NT threads per row, G rows a workgroup (G > 1: a wave each).  CH > 0: the row, of at most NT CH chunks, stays in registers
+// from its sums to its gradient, so that it is read once; CH = 0: any length, read again for the gradient.
+template <bool BF16, bool POLICY, bool ENT, int NT, int CH, int G>
+__global__ __launch_bounds__(NT * G) void token_loss_kernel(TokenLossArgs a) {
   constexpr int V = Row<BF16>::V, NW = NT / 64;
+  static_assert(G == 1 || NT == 64, "rows that share a workgroup have no barrier");
   __shared__ Sums waves[NW];
   __shared__ RowGrad shared_grad;
-  const int row = a.row0 + blockIdx.x, tid = threadIdx.x;
-  const int label = a.labels[row];
-  const bool token = (unsigned)label < (unsigned)a.C;
-  const float g = POLICY && a.grad_loss ? a.grad_loss[row] : 1.f;
-  const float a_in = !POLICY && a.grad_logp ? a.grad_logp[row] : 0.f;
-  const float h_in = !POLICY && a.grad_entropy ? a.grad_entropy[row] : 0.f;
-  const bool weightless = POLICY ? g == 0.f : a_in == 0.f && h_in == 0.f;
-  const bool outputs = a.loss || a.logp || a.kl || a.entropy;
+  const int row = a.row0 + blockIdx.x * G + (G > 1 ? threadIdx.x / NT : 0), tid = threadIdx.x % NT;
+  if (G > 1 && row >= a.n) return;
   Row<BF16> r;
-  r.init(a.logits, row * a.ld_row, a.C, label);
+  bool weightless;
+  const bool token = open_row<BF16, POLICY>(a, row, r, weightless);
   char* const d_row = (char*)a.grad + row * a.ld_grad * (16 / V);
-  if (a.grad && (!token || weightless)) r.template zero<NT>(d_row);
+  if (a.grad && (!token || weightless)) r.template zero<NT>(d_row, tid);
   if (!token) {
-    if (tid == 0) {
-      if (a.loss) a.loss[row] = 0.f;
-      if (a.logp) a.logp[row] = 0.f;
-      if (a.kl) a.kl[row] = 0.f;
-      if (a.entropy) a.entropy[row] = 0.f;
-    }
+    if (tid == 0) no_token(a, row);
     return;
   }
-  if (weightless && !outputs) return;
+  if (weightless && !(a.loss || a.logp || a.kl || a.entropy)) return;
 
   u32x4 held[CH > 0 ? CH : 1];
-  const u32x4 masked = BF16 ? u32x4{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u}
-                            : u32x4{0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u};
-  Sums sums{-INFINITY, 0.f, 0.f};
   if constexpr (CH > 0) {
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      held[i] = masked;
+      held[i] = masked_chunk<BF16>();
       if (i * NT + tid < r.chunks) held[i] = r.template load<true>(i * NT + tid);
     }
   }
-  const float z_label = element<BF16>(r.x, label);
-  float z[V];
-  if constexpr (CH > 0) {
+  const float z_label = element<BF16>(r.x, r.label);
+  auto each = [&](auto&& f) {
+    if constexpr (CH > 0) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      unpack<BF16, V>(held[i], z);
-      add_chunk<V, ENT>(sums, z, a.s);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  } else {
-    constexpr int UN = 4;
-    for (int i0 = tid; i0 < r.chunks; i0 += NT * UN) {
-      u32x4 q[UN];
-#pragma unroll
-      for (int u = 0; u < UN; ++u) {
-        q[u] = masked;
-        if (i0 + u * NT < r.chunks) q[u] = r.template load<true>(i0 + u * NT);
+      for (int i = 0; i < CH; ++i) {
+        float z[V];
+        // opaque here, or the compiler keeps every pass's unpacked values for the next one
+        asm volatile("" : "+v"(held[i][0]), "+v"(held[i][1]), "+v"(held[i][2]), "+v"(held[i][3]));
+        unpack<BF16, V>(held[i], z);
+        f(z, i * NT + tid);
+        __builtin_amdgcn_sched_barrier(0);                   // one chunk's values at a time in registers
       }
-#pragma unroll
-      for (int u = 0; u < UN; ++u) {
-        unpack<BF16, V>(q[u], z);
-        add_chunk<V, ENT>(sums, z, a.s);
-      }
+    } else {
+      for_chunks<BF16, false, NT>(r, tid, r.chunks, f);
     }
+  };
+  Sums sums{z_label, 0.f, 0.f};
+  float lost = 0.f;
+  each([&](const float* z, int) { add_chunk<V, ENT, false>(sums, lost, z, z_label, a.s); });
+  sums = join<NW, ENT, false>(sums, a.s.hi, waves);
+  if (!bounded<ENT>(sums)) {                                 // the same in all of the row's threads
+    if constexpr (NW > 1) __syncthreads();
+    sums = Sums{-INFINITY, 0.f, 0.f};
+    each([&](const float* z, int) { add_chunk_any<V, ENT>(sums, z, a.s.hi); });
+    sums = join<NW, ENT, true>(sums, a.s.hi, waves);
   }
-  sums = join<NW, ENT>(sums, a.s, waves);
-  if (tid < 64) {
-    const RowFacts f = row_facts<ENT>(sums, z_label, a.s, a.inv_t);
-    float da = a_in, dh = h_in;
-    if constexpr (POLICY) {
-      // 64 bits: r and exp(d) are powers of differences, and kl is what is left of them
-      double loss = 0.0, kl = 0.0, slope = 0.0;
-      const double A = a.advantage[row];
-      if (A != 0.0) {
-        const double ratio = a.old_logp ? (double)(float)exp(f.logp - (double)a.old_logp[row]) : f.logp == f.logp ? 1.0 : f.logp;
-        const double kept = fmin(fmax(ratio, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high);
-        const double plain = ratio * A, cut = kept * A;
-        loss = plain != plain ? plain : -fmin(plain, cut);
-        slope = plain != plain ? plain : plain <= cut ? -plain : 0.0;
-      }
-      if (a.ref_logp) {
-        const double d = (double)a.ref_logp[row] - f.logp, e = (double)(float)exp(d);
-        kl = e < INFINITY || d != d ? expm1(d) - d : INFINITY;
-        if (a.kl_coef != 0.f) {
-          loss += (double)a.kl_coef * kl;
-          slope -= (double)a.kl_coef * (e < INFINITY || d != d ? expm1(d) : INFINITY);
-        }
-      }
-      if (a.entropy_coef != 0.f) loss -= (double)a.entropy_coef * (double)f.entropy;
-      if (!f.defined) loss = NAN;
-      if (tid == 0) {
-        if (a.loss) a.loss[row] = (float)loss;
-        if (a.kl) a.kl[row] = f.defined ? (float)kl : NAN;
-      }
-      da = loss != loss ? NAN : g * (float)slope;
-      dh = g * -a.entropy_coef;
+  RowGrad d{};
+  if (NW == 1 || threadIdx.x < 64) {
+    d = finish_row<POLICY, ENT>(a, row, row_facts<ENT>(sums, z_label, a.s.hi, a.inv_t), tid == 0);
+    if (NW > 1 && tid == 0) shared_grad = d;
+  }
+  if (!a.grad || weightless) return;
+  if constexpr (NW > 1) {
+    __syncthreads();
+    d = shared_grad;
+  }
+  const float top = reference(sums.top);
+  each([&](float* z, int i) {
+    if (i < r.chunks) store_gradient<BF16, ENT>(r, d_row, i, z, top, a.s.hi, d);
+  });
+}
+
+// ---------------------------------------------------------------- rows in parts
+
+// The sums of part p of row i into parts[i][p]: chunks p per .. + per - 1.
+template <bool BF16, bool ENT, bool PRECISE, int NT>
+__device__ __forceinline__ void part_sums(const Row<BF16>& r, int p, int per, const Scale& s, Sums* out) {
+  constexpr int V = Row<BF16>::V, NW = NT / 64;
+  __shared__ Sums waves[NW];
+  const int first = p * per + threadIdx.x, last = min(r.chunks, (p + 1) * per);
+  const float z_label = element<BF16>(r.x, r.label);
+  Sums sums{z_label, 0.f, 0.f};
+  float lost = 0.f;
+  for_chunks<BF16, false, NT>(r, first, last, [&](const float* z, int) { add_chunk<V, ENT, PRECISE>(sums, lost, z, z_label, s); });
+  if (PRECISE) sums.sum += kLn2 * lost;
+  sums = join<NW, ENT, false>(sums, s.hi, waves);
+  if (!bounded<ENT>(sums)) {
+    __syncthreads();
+    sums = Sums{-INFINITY, 0.f, 0.f};
+    for_chunks<BF16, false, NT>(r, first, last, [&](const float* z, int) { add_chunk_any<V, ENT>(sums, z, s.hi); });
+    sums = join<NW, ENT, true>(sums, s.hi, waves);
+  }
+  if (threadIdx.x == 0) *out = sums;
+}
+// A row's sums from its parts', in every lane of a wave.
+template <bool ENT>
+__device__ __forceinline__ Sums join_parts(const Sums* parts, int n, float s) {
+  const int lane = threadIdx.x & 63;
+  Sums a{-INFINITY, 0.f, 0.f};
+  for (int p = lane; p < n; p += 64) {
+    Sums b = parts[p];
+    const float top = fmaxf(a.top, b.top);
+    const float ref = reference(top);
+    a = moved<ENT>(a, ref, s);
+    b = moved<ENT>(b, ref, s);
+    a = Sums{top, a.sum + b.sum, a.moment + b.moment};
+  }
+  Sums none[1];
+  return join<1, ENT, true>(a, s, none);
+}
+
+template <bool BF16, bool POLICY, bool ENT, int NT>
+__global__ __launch_bounds__(NT) void token_parts_kernel(TokenLossArgs a) {
+  const int row = a.row0 + blockIdx.y;
+  Row<BF16> r;
+  bool weightless;
+  const bool token = open_row<BF16, POLICY>(a, row, r, weightless);
+  if (!token || (weightless && !(a.loss || a.logp || a.kl || a.entropy))) return;
+  part_sums<BF16, ENT, false, NT>(r, blockIdx.x, a.per_part, a.s, (Sums*)a.parts + (long long)row * a.n_parts + blockIdx.x);
+}
+
+// The outputs (by the first part) and a part's gradient.
+template <bool BF16, bool POLICY, bool ENT, int NT>
+__global__ __launch_bounds__(NT) void token_parts_grad_kernel(TokenLossArgs a) {
+  constexpr int V = Row<BF16>::V;
+  __shared__ RowGrad shared_grad;
+  __shared__ float shared_top;
+  const int row = a.row0 + blockIdx.y, p = blockIdx.x;
+  Row<BF16> r;
+  bool weightless;
+  const bool token = open_row<BF16, POLICY>(a, row, r, weightless);
+  const int first = p * a.per_part + threadIdx.x, last = min(r.chunks, (p + 1) * a.per_part);
+  char* const d_row = (char*)a.grad + row * a.ld_grad * (16 / V);
+  if (!token || weightless) {
+    if (a.grad)
+      for (int i = first; i < last; i += NT) r.zero_chunk(d_row, i);
+    if (!token) {
+      if (p == 0 && threadIdx.x == 0) no_token(a, row);
+      return;
     }
-    if (tid == 0) {
-      if (a.logp) a.logp[row] = (float)f.logp;
-      if (a.entropy) a.entropy[row] = f.entropy;
-      shared_grad = row_grad<ENT>(f, da, dh, (float)a.inv_t);
+    if (p > 0 || !(a.loss || a.logp || a.kl || a.entropy)) return;
+  }
+  if (threadIdx.x < 64) {
+    const Sums sums = join_parts<ENT>((const Sums*)a.parts + (long long)row * a.n_parts, a.n_parts, a.s.hi);
+    const float z_label = element<BF16>(r.x, r.label);
+    const RowGrad d = finish_row<POLICY, ENT>(a, row, row_facts<ENT>(sums, z_label, a.s.hi, a.inv_t), p == 0 && threadIdx.x == 0);
+    if (threadIdx.x == 0) {
+      shared_grad = d;
+      shared_top = reference(sums.top);
     }
   }
   if (!a.grad || weightless) return;
   __syncthreads();
   const RowGrad d = shared_grad;
-  const float top = reference(sums.top);
-  auto gradient = [&](u32x4 q, int i) {
-    unpack<BF16, V>(q, z);
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const float x = (z[j] - top) * a.s;
-      z[j] = power2(x) * (ENT ? d.f0 + d.f1 * finite_log2(x) : d.f0);
-    }
-    r.store(d_row, i, z, d.at_label);
-  };
-  if constexpr (CH > 0) {
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      // opaque here, or the compiler keeps the first pass's unpacked values
-      asm volatile("" : "+v"(held[i][0]), "+v"(held[i][1]), "+v"(held[i][2]), "+v"(held[i][3]));
-      if (i * NT + tid < r.chunks) gradient(held[i], i * NT + tid);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  } else {
-    for (int i = tid; i < r.chunks; i += NT) gradient(r.template load<true>(i), i);
-  }
+  const float top = shared_top;
+  for_chunks<BF16, true, NT>(r, first, last, [&](float* z, int i) {
+    if (i < last) store_gradient<BF16, ENT>(r, d_row, i, z, top, a.s.hi, d);
+  });
 }
 
 // ---------------------------------------------------------------- preference
@@ -389,53 +555,27 @@ __device__ __forceinline__ int offset_at(const PreferenceArgs& a, int i) {
   return (int)(at < 0 ? 0 : at > a.n ? a.n : at);
 }
 
+// The sums of the rows of pairs pair0 .. pair1 - 1, a workgroup a part of a row in turn.
 template <bool BF16, int NT>
-__global__ __launch_bounds__(NT) void preference_stats_kernel(PreferenceArgs a) {
-  constexpr int V = Row<BF16>::V, NW = NT / 64, UN = 4;
-  __shared__ Sums waves[NW];
-  const int row = a.row0 + blockIdx.x, tid = threadIdx.x;
-  if (row < offset_at(a, 0) || row >= offset_at(a, 2 * a.pairs)) return;
-  const int label = a.labels[row];
-  if ((unsigned)label >= (unsigned)a.C) return;
-  Row<BF16> r;
-  r.init(a.logits, row * a.ld_row, a.C, label);
-  const u32x4 masked = BF16 ? u32x4{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u}
-                            : u32x4{0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u};
-  const float z_label = element<BF16>(r.x, label);
-  Sums sums{-INFINITY, 0.f, 0.f};
-  for (int i0 = tid; i0 < r.chunks; i0 += NT * UN) {
-    u32x4 q[UN];
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      q[u] = masked;
-      if (i0 + u * NT < r.chunks) q[u] = r.template load<false>(i0 + u * NT);
-    }
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      float z[V];
-      unpack<BF16, V>(q[u], z);
-      add_chunk<V, false>(sums, z, a.s);
-    }
-  }
-  sums = join<NW, false>(sums, a.s, waves);
-  if (tid < 64) {
-    const RowFacts f = row_facts<false>(sums, z_label, a.s, a.inv_t);
-    if (tid == 0) {
-      PreferenceRow& out = a.rows[row];
-      out.delta = f.logp - (a.ref_logp ? (double)a.ref_logp[row] : 0.0);
-      out.top = reference(sums.top);
-      out.share = f.defined ? f.share : NAN;
-      out.rest = f.defined ? f.rest : NAN;
-    }
+__global__ __launch_bounds__(NT) void preference_sums_kernel(PreferenceArgs a) {
+  const int end = offset_at(a, 2 * a.pair1);
+  for (int row = offset_at(a, 2 * a.pair0) + blockIdx.y; row < end; row += gridDim.y) {
+    const int label = a.labels[row];
+    if ((unsigned)label >= (unsigned)a.C) continue;
+    Row<BF16> r;
+    r.init(a.logits, row * a.ld_row, a.C, label);
+    part_sums<BF16, false, true, NT>(r, blockIdx.x, a.per_part, a.s, (Sums*)a.parts + (long long)row * a.n_parts + blockIdx.x);
+    __syncthreads();
   }
 }
 
-// One workgroup per pair: its answers' sums in 64 bits (a thread's rows in their order, then a tree, the same every
-// time), the loss, and every row's weight.
+// One workgroup per pair: its rows' log p from their sums, its answers' sums in 64 bits (a thread's rows in their order, then
+// a tree, the same every time), the loss, and every row's weight.
+template <bool BF16>
 __global__ __launch_bounds__(256) void preference_pairs_kernel(PreferenceArgs a) {
   __shared__ double sums[2][4];
   __shared__ int counts[2][4];
-  const int p = blockIdx.x, tid = threadIdx.x;
+  const int p = a.pair0 + blockIdx.x, tid = threadIdx.x;
   int at[3];
 #pragma unroll
   for (int k = 0; k < 3; ++k) at[k] = offset_at(a, 2 * p + k);
@@ -444,11 +584,27 @@ __global__ __launch_bounds__(256) void preference_pairs_kernel(PreferenceArgs a)
   for (int k = 0; k < 2; ++k) {
     double sum = 0.0;
     int count = 0;
-    for (int row = at[k] + tid; row < at[k + 1]; row += 256)
-      if (token(row)) {
-        sum += a.rows[row].delta;
-        ++count;
+    for (int row = at[k] + tid; row < at[k + 1]; row += 256) {
+      const int label = a.labels[row];
+      if ((unsigned)label >= (unsigned)a.C) continue;
+      const Sums* parts = (const Sums*)a.parts + (long long)row * a.n_parts;
+      Sums all{-INFINITY, 0.f, 0.f};
+      for (int q = 0; q < a.n_parts; ++q) {
+        Sums b = parts[q];
+        const float top = fmaxf(all.top, b.top), ref = reference(top);
+        all = moved<false>(all, ref, a.s.hi);
+        b = moved<false>(b, ref, a.s.hi);
+        all = Sums{top, all.sum + b.sum, 0.f};
       }
+      const float z = element<BF16>((const char*)a.logits + row * a.ld_row * (BF16 ? 2 : 4), label);
+      const RowFacts f = row_facts<false>(all, z, a.s.hi, a.inv_t);
+      PreferenceRow& out = a.rows[row];
+      out.top = reference(all.top);
+      out.share = f.defined ? f.share : NAN;
+      out.rest = f.defined ? f.rest : NAN;
+      sum += f.logp - (a.ref_logp ? (double)a.ref_logp[row] : 0.0);
+      ++count;
+    }
     sum = wave_add(sum);
     count = wave_add(count);
     if ((tid & 63) == 0) {
@@ -462,12 +618,13 @@ __global__ __launch_bounds__(256) void preference_pairs_kernel(PreferenceArgs a)
   for (int k = 0; k < 2; ++k) {
     const int count = counts[k][0] + counts[k][1] + counts[k][2] + counts[k][3];
     per[k] = a.mean && count ? 1.0 / count : 1.0;
-    score[k] = (double)a.beta * ((sums[k][0] + sums[k][1] + sums[k][2] + sums[k][3]) * per[k]);
+    score[k] = a.beta * ((sums[k][0] + sums[k][1] + sums[k][2] + sums[k][3]) * per[k]);
   }
   const double u = score[0] - score[1], smooth = a.smoothing;
-  const double soft = log1p(exp(-fabs(u))), up = u > 0 ? 1 / (1 + exp(-u)) : exp(u) / (1 + exp(u));   // sigmoid(u)
-  const double down = u > 0 ? exp(-u) / (1 + exp(-u)) : 1 / (1 + exp(u));                            // sigmoid(-u)
+  const double e = exp(-fabs(u)), big = 1 / (1 + e), small = e / (1 + e);
+  const double up = u > 0 ? big : small, down = u > 0 ? small : big;   // sigmoid(u), sigmoid(-u)
   if (tid == 0) {
+    const double soft = log1p(e);
     double loss = (1 - smooth) * (soft + (u < 0 ? -u : 0.0));
     if (smooth > 0) loss += smooth * (soft + (u > 0 ? u : 0.0));
     if (a.loss) a.loss[p] = u == u ? (float)loss : NAN;
@@ -478,7 +635,7 @@ __global__ __launch_bounds__(256) void preference_pairs_kernel(PreferenceArgs a)
   }
   if (!a.grad) return;
   const double g = a.grad_loss ? (double)a.grad_loss[p] : 1.0;
-  const double du = g == 0 ? 0.0 : (double)a.beta * g * (smooth * up - (1 - smooth) * down);
+  const double du = g == 0 ? 0.0 : u == u ? a.beta * g * (smooth * up - (1 - smooth) * down) : NAN;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const float weight = (float)((k ? -du : du) * per[k] * a.inv_t);
@@ -489,89 +646,115 @@ __global__ __launch_bounds__(256) void preference_pairs_kernel(PreferenceArgs a)
 template <bool BF16, int NT>
 __global__ __launch_bounds__(NT) void preference_grad_kernel(PreferenceArgs a) {
   constexpr int V = Row<BF16>::V;
-  const int row = a.row0 + blockIdx.x, tid = threadIdx.x;
-  if (row < offset_at(a, 0) || row >= offset_at(a, 2 * a.pairs)) return;
-  const PreferenceRow f = a.rows[row];
-  Row<BF16> r;
-  r.init(a.logits, row * a.ld_row, a.C, a.labels[row]);
-  char* const d_row = (char*)a.grad + row * a.ld_grad * (16 / V);
-  if (f.weight == 0.f) return r.template zero<NT>(d_row);
-  const float factor = -f.weight * f.share, at_label = f.weight * f.rest;
-  for (int i = tid; i < r.chunks; i += NT) {
-    float z[V];
-    unpack<BF16, V>(r.template load<false>(i), z);
-#pragma unroll
-    for (int j = 0; j < V; ++j) z[j] = factor * power2((z[j] - f.top) * a.s);
-    r.store(d_row, i, z, at_label);
+  const int begin = offset_at(a, 2 * a.pair0), end = offset_at(a, 2 * a.pair1);
+  for (int k = blockIdx.y; k < end - begin; k += gridDim.y) {
+    const int row = end - 1 - k;                             // the last rows read are the likeliest to lie in a cache
+    const PreferenceRow f = a.rows[row];
+    Row<BF16> r;
+    r.init(a.logits, row * a.ld_row, a.C, a.labels[row]);
+    char* const d_row = (char*)a.grad + row * a.ld_grad * (16 / V);
+    const int first = blockIdx.x * a.per_part + threadIdx.x, last = min(r.chunks, ((int)blockIdx.x + 1) * a.per_part);
+    if (f.weight == 0.f) {
+      for (int i = first; i < last; i += NT) r.zero_chunk(d_row, i);
+      continue;
+    }
+    const RowGrad d{-f.weight * f.share, 0.f, f.weight * f.rest};
+    for_chunks<BF16, true, NT>(r, first, last, [&](float* z, int i) {
+      if (i < last) store_gradient<BF16, false>(r, d_row, i, z, f.top, a.s.hi, d);
+    });
   }
 }
 
-// 2^20 rows a launch at most.
-template <typename Args, typename F>
-hipError_t launch_row_ranges(const Args& a, F&& launch_rows) {
-  Args part = a;
-  for (long long row = 0; row < a.n; row += 1 << 20) {
-    part.row0 = (int)row;
-    launch_rows(part, dim3((unsigned)std::min<long long>(a.n - row, 1 << 20)));
+// Workgroups of a launch's second axis, and rows that it takes at most.
+constexpr int kGridRows = 1 << 15;
+
+template <bool BF16, bool POLICY, bool ENT, int NT, int CH, int G>
+hipError_t launch_loss_rows(const TokenLossArgs& args, hipStream_t s) {
+  TokenLossArgs a = args;
+  for (long long row = 0; row < args.n; row += (1 << 20) * G) {   // 2^20 workgroups a launch at most
+    a.row0 = (int)row;
+    const long long rows = std::min<long long>(args.n - row, (1 << 20) * G);
+    launch(token_loss_kernel<BF16, POLICY, ENT, NT, CH, G>, dim3((unsigned)((rows + G - 1) / G)), dim3(NT * G), s, a);
     const hipError_t st = hipGetLastError();
     if (st != hipSuccess) return st;
   }
   return hipSuccess;
 }
 
-template <bool BF16, bool POLICY, bool ENT, int NT, int CH>
-hipError_t launch_loss_rows(const TokenLossArgs& a, hipStream_t s) {
-  return launch_row_ranges(a, [&](const TokenLossArgs& part, dim3 grid) {
-    launch(token_loss_kernel<BF16, POLICY, ENT, NT, CH>, grid, dim3(NT), s, part);
-  });
+// Parts of a row of so many chunks, so that n rows give work to the whole GPU; 1: rows stay whole.
+int parts_of(long long n, int chunks) {
+  constexpr int kLeast = 512, kGroups = 512;                 // chunks of a part at least; workgroups to aim at
+  return (int)std::max<long long>(1, std::min<long long>(kGroups / std::max<long long>(n, 1), chunks / kLeast));
 }
 
 template <bool BF16, bool POLICY, bool ENT>
-hipError_t launch_loss_by_length(const TokenLossArgs& a, hipStream_t s) {
+hipError_t launch_loss_parts(const TokenLossArgs& a, hipStream_t s) {
+  constexpr int NT = 256;
+  launch(token_parts_kernel<BF16, POLICY, ENT, NT>, dim3(a.n_parts, a.n), dim3(NT), s, a);
+  const hipError_t st = hipGetLastError();
+  if (st != hipSuccess) return st;
+  launch(token_parts_grad_kernel<BF16, POLICY, ENT, NT>, dim3(a.grad ? a.n_parts : 1, a.n), dim3(NT), s, a);
+  return hipGetLastError();
+}
+
+template <bool BF16, bool POLICY, bool ENT>
+hipError_t launch_loss_by_length(const TokenLossArgs& args, hipStream_t s) {
+  TokenLossArgs a = args;
   const int chunks = (a.C + Row<BF16>::V - 1) / Row<BF16>::V;
-  if (!a.grad) {
-    if (chunks <= 128 * 4) return launch_loss_rows<BF16, POLICY, ENT, 128, 0>(a, s);
-    if (chunks <= 256 * 16) return launch_loss_rows<BF16, POLICY, ENT, 256, 0>(a, s);
-    return launch_loss_rows<BF16, POLICY, ENT, 1024, 0>(a, s);
-  }
-  if (chunks <= 128 * 2) return launch_loss_rows<BF16, POLICY, ENT, 128, 2>(a, s);
-  if (chunks <= 128 * 8) return launch_loss_rows<BF16, POLICY, ENT, 128, 8>(a, s);
-  if (chunks <= 256 * 8) return launch_loss_rows<BF16, POLICY, ENT, 256, 8>(a, s);
-  if (chunks <= 256 * 16) return launch_loss_rows<BF16, POLICY, ENT, 256, 16>(a, s);
-  if (chunks <= 512 * 16) return launch_loss_rows<BF16, POLICY, ENT, 512, 16>(a, s);
-  if (chunks <= 1024 * 16) return launch_loss_rows<BF16, POLICY, ENT, 1024, 16>(a, s);
-  if (chunks <= 1024 * 20) return launch_loss_rows<BF16, POLICY, ENT, 1024, 20>(a, s);
-  return launch_loss_rows<BF16, POLICY, ENT, 1024, 0>(a, s);
+  a.n_parts = parts_of(a.n, chunks);
+  a.per_part = (chunks + a.n_parts - 1) / a.n_parts;
+  if (a.n_parts > 1) return launch_loss_parts<BF16, POLICY, ENT>(a, s);
+  if (chunks <= 64 * 4) return launch_loss_rows<BF16, POLICY, ENT, 64, 4, 4>(a, s);
+  if (chunks <= 128 * 8) return launch_loss_rows<BF16, POLICY, ENT, 128, 8, 1>(a, s);
+  if (chunks <= 256 * 8) return launch_loss_rows<BF16, POLICY, ENT, 256, 8, 1>(a, s);
+  return launch_loss_rows<BF16, POLICY, ENT, 512, 0, 1>(a, s);
 }
 
 template <bool BF16>
 hipError_t launch_loss(const TokenLossArgs& a, hipStream_t s) {
-  const bool ent = a.entropy || a.grad_entropy || a.entropy_coef != 0.f;
+  const bool ent = a.entropy || a.grad_entropy || a.entropy_coef != 0.0;
   if (a.policy) return ent ? launch_loss_by_length<BF16, true, true>(a, s) : launch_loss_by_length<BF16, true, false>(a, s);
   return ent ? launch_loss_by_length<BF16, false, true>(a, s) : launch_loss_by_length<BF16, false, false>(a, s);
 }
 
 template <bool BF16>
-hipError_t launch_preference_of(const PreferenceArgs& a, hipStream_t s) {
-  hipError_t st = launch_row_ranges(a, [&](const PreferenceArgs& part, dim3 grid) {
-    launch(preference_stats_kernel<BF16, 256>, grid, dim3(256), s, part);
-  });
+hipError_t launch_preference_of(const PreferenceArgs& args, hipStream_t s) {
+  PreferenceArgs a = args;
+  const int chunks = (a.C + Row<BF16>::V - 1) / Row<BF16>::V;
+  a.n_parts = parts_of(a.n, chunks);
+  a.per_part = (chunks + a.n_parts - 1) / a.n_parts;
+  const dim3 grid(a.n_parts, std::min(a.n, kGridRows));
+  a.pair0 = 0;
+  a.pair1 = a.pairs;
+  launch(preference_sums_kernel<BF16, 256>, grid, dim3(256), s, a);
+  hipError_t st = hipGetLastError();
   if (st != hipSuccess) return st;
-  launch(preference_pairs_kernel, dim3(a.pairs), dim3(256), s, a);
+  launch(preference_pairs_kernel<BF16>, dim3(a.pair1 - a.pair0), dim3(256), s, a);
   st = hipGetLastError();
   if (st != hipSuccess || !a.grad) return st;
-  return launch_row_ranges(a, [&](const PreferenceArgs& part, dim3 grid) {
-    launch(preference_grad_kernel<BF16, 256>, grid, dim3(256), s, part);
-  });
+  launch(preference_grad_kernel<BF16, 256>, grid, dim3(256), s, a);
+  return hipGetLastError();
 }
 
 }  // namespace
+
+long long token_loss_workspace_bytes(int n, int n_classes) {
+  // the parts of a row of fp32 values, which has more chunks
+  const int parts = parts_of(n, (n_classes + 3) / 4);
+  return parts > 1 ? ((long long)n * parts * (long long)sizeof(Sums) + 15) / 16 * 16 : 0;
+}
+long long preference_workspace_bytes(int n, int n_classes) {
+  return ((long long)n * (long long)sizeof(PreferenceRow) + 15) / 16 * 16 +
+         ((long long)n * parts_of(n, (n_classes + 3) / 4) * (long long)sizeof(Sums) + 15) / 16 * 16;
+}
 
 hipError_t launch_token_loss(const TokenLossArgs& a, bool bf16, hipStream_t s) {
   return bf16 ? launch_loss<true>(a, s) : launch_loss<false>(a, s);
 }
 
-hipError_t launch_preference(const PreferenceArgs& a, bool bf16, hipStream_t s) {
+hipError_t launch_preference(const PreferenceArgs& args, bool bf16, hipStream_t s) {
+  PreferenceArgs a = args;
+  a.parts = (char*)a.rows + ((long long)a.n * (long long)sizeof(PreferenceRow) + 15) / 16 * 16;
   return bf16 ? launch_preference_of<true>(a, s) : launch_preference_of<false>(a, s);
 }
 

@@ -33,24 +33,27 @@ long long combine_bytes(int n_models, int n, int n_classes) {
 bool fc_mx4_sizes(int n, int c_in, int c_out) {
   return n >= 1 && n <= (1 << 24) && c_out >= 1 && c_out <= (1 << 24) && c_in >= 32 && c_in <= (1 << 20) && c_in % 32 == 0;
 }
-bool preference_sizes(int n, int n_pairs) { return n >= 1 && n_pairs >= 1 && n_pairs <= (1 << 24); }
-long long preference_bytes(int n) { return ((long long)n * (long long)sizeof(PreferenceRow) + 15) / 16 * 16; }
+bool row_sizes(int n, int n_classes) { return n >= 1 && n_classes >= 1 && n_classes <= kMaxTokenClasses; }
+bool bad_workspace(const void* workspace, long long bytes, long long need) {
+  return need && (!workspace || bytes < need || !aligned16(workspace));
+}
 
 // What the losses over given tokens have alike.
-int check_rows(const void* logits, int dtype, long long ld_row, int n, int n_classes, const void* labels, float temperature,
-               const void* grad_logits, long long ld_grad) {
+int check_rows(const void* logits, int dtype, long long ld_row, int n, int n_classes, const void* labels, double temperature,
+               const void* grad_logits, long long ld_grad, const void* workspace, long long bytes, long long (*need)(int, int)) {
   if (!logits || !labels) return invalid("null pointer");
   if (!known(dtype)) return invalid("dtype must be RAFIKI_FP32 or RAFIKI_BF16");
-  if (n < 1 || n_classes < 1 || n_classes > kMaxTokenClasses)
-    return invalid("n must be >= 1 and n_classes in [1, 2^20]");
-  if (!(temperature >= 0x1p-20f && temperature <= 0x1p20f)) return invalid("temperature must be in [2^-20, 2^20]");
+  if (!row_sizes(n, n_classes)) return invalid("n must be >= 1 and n_classes in [1, 2^20]");
+  if (!(temperature >= 0x1p-20 && temperature <= 0x1p20)) return invalid("temperature must be in [2^-20, 2^20]");
   if (ld_row < 0 || (grad_logits && ld_grad < n_classes)) return invalid("row distances: ld_row >= 0, ld_grad >= n_classes");
   if (!aligned_to(logits, dtype) || !aligned_to(grad_logits, dtype)) return invalid("rows are not aligned to their type");
+  if (bad_workspace(workspace, bytes, need(n, n_classes)))
+    return invalid("workspace is null, too small or not on a 16-byte boundary");
   return RAFIKI_OK;
 }
 
 template <typename Args>
-Args row_args(const void* logits, long long ld_row, int n, int n_classes, const int32_t* labels, float temperature,
+Args row_args(const void* logits, long long ld_row, int n, int n_classes, const int32_t* labels, double temperature,
               void* grad_logits, long long ld_grad) {
   Args a{};
   a.logits = logits;
@@ -58,8 +61,10 @@ Args row_args(const void* logits, long long ld_row, int n, int n_classes, const 
   a.n = n;
   a.C = n_classes;
   a.labels = labels;
-  a.inv_t = 1.0 / (double)temperature;
-  a.s = (float)(1.4426950408889634 / (double)temperature);
+  a.inv_t = 1.0 / temperature;
+  const double s = 1.4426950408889634 / temperature;
+  a.s.hi = (float)s;
+  a.s.lo = (float)(s - (double)a.s.hi);
   a.grad = grad_logits;
   a.ld_grad = ld_grad;
   return a;
@@ -172,9 +177,11 @@ int rafiki_distill_loss(const void* logits, int dtype, long long ld_row, int n, 
 }
 
 int rafiki_token_logp(const void* logits, int dtype, long long ld_row, int n, int n_classes, const int32_t* labels,
-                      float temperature, const float* grad_logp, const float* grad_entropy, float* out_logp,
-                      float* out_entropy, void* grad_logits, long long ld_grad, void* stream) {
-  const int rc = check_rows(logits, dtype, ld_row, n, n_classes, labels, temperature, grad_logits, ld_grad);
+                      double temperature, const float* grad_logp, const float* grad_entropy, float* out_logp,
+                      float* out_entropy, void* grad_logits, long long ld_grad, void* workspace,
+                      long long workspace_bytes, void* stream) {
+  const int rc = check_rows(logits, dtype, ld_row, n, n_classes, labels, temperature, grad_logits, ld_grad, workspace,
+                            workspace_bytes, token_loss_workspace_bytes);
   if (rc) return rc;
   if (!out_logp && !out_entropy && !grad_logits) return invalid("no output is asked for");
   if (grad_logits && !grad_logp && !grad_entropy) return invalid("grad_logits needs grad_logp or grad_entropy");
@@ -183,19 +190,28 @@ int rafiki_token_logp(const void* logits, int dtype, long long ld_row, int n, in
   a.grad_entropy = grad_logits ? grad_entropy : nullptr;
   a.logp = out_logp;
   a.entropy = out_entropy;
+  a.parts = workspace;
   return launched(launch_token_loss(a, dtype == RAFIKI_BF16, (hipStream_t)stream), "token_logp");
 }
 
+int rafiki_token_workspace(int n, int n_classes, long long* bytes) {
+  if (!bytes) return invalid("null pointer");
+  if (!row_sizes(n, n_classes)) return invalid("n must be >= 1 and n_classes in [1, 2^20]");
+  *bytes = token_loss_workspace_bytes(n, n_classes);
+  return RAFIKI_OK;
+}
+
 int rafiki_policy_loss(const void* logits, int dtype, long long ld_row, int n, int n_classes, const int32_t* labels,
-                       const float* advantage, const float* old_logp, const float* ref_logp, float temperature,
-                       float clip_low, float clip_high, float kl_coef, float entropy_coef, const float* grad_loss,
+                       const float* advantage, const float* old_logp, const float* ref_logp, double temperature,
+                       double clip_low, double clip_high, double kl_coef, double entropy_coef, const float* grad_loss,
                        float* out_loss, float* out_logp, float* out_kl, float* out_entropy, void* grad_logits,
-                       long long ld_grad, void* stream) {
-  const int rc = check_rows(logits, dtype, ld_row, n, n_classes, labels, temperature, grad_logits, ld_grad);
+                       long long ld_grad, void* workspace, long long workspace_bytes, void* stream) {
+  const int rc = check_rows(logits, dtype, ld_row, n, n_classes, labels, temperature, grad_logits, ld_grad, workspace,
+                            workspace_bytes, token_loss_workspace_bytes);
   if (rc) return rc;
   if (!advantage) return invalid("null advantage");
   if (!out_loss && !out_logp && !out_kl && !out_entropy && !grad_logits) return invalid("no output is asked for");
-  if (!(clip_low >= 0.f && clip_low <= 1.f) || !(clip_high >= 0.f))
+  if (!(clip_low >= 0 && clip_low <= 1) || !(clip_high >= 0))
     return invalid("clip_low must be in [0, 1] and clip_high >= 0");
   if (!std::isfinite(kl_coef) || !std::isfinite(entropy_coef)) return invalid("kl_coef and entropy_coef must be finite");
   TokenLossArgs a = row_args<TokenLossArgs>(logits, ld_row, n, n_classes, labels, temperature, grad_logits, ld_grad);
@@ -212,30 +228,30 @@ int rafiki_policy_loss(const void* logits, int dtype, long long ld_row, int n, i
   a.logp = out_logp;
   a.kl = out_kl;
   a.entropy = out_entropy;
+  a.parts = workspace;
   return launched(launch_token_loss(a, dtype == RAFIKI_BF16, (hipStream_t)stream), "policy_loss");
 }
 
-int rafiki_preference_workspace(int n, int n_pairs, long long* bytes) {
+int rafiki_preference_workspace(int n, int n_classes, long long* bytes) {
   if (!bytes) return invalid("null pointer");
-  if (!preference_sizes(n, n_pairs)) return invalid("n must be >= 1 and n_pairs in [1, 2^24]");
-  *bytes = preference_bytes(n);
+  if (!row_sizes(n, n_classes)) return invalid("n must be >= 1 and n_classes in [1, 2^20]");
+  *bytes = preference_workspace_bytes(n, n_classes);
   return RAFIKI_OK;
 }
 
 int rafiki_preference_loss(const void* logits, int dtype, long long ld_row, int n, int n_classes,
                            const int32_t* labels, const int32_t* offsets, int n_pairs, const float* ref_logp,
-                           float temperature, float beta, float smoothing, int mean, const float* grad_loss,
+                           double temperature, double beta, double smoothing, int mean, const float* grad_loss,
                            float* out_loss, float* out_scores, void* grad_logits, long long ld_grad, void* workspace,
                            long long workspace_bytes, void* stream) {
-  const int rc = check_rows(logits, dtype, ld_row, n, n_classes, labels, temperature, grad_logits, ld_grad);
+  const int rc = check_rows(logits, dtype, ld_row, n, n_classes, labels, temperature, grad_logits, ld_grad, workspace,
+                            workspace_bytes, preference_workspace_bytes);
   if (rc) return rc;
   if (!out_loss && !out_scores && !grad_logits) return invalid("no output is asked for");
-  if (!preference_sizes(n, n_pairs)) return invalid("n_pairs must be in [1, 2^24]");
+  if (n_pairs < 1 || n_pairs > (1 << 24)) return invalid("n_pairs must be in [1, 2^24]");
   if (!offsets && n % (2LL * n_pairs)) return invalid("without offsets n must be a multiple of 2 n_pairs");
-  if (!(beta > 0.f) || !std::isfinite(beta) || !(smoothing >= 0.f && smoothing <= 0.5f))
+  if (!(beta > 0) || !std::isfinite(beta) || !(smoothing >= 0 && smoothing <= 0.5))
     return invalid("beta must be positive and finite, smoothing in [0, 0.5]");
-  if (!workspace || workspace_bytes < preference_bytes(n) || !aligned16(workspace))
-    return invalid("workspace is null, too small or not on a 16-byte boundary");
   PreferenceArgs a = row_args<PreferenceArgs>(logits, ld_row, n, n_classes, labels, temperature, grad_logits, ld_grad);
   a.pairs = n_pairs;
   a.offsets = offsets;

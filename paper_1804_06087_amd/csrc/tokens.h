@@ -69,13 +69,17 @@ struct FcI8Args {
   int* partial;               // [splits][n][c_out] int32 sums (splits > 1)
 };
 
+// log2(e) / T, and what fp32 leaves of it.
+struct Scale {
+  float hi, lo;
+};
 struct TokenLossArgs {
   const void* logits;
   long long ld_row;
   int n, C, row0;             // row0: the launch's first row
   const int32_t* labels;
   double inv_t;               // 1 / T
-  float s;                    // log2(e) / T
+  Scale s;
   bool policy;
   const float* grad_logp;     // token_logp
   const float* grad_entropy;
@@ -83,30 +87,32 @@ struct TokenLossArgs {
   const float* old_logp;
   const float* ref_logp;
   const float* grad_loss;
-  float clip_low, clip_high;
-  float kl_coef, entropy_coef;
+  double clip_low, clip_high, kl_coef, entropy_coef;
   float* loss;
   float* logp;
   float* kl;
   float* entropy;
   void* grad;
   long long ld_grad;
+  int n_parts, per_part;      // parts of a row, chunks of a part
+  void* parts;                // sums of the parts (n_parts > 1)
 };
 
 struct PreferenceRow {        // of the workspace
-  double delta;               // log p - ref
-  float top, share, rest;     // the other classes' maximum, p there, 1 - p of the label
+  float top, share, rest;     // the powers' reference, p there, 1 - p of the label
   float weight;               // dL / d log p over T
 };
 struct PreferenceArgs {
   const void* logits;
   long long ld_row;
-  int n, C, row0, pairs;
+  int n, C, pairs;
+  int pair0, pair1;           // the launch's pairs
   const int32_t* labels;
   const int32_t* offsets;
   const float* ref_logp;
   double inv_t;
-  float s, beta, smoothing;
+  Scale s;
+  double beta, smoothing;
   int mean;
   const float* grad_loss;
   float* loss;
@@ -114,6 +120,8 @@ struct PreferenceArgs {
   void* grad;
   long long ld_grad;
   PreferenceRow* rows;        // [n]
+  int n_parts, per_part;
+  void* parts;                // [n][n_parts]
 };
 
 struct FcMx4Args {
@@ -137,6 +145,8 @@ hipError_t launch_quantize(const void* x, bool bf16, long long ld_x, int n, int 
 hipError_t launch_fc_i8(const FcI8Args& a, hipStream_t s);
 long long fc_i8_workspace_bytes(int n, int c_in, int c_out);
 hipError_t launch_token_loss(const TokenLossArgs& a, bool bf16, hipStream_t s);
+long long token_loss_workspace_bytes(int n, int n_classes);
+long long preference_workspace_bytes(int n, int n_classes);
 hipError_t launch_preference(const PreferenceArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_quantize_mx4(const void* x, bool bf16, long long ld_x, int n, int c, uint8_t* q, long long ld_q,
                                uint8_t* scale, long long ld_scale, hipStream_t s);

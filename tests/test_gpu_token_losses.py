@@ -114,7 +114,6 @@ def run_logp(z, labels, t, a=None, h=None, logp=True, entropy=True, grad=True, *
 
 def check_logp(z, labels, t, a, h, out, dtype):
     zh = host(z)
-    t = float(np.float32(t))
     for i in range(len(labels)):
         y, ai, hi = int(labels[i]), 0.0 if a is None else float(a[i]), 0.0 if h is None else float(h[i])
         token = 0 <= y < zh.shape[1]
@@ -321,7 +320,6 @@ def run_policy(z, labels, A, old=None, ref=None, g=None, t=1.0, low=0.2, high=0.
 
 def check_policy(z, labels, A, old, ref, g, t, low, high, klc, ent, o, dtype):
     zh = host(z)
-    t, klc, ent = (float(np.float32(v)) for v in (t, klc, ent))
     for i in range(len(labels)):
         y = int(labels[i])
         at = lambda v, d=None: d if v is None else float(v[i])  # noqa: E731
@@ -380,8 +378,7 @@ def policy_inputs(rng, z, labels, t, low, high):
 def test_policy(n, C, t, kl, ent, dtype):
     rng = np.random.default_rng(n + C)
     z, labels = lm_rows(rng, n, C, dtype)
-    t32 = float(np.float32(t))
-    A, old, ref, g = policy_inputs(rng, z, labels, t32, 0.2, 0.28)
+    A, old, ref, g = policy_inputs(rng, z, labels, t, 0.2, 0.28)
     z = z.to(DEV)
     g[2] = 0
     A[3] = 0
@@ -463,7 +460,6 @@ def run_preference(z, labels, offsets, ref=None, t=1.0, beta=0.1, smoothing=0.0,
 def check_preference(z, labels, offsets, ref, t, beta, smoothing, mean, g, out, dtype):
     loss, scores, grad = out
     zh = host(z)
-    t, beta, smoothing = (float(np.float32(v)) for v in (t, beta, smoothing))
     want_loss, want_scores, want_grad = ot.preference(zh, labels, offsets, ref, t, beta, smoothing, mean, g)
     C = zh.shape[1]
     for p in range(len(want_loss)):
@@ -570,7 +566,7 @@ def test_preference_bad_offsets_stay_inside():
     loss = full(4)
     labels = torch.zeros(n, dtype=torch.int32, device=DEV)
     for offsets in ([0, 4, 2, 5, 1], [-5, 3, 100, 2 ** 31 - 1, -2 ** 31], [6, 6, 6, 6, 6], [3, 2, 1, 0, -1]):
-        need = bd.preference_workspace(n, 2)
+        need = bd.preference_workspace(n, C)
         ws = full(need + 32, dtype=torch.uint8)
         ws.fill_(9)
         bd.preference_loss(z, labels, loss[1:3], grad, offsets=dev(np.int32(offsets)), workspace=ws[16:16 + need])
@@ -591,7 +587,7 @@ def chain_setup(seed, pairs=2, length=5, c_in=200, C=3001):
              grad=torch.full((n, C), -7.0, device=DEV), pair_loss=full(pairs), scores=full(pairs, 2),
              pair_grad=torch.full((n, C), -7.0, device=DEV))
     b["x"], b["w"], b["ref_w"] = bd.mx4_empty(n, c_in), bd.mx4_empty(C, c_in), bd.mx4_empty(C, c_in)
-    need = (bd.combine_workspace(1, n, C), bd.fc_mx4_workspace(n, c_in + -c_in % 32, C), bd.preference_workspace(n, pairs))
+    need = (bd.combine_workspace(1, n, C), bd.fc_mx4_workspace(n, c_in + -c_in % 32, C), bd.preference_workspace(n, C))
     b["ws"] = [torch.empty(max(k, 16), dtype=torch.uint8, device=DEV) for k in need]
     b["pairs"] = pairs
     return b
@@ -707,7 +703,7 @@ def test_inputs_and_surroundings_are_left_alone():
     A = torch.randn(n, device=DEV)
     bd.policy_loss(z, dev(labels), A, buf[2:-2])
     bd.token_logp(z, dev(labels), buf[2:-2])
-    need = bd.preference_workspace(n, 1)
+    need = bd.preference_workspace(n, C)
     ws = torch.full((need + 32,), 9, dtype=torch.uint8, device=DEV)
     loss = full(3)
     bd.preference_loss(z, dev(labels), loss[1:2], n_pairs=1, workspace=ws[16:16 + need])

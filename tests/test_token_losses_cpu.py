@@ -17,14 +17,15 @@ P = 4096          # a stand-in for a device pointer: never read, every call belo
 
 def _logp(**over):
     a = dict(logits=P, dtype=0, ld_row=10, n=4, C=10, labels=P, t=1.0, g_logp=P, g_entropy=P, logp=P, entropy=P, grad=P,
-             ld_grad=10, stream=None)
+             ld_grad=10, ws=P, ws_bytes=1 << 20, stream=None)
     a.update(over)
     return pkg.load_library().rafiki_token_logp(*a.values())
 
 
 def _policy(**over):
     a = dict(logits=P, dtype=0, ld_row=10, n=4, C=10, labels=P, advantage=P, old=P, ref=P, t=1.0, low=0.2, high=0.2,
-             kl=0.1, ent=0.0, g=None, loss=P, logp=P, out_kl=P, entropy=P, grad=P, ld_grad=10, stream=None)
+             kl=0.1, ent=0.0, g=None, loss=P, logp=P, out_kl=P, entropy=P, grad=P, ld_grad=10, ws=P,
+             ws_bytes=1 << 20, stream=None)
     a.update(over)
     return pkg.load_library().rafiki_policy_loss(*a.values())
 
@@ -56,6 +57,8 @@ ROWS = ({"logits": None}, {"labels": None}, {"dtype": 2}, {"dtype": -1}, {"n": 0
 
 @pytest.mark.parametrize("call,over", [
     *[(c, o) for c in (_logp, _policy, _preference) for o in ROWS],
+    *[(c, {"C": 1 << 20, "ld_grad": 1 << 20, **o}) for c in (_logp, _policy)
+      for o in ({"ws": None}, {"ws": P + 8}, {"ws_bytes": 15})],          # few rows that are long
     *[(_logp, o) for o in ({"logp": None, "entropy": None, "grad": None}, {"g_logp": None, "g_entropy": None})],
     *[(_policy, o) for o in ({"advantage": None}, {"loss": None, "logp": None, "out_kl": None, "entropy": None, "grad": None},
                              {"low": -0.1}, {"low": 1.1}, {"low": math.nan}, {"high": -0.1}, {"high": math.nan},
@@ -79,10 +82,12 @@ def test_refusals(call, over):
 
 def test_workspace_sizes():
     lib, b = pkg.load_library(), C.c_longlong(-1)
-    assert lib.rafiki_preference_workspace(1, 1, None) == INVALID
-    for bad in ((0, 1), (1, 0), (1, (1 << 24) + 1)):
-        assert lib.rafiki_preference_workspace(*bad, C.byref(b)) == INVALID
+    for f in (lib.rafiki_preference_workspace, lib.rafiki_token_workspace):
+        assert f(1, 1, None) == INVALID
+        for bad in ((0, 1), (1, 0), (1, (1 << 20) + 1)):
+            assert f(*bad, C.byref(b)) == INVALID
     assert bd.preference_workspace(1 << 30, 1) > 1 << 32                 # 64-bit size
+    assert bd.token_workspace(1 << 30, 1 << 20) >= 0
     assert lib.rafiki_fc_mx4_workspace(1, 32, 1, None) == INVALID
     for bad in ((0, 32, 1), (1, 0, 1), (1, 32, 0), (1, 48, 1), (1, (1 << 20) + 32, 1)):
         assert lib.rafiki_fc_mx4_workspace(*bad, C.byref(b)) == INVALID

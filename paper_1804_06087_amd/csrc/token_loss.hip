@@ -9,6 +9,7 @@
 #include "tokens.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace rafiki {
 
@@ -57,15 +58,17 @@ __device__ __forceinline__ u32x4 pack(const float z[V]) {
   return q;
 }
 
+// Over W neighbouring lanes.
+template <int W = 64>
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  for (int o = W / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
   return v;
 }
-template <typename T>
+template <int W = 64, typename T>
 __device__ __forceinline__ T wave_add(T v) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  for (int o = W / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
   return v;
 }
 
@@ -153,17 +156,33 @@ struct Row {
   }
 };
 
-// Sums over classes, the label's apart: 2^x with x = (z - top) s, and of those times x.
+// Sums over classes, the label's apart: 2^x with x = (z - top) s, and of those times x.  A thread adds a chunk's in 32 bits and
+// the chunks in 64: unlikely classes by the thousand, each below the last bit of a likely one's sum, would be lost in 32
+// (log p of 131071 classes off by 1.4e-6 on average; the additions cost nothing that the loads do not hide).
 struct Sums {
-  float top, sum, moment;
+  double sum, moment;
+  float top;
 };
-// x = d s of a difference d of logits, and the power; PRECISE: s in two parts, and what is rounded off x into `lost`, whose
-// sum times ln 2 belongs to the sum of powers.
-template <bool PRECISE>
-__device__ __forceinline__ float term(float d, const Scale& s, float& x, float& lost) {
+template <int V>
+__device__ __forceinline__ float tree_sum(const float v[V]) {
+  if constexpr (V == 8) return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+  else return (v[0] + v[1]) + (v[2] + v[3]);
+}
+// The power of x = (z - ref) s; PRECISE: what is rounded off x, by s, the product and the difference (of fp32 values), into
+// `lost`, whose sum times ln 2 belongs to the sum of powers.
+template <bool PRECISE, bool EXACT_DIFFERENCE>
+__device__ __forceinline__ float term(float z, float ref, const Scale& s, float& x, float& lost) {
+  const float d = z - ref;
   x = d * s.hi;
   const float e = power2(x);
-  if constexpr (PRECISE) lost = fmaf(e, fminf(fmaf(d, s.lo, fmaf(d, s.hi, -x)), 1.f), lost);   // NaN where d = -inf and e = 0: 1
+  if constexpr (PRECISE) {
+    float off = fmaf(d, s.lo, fmaf(d, s.hi, -x));
+    if constexpr (!EXACT_DIFFERENCE) {
+      const float back = d - z;
+      off = fmaf((z - (d - back)) - (ref + back), s.hi, off);
+    }
+    lost = fmaf(e, fminf(off, 1.f), lost);                   // NaN where d = -inf and e = 0: 1
+  }
   return e;
 }
 // Relative to the label's logit, which needs no maximum: sums stay below 2^127 as long as p_l is above 2^-127, and what underflows
@@ -171,17 +190,28 @@ __device__ __forceinline__ float term(float d, const Scale& s, float& x, float& 
 // add_chunk_any.
 template <int V, bool ENT, bool PRECISE>
 __device__ __forceinline__ void add_chunk(Sums& a, float& lost, const float z[V], float ref, const Scale& s) {
+  float e[V], m = 0.f;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     float x;
-    const float e = term<PRECISE>(z[j] - ref, s, x, lost);
-    a.sum += e;
-    if constexpr (ENT) a.moment = fmaf(e, finite_log2(x), a.moment);
+    e[j] = term<PRECISE, V == 8>(z[j], ref, s, x, lost);
+    if constexpr (ENT) m = fmaf(e[j], finite_log2(x), m);
   }
+  a.sum += (double)tree_sum<V>(e);
+  if constexpr (ENT) a.moment += (double)m;
 }
 template <bool ENT>
 __device__ __forceinline__ bool bounded(const Sums& a) {
-  return a.sum < INFINITY && (!ENT || fabsf(a.moment) < INFINITY);
+  return a.sum < 0x1p126 && (!ENT || fabs(a.moment) < 0x1p126);
+}
+// The same sums relative to `ref`.
+template <bool ENT>
+__device__ __forceinline__ Sums moved(Sums v, float ref, float s) {
+  const float step = (v.top - ref) * s;
+  const double grown = v.sum == 0.0 ? 0.0 : (double)power2(step);
+  if (ENT) v.moment = (v.moment + v.sum * (double)finite_log2(step)) * grown;
+  v.sum *= grown;
+  return v;
 }
 // For any values: relative to the largest so far.
 template <int V, bool ENT>
@@ -189,36 +219,30 @@ __device__ __forceinline__ void add_chunk_any(Sums& a, const float z[V], float s
   float now = a.top;
 #pragma unroll
   for (int j = 0; j < V; ++j) now = fmaxf(now, z[j]);
-  const float ref = reference(now), step = (a.top - ref) * s, grown = power2(step);
-  if constexpr (ENT) a.moment = (a.moment + a.sum * finite_log2(step)) * grown;
-  a.sum *= grown;
+  a = moved<ENT>(a, reference(now), s);
+  float e[V], m = 0.f;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const float x = (z[j] - ref) * s, e = power2(x);
-    a.sum += e;
-    if constexpr (ENT) a.moment += e * finite_log2(x);
+    const float x = (z[j] - reference(now)) * s;
+    e[j] = power2(x);
+    if constexpr (ENT) m = fmaf(e[j], finite_log2(x), m);
   }
+  a.sum += (double)tree_sum<V>(e);
+  if constexpr (ENT) a.moment += (double)m;
   a.top = now;
 }
-// The same sums relative to `ref`.
-template <bool ENT>
-__device__ __forceinline__ Sums moved(Sums v, float ref, float s) {
-  const float step = (v.top - ref) * s, grown = v.sum == 0.f ? 0.f : power2(step);
-  if (ENT) v.moment = (v.moment + v.sum * finite_log2(step)) * grown;
-  v.sum *= grown;
-  return v;
-}
-// The sums of NW waves' threads in every thread; a barrier if NW > 1, and before `waves` is used again.  With ANY the threads'
+// The sums of NT threads in each of them; a barrier if NT > 64, and before `waves` is used again.  With ANY the threads'
 // references differ.
-template <int NW, bool ENT, bool ANY>
-__device__ __forceinline__ Sums join(Sums a, float s, Sums (&waves)[NW]) {
+template <int NT, bool ENT, bool ANY>
+__device__ __forceinline__ Sums join(Sums a, float s, Sums* waves) {
+  constexpr int NW = NT / 64, W = NT < 64 ? NT : 64;
   if constexpr (ANY) {
-    const float all = wave_max(a.top);
+    const float all = wave_max<W>(a.top);
     a = moved<ENT>(a, reference(all), s);
     a.top = all;
   }
-  a.sum = wave_add(a.sum);
-  if (ENT) a.moment = wave_add(a.moment);
+  a.sum = wave_add<W>(a.sum);
+  if (ENT) a.moment = wave_add<W>(a.moment);
   if constexpr (NW > 1) {
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = a;
     __syncthreads();
@@ -227,7 +251,7 @@ __device__ __forceinline__ Sums join(Sums a, float s, Sums (&waves)[NW]) {
 #pragma unroll
       for (int w = 0; w < NW; ++w) top = fmaxf(top, waves[w].top);
     }
-    Sums r{top, 0.f, 0.f};
+    Sums r{0.0, 0.0, top};
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
       const Sums v = ANY ? moved<ENT>(waves[w], reference(top), s) : waves[w];
@@ -252,20 +276,21 @@ __device__ __forceinline__ RowFacts row_facts(const Sums& r, float z, float s, d
   RowFacts f;
   const float top = reference(r.top), t = reference(fmaxf(r.top, z));
   const float down = finite_log2((top - t) * s), x = finite_log2((z - t) * s);
-  const float e_r = r.sum == 0.f ? 0.f : power2(down), e_y = power2((z - t) * s);
-  const float part = r.sum * e_r, total = part + e_y;
-  f.defined = total > 0.f && total < INFINITY && t < INFINITY;
-  f.rest = part / total;
-  f.p = e_y / total;
-  f.share = e_r / total;
-  const float log2_total = log2f(total);
-  f.log2_share = down - log2_total;
-  f.entropy = ENT ? kLn2 * (log2_total - ((r.moment + r.sum * down) * e_r + e_y * x) / total) : 0.f;
+  const double e_r = r.sum == 0.0 ? 0.0 : (double)power2(down), e_y = (double)power2((z - t) * s);
+  const double part = r.sum * e_r, total = part + e_y;
+  f.defined = total > 0.0 && total < INFINITY && t < INFINITY;
+  const double inv = 1.0 / total;
+  f.rest = (float)(part * inv);
+  f.p = (float)(e_y * inv);
+  f.share = (float)(e_r * inv);
+  const double ln_total = log(total);
+  f.log2_share = down - (float)(ln_total * 1.4426950408889634);
+  f.entropy = ENT ? (float)(ln_total - 0.6931471805599453 * ((r.moment + r.sum * (double)down) * e_r + e_y * (double)x) * inv) : 0.f;
   // log p in 64 bits: the difference of two logits may exceed fp32, and what follows subtracts it
   const double D = ((double)z - (double)top) * inv_t;
-  if (r.sum == 0.f) f.logp = 0.0;
-  else if (D >= 0) f.logp = -log1p((double)r.sum * (D > 0 ? (double)expf((float)-D) : 1.0));
-  else f.logp = D - log((double)r.sum + (double)expf((float)D));
+  if (r.sum == 0.0) f.logp = 0.0;
+  else if (D >= 0) f.logp = -log1p(r.sum * (D > 0 ? exp(-D) : 1.0));
+  else f.logp = D - log(r.sum + exp(D));
   if (!f.defined) {
     f.logp = NAN;
     f.entropy = NAN;
@@ -340,16 +365,17 @@ __device__ __forceinline__ u32x4 masked_chunk() {
   return u32x4{m, m, m, m};
 }
 
-// f(a chunk's values) for the chunks first + tid, + NT, .. below `last` of a row that is read for it, UN in flight.
-template <bool BF16, bool STREAM, int NT, typename F>
+// f(a chunk's values) for the chunks first, first + NT, .. below `last` of a row that is read for it, UN in flight (LAST: for the
+// last time, one chunk after another).
+template <bool BF16, bool LAST, int UN, int NT, typename F>
 __device__ __forceinline__ void for_chunks(const Row<BF16>& r, int first, int last, F&& f) {
-  constexpr int V = Row<BF16>::V, UN = 4;
+  constexpr int V = Row<BF16>::V;
   for (int i0 = first; i0 < last; i0 += NT * UN) {
     u32x4 q[UN];
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
       q[u] = masked_chunk<BF16>();
-      if (i0 + u * NT < last) q[u] = r.template load<STREAM>(i0 + u * NT);
+      if (i0 + u * NT < last) q[u] = r.template load<LAST>(i0 + u * NT);
     }
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
@@ -388,12 +414,12 @@ __device__ __forceinline__ void no_token(const TokenLossArgs& a, int row) {
   if (a.entropy) a.entropy[row] = 0.f;
 }
 
-// NT threads per row, G rows a workgroup (G > 1: a wave each).  CH > 0: the row, of at most NT CH chunks, stays in registers
+// NT threads per row, G rows a workgroup (G > 1: up to a wave each).  CH > 0: the row, of at most NT CH chunks, stays in registers
 // from its sums to its gradient, so that it is read once; CH = 0: any length, read again for the gradient.
-template <bool BF16, bool POLICY, bool ENT, int NT, int CH, int G>
+template <bool BF16, bool POLICY, bool ENT, int NT, int CH, int G, bool REST>
 __global__ __launch_bounds__(NT * G) void token_loss_kernel(TokenLossArgs a) {
-  constexpr int V = Row<BF16>::V, NW = NT / 64;
-  static_assert(G == 1 || NT == 64, "rows that share a workgroup have no barrier");
+  constexpr int V = Row<BF16>::V, NW = (NT + 63) / 64;
+  static_assert(G == 1 || NT <= 64, "rows that share a workgroup have no barrier");
   __shared__ Sums waves[NW];
   __shared__ RowGrad shared_grad;
   const int row = a.row0 + blockIdx.x * G + (G > 1 ? threadIdx.x / NT : 0), tid = threadIdx.x % NT;
@@ -418,7 +444,7 @@ __global__ __launch_bounds__(NT * G) void token_loss_kernel(TokenLossArgs a) {
     }
   }
   const float z_label = element<BF16>(r.x, r.label);
-  auto each = [&](auto&& f) {
+  auto each = [&](auto last, auto&& f) {
     if constexpr (CH > 0) {
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
@@ -429,19 +455,18 @@ __global__ __launch_bounds__(NT * G) void token_loss_kernel(TokenLossArgs a) {
         f(z, i * NT + tid);
         __builtin_amdgcn_sched_barrier(0);                   // one chunk's values at a time in registers
       }
-    } else {
-      for_chunks<BF16, false, NT>(r, tid, r.chunks, f);
     }
+    if constexpr (REST) for_chunks<BF16, decltype(last)::value, (decltype(last)::value && CH != 0 ? 1 : 4), NT>(r, NT * CH + tid, r.chunks, f);
   };
-  Sums sums{z_label, 0.f, 0.f};
+  Sums sums{0.0, 0.0, z_label};
   float lost = 0.f;
-  each([&](const float* z, int) { add_chunk<V, ENT, false>(sums, lost, z, z_label, a.s); });
-  sums = join<NW, ENT, false>(sums, a.s.hi, waves);
+  each(std::false_type{}, [&](const float* z, int) { add_chunk<V, ENT, false>(sums, lost, z, z_label, a.s); });
+  sums = join<NT, ENT, false>(sums, a.s.hi, waves);
   if (!bounded<ENT>(sums)) {                                 // the same in all of the row's threads
     if constexpr (NW > 1) __syncthreads();
-    sums = Sums{-INFINITY, 0.f, 0.f};
-    each([&](const float* z, int) { add_chunk_any<V, ENT>(sums, z, a.s.hi); });
-    sums = join<NW, ENT, true>(sums, a.s.hi, waves);
+    sums = Sums{0.0, 0.0, -INFINITY};
+    each(std::false_type{}, [&](const float* z, int) { add_chunk_any<V, ENT>(sums, z, a.s.hi); });
+    sums = join<NT, ENT, true>(sums, a.s.hi, waves);
   }
   RowGrad d{};
   if (NW == 1 || threadIdx.x < 64) {
@@ -454,48 +479,52 @@ __global__ __launch_bounds__(NT * G) void token_loss_kernel(TokenLossArgs a) {
     d = shared_grad;
   }
   const float top = reference(sums.top);
-  each([&](float* z, int i) {
+  each(std::true_type{}, [&](float* z, int i) {
     if (i < r.chunks) store_gradient<BF16, ENT>(r, d_row, i, z, top, a.s.hi, d);
   });
 }
 
 // ---------------------------------------------------------------- rows in parts
 
-// The sums of part p of row i into parts[i][p]: chunks p per .. + per - 1.
+// The sums over a row's chunks first, first + NT, .. below `last`, joined over NT threads.
+template <bool BF16, bool ENT, bool PRECISE, int NT>
+__device__ __forceinline__ Sums row_sums(const Row<BF16>& r, int first, int last, float z_label, const Scale& s, Sums* waves) {
+  constexpr int V = Row<BF16>::V;
+  Sums sums{0.0, 0.0, z_label};
+  float lost = 0.f;
+  for_chunks<BF16, false, 4, NT>(r, first, last, [&](const float* z, int) { add_chunk<V, ENT, PRECISE>(sums, lost, z, z_label, s); });
+  if (PRECISE) sums.sum += (double)(kLn2 * lost);
+  sums = join<NT, ENT, false>(sums, s.hi, waves);
+  if (!bounded<ENT>(sums)) {
+    if (NT > 64) __syncthreads();
+    sums = Sums{0.0, 0.0, -INFINITY};
+    for_chunks<BF16, false, 4, NT>(r, first, last, [&](const float* z, int) { add_chunk_any<V, ENT>(sums, z, s.hi); });
+    sums = join<NT, ENT, true>(sums, s.hi, waves);
+  }
+  return sums;
+}
+// The sums of a row's part p, chunks p per .. + per - 1, into *out.
 template <bool BF16, bool ENT, bool PRECISE, int NT>
 __device__ __forceinline__ void part_sums(const Row<BF16>& r, int p, int per, const Scale& s, Sums* out) {
-  constexpr int V = Row<BF16>::V, NW = NT / 64;
-  __shared__ Sums waves[NW];
-  const int first = p * per + threadIdx.x, last = min(r.chunks, (p + 1) * per);
-  const float z_label = element<BF16>(r.x, r.label);
-  Sums sums{z_label, 0.f, 0.f};
-  float lost = 0.f;
-  for_chunks<BF16, false, NT>(r, first, last, [&](const float* z, int) { add_chunk<V, ENT, PRECISE>(sums, lost, z, z_label, s); });
-  if (PRECISE) sums.sum += kLn2 * lost;
-  sums = join<NW, ENT, false>(sums, s.hi, waves);
-  if (!bounded<ENT>(sums)) {
-    __syncthreads();
-    sums = Sums{-INFINITY, 0.f, 0.f};
-    for_chunks<BF16, false, NT>(r, first, last, [&](const float* z, int) { add_chunk_any<V, ENT>(sums, z, s.hi); });
-    sums = join<NW, ENT, true>(sums, s.hi, waves);
-  }
+  __shared__ Sums waves[NT / 64];
+  const Sums sums = row_sums<BF16, ENT, PRECISE, NT>(r, p * per + threadIdx.x, min(r.chunks, (p + 1) * per),
+                                                     element<BF16>(r.x, r.label), s, waves);
   if (threadIdx.x == 0) *out = sums;
 }
 // A row's sums from its parts', in every lane of a wave.
 template <bool ENT>
 __device__ __forceinline__ Sums join_parts(const Sums* parts, int n, float s) {
   const int lane = threadIdx.x & 63;
-  Sums a{-INFINITY, 0.f, 0.f};
+  Sums a{0.0, 0.0, -INFINITY};
   for (int p = lane; p < n; p += 64) {
     Sums b = parts[p];
     const float top = fmaxf(a.top, b.top);
     const float ref = reference(top);
     a = moved<ENT>(a, ref, s);
     b = moved<ENT>(b, ref, s);
-    a = Sums{top, a.sum + b.sum, a.moment + b.moment};
+    a = Sums{a.sum + b.sum, a.moment + b.moment, top};
   }
-  Sums none[1];
-  return join<1, ENT, true>(a, s, none);
+  return join<64, ENT, true>(a, s, nullptr);
 }
 
 template <bool BF16, bool POLICY, bool ENT, int NT>
@@ -542,7 +571,7 @@ __global__ __launch_bounds__(NT) void token_parts_grad_kernel(TokenLossArgs a) {
   __syncthreads();
   const RowGrad d = shared_grad;
   const float top = shared_top;
-  for_chunks<BF16, true, NT>(r, first, last, [&](float* z, int i) {
+  for_chunks<BF16, true, 1, NT>(r, first, last, [&](float* z, int i) {
     if (i < last) store_gradient<BF16, ENT>(r, d_row, i, z, top, a.s.hi, d);
   });
 }
@@ -555,11 +584,11 @@ __device__ __forceinline__ int offset_at(const PreferenceArgs& a, int i) {
   return (int)(at < 0 ? 0 : at > a.n ? a.n : at);
 }
 
-// The sums of the rows of pairs pair0 .. pair1 - 1, a workgroup a part of a row in turn.
+// The sums of all rows, a workgroup a part of a row in turn.
 template <bool BF16, int NT>
-__global__ __launch_bounds__(NT) void preference_sums_kernel(PreferenceArgs a) {
-  const int end = offset_at(a, 2 * a.pair1);
-  for (int row = offset_at(a, 2 * a.pair0) + blockIdx.y; row < end; row += gridDim.y) {
+__global__ __launch_bounds__(NT, 6) void preference_sums_kernel(PreferenceArgs a) {
+  const int end = offset_at(a, 2 * a.pairs);
+  for (int row = offset_at(a, 0) + blockIdx.y; row < end; row += gridDim.y) {
     const int label = a.labels[row];
     if ((unsigned)label >= (unsigned)a.C) continue;
     Row<BF16> r;
@@ -569,13 +598,41 @@ __global__ __launch_bounds__(NT) void preference_sums_kernel(PreferenceArgs a) {
   }
 }
 
+// A pair's outputs (where `writes`) and its answers' weights, dL / d log p of a token over T, from its sums of log p - ref.
+__device__ __forceinline__ void finish_pair(const PreferenceArgs& a, int p, const double total[2], const int count[2],
+                                            bool writes, float weight[2]) {
+  double score[2], per[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    per[k] = a.mean && count[k] ? 1.0 / count[k] : 1.0;
+    score[k] = a.beta * (total[k] * per[k]);
+  }
+  const double u = score[0] - score[1], smooth = a.smoothing;
+  const double e = exp(-fabs(u)), big = 1 / (1 + e), small = e / (1 + e);
+  const double up = u > 0 ? big : small, down = u > 0 ? small : big;   // sigmoid(u), sigmoid(-u)
+  if (writes) {
+    const double soft = log1p(e);
+    double loss = (1 - smooth) * (soft + (u < 0 ? -u : 0.0));
+    if (smooth > 0) loss += smooth * (soft + (u > 0 ? u : 0.0));
+    if (a.loss) a.loss[p] = u == u ? (float)loss : NAN;
+    if (a.scores) {
+      a.scores[2 * p] = (float)score[0];
+      a.scores[2 * p + 1] = (float)score[1];
+    }
+  }
+  const double g = a.grad_loss ? (double)a.grad_loss[p] : 1.0;
+  const double du = g == 0 ? 0.0 : u == u ? a.beta * g * (smooth * up - (1 - smooth) * down) : NAN;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) weight[k] = (float)((k ? -du : du) * per[k] * a.inv_t);
+}
+
 // One workgroup per pair: its rows' log p from their sums, its answers' sums in 64 bits (a thread's rows in their order, then
 // a tree, the same every time), the loss, and every row's weight.
 template <bool BF16>
 __global__ __launch_bounds__(256) void preference_pairs_kernel(PreferenceArgs a) {
   __shared__ double sums[2][4];
   __shared__ int counts[2][4];
-  const int p = a.pair0 + blockIdx.x, tid = threadIdx.x;
+  const int p = blockIdx.x, tid = threadIdx.x;
   int at[3];
 #pragma unroll
   for (int k = 0; k < 3; ++k) at[k] = offset_at(a, 2 * p + k);
@@ -588,13 +645,13 @@ __global__ __launch_bounds__(256) void preference_pairs_kernel(PreferenceArgs a)
       const int label = a.labels[row];
       if ((unsigned)label >= (unsigned)a.C) continue;
       const Sums* parts = (const Sums*)a.parts + (long long)row * a.n_parts;
-      Sums all{-INFINITY, 0.f, 0.f};
+      Sums all{0.0, 0.0, -INFINITY};
       for (int q = 0; q < a.n_parts; ++q) {
         Sums b = parts[q];
         const float top = fmaxf(all.top, b.top), ref = reference(top);
         all = moved<false>(all, ref, a.s.hi);
         b = moved<false>(b, ref, a.s.hi);
-        all = Sums{top, all.sum + b.sum, 0.f};
+        all = Sums{all.sum + b.sum, 0.0, top};
       }
       const float z = element<BF16>((const char*)a.logits + row * a.ld_row * (BF16 ? 2 : 4), label);
       const RowFacts f = row_facts<false>(all, z, a.s.hi, a.inv_t);
@@ -613,42 +670,84 @@ __global__ __launch_bounds__(256) void preference_pairs_kernel(PreferenceArgs a)
     }
   }
   __syncthreads();
-  double score[2], per[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int count = counts[k][0] + counts[k][1] + counts[k][2] + counts[k][3];
-    per[k] = a.mean && count ? 1.0 / count : 1.0;
-    score[k] = a.beta * ((sums[k][0] + sums[k][1] + sums[k][2] + sums[k][3]) * per[k]);
-  }
-  const double u = score[0] - score[1], smooth = a.smoothing;
-  const double e = exp(-fabs(u)), big = 1 / (1 + e), small = e / (1 + e);
-  const double up = u > 0 ? big : small, down = u > 0 ? small : big;   // sigmoid(u), sigmoid(-u)
-  if (tid == 0) {
-    const double soft = log1p(e);
-    double loss = (1 - smooth) * (soft + (u < 0 ? -u : 0.0));
-    if (smooth > 0) loss += smooth * (soft + (u > 0 ? u : 0.0));
-    if (a.loss) a.loss[p] = u == u ? (float)loss : NAN;
-    if (a.scores) {
-      a.scores[2 * p] = (float)score[0];
-      a.scores[2 * p + 1] = (float)score[1];
-    }
-  }
+  float weight[2];
+  const double total[2] = {sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3], sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3]};
+  const int count[2] = {counts[0][0] + counts[0][1] + counts[0][2] + counts[0][3],
+                        counts[1][0] + counts[1][1] + counts[1][2] + counts[1][3]};
+  finish_pair(a, p, total, count, tid == 0, weight);
   if (!a.grad) return;
-  const double g = a.grad_loss ? (double)a.grad_loss[p] : 1.0;
-  const double du = g == 0 ? 0.0 : u == u ? a.beta * g * (smooth * up - (1 - smooth) * down) : NAN;
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const float weight = (float)((k ? -du : du) * per[k] * a.inv_t);
-    for (int row = at[k] + tid; row < at[k + 1]; row += 256) a.rows[row].weight = token(row) ? weight : 0.f;
+  for (int k = 0; k < 2; ++k)
+    for (int row = at[k] + tid; row < at[k + 1]; row += 256) a.rows[row].weight = token(row) ? weight[k] : 0.f;
+}
+
+// Small problems in one launch: a workgroup per pair, a wave a row in turn, whose logits it reads again for the gradient.
+template <bool BF16>
+__global__ __launch_bounds__(1024) void preference_few_kernel(PreferenceArgs a) {
+  constexpr int V = Row<BF16>::V, NW = 16;
+  __shared__ double sums[2][NW];
+  __shared__ int counts[2][NW];
+  const int p = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int begin = offset_at(a, 2 * p), middle = offset_at(a, 2 * p + 1), end = offset_at(a, 2 * p + 2);
+  double sum[2] = {0.0, 0.0};
+  int tokens[2] = {0, 0};
+  for (int row = begin + wave; row < end; row += NW) {
+    Row<BF16> r;
+    r.init(a.logits, row * a.ld_row, a.C, a.labels[row]);
+    if ((unsigned)r.label >= (unsigned)a.C) continue;
+    const float z_label = element<BF16>(r.x, r.label);
+    const Sums all = row_sums<BF16, false, true, 64>(r, lane, r.chunks, z_label, a.s, nullptr);
+    const RowFacts f = row_facts<false>(all, z_label, a.s.hi, a.inv_t);
+    if (lane == 0) {
+      PreferenceRow& out = a.rows[row];
+      out.top = reference(all.top);
+      out.share = f.defined ? f.share : NAN;
+      out.rest = f.defined ? f.rest : NAN;
+    }
+    const double delta = f.logp - (a.ref_logp ? (double)a.ref_logp[row] : 0.0);
+    if (row < middle) sum[0] += delta, ++tokens[0];
+    else sum[1] += delta, ++tokens[1];
+  }
+  if (lane < 2) {
+    sums[lane][wave] = lane ? sum[1] : sum[0];
+    counts[lane][wave] = lane ? tokens[1] : tokens[0];
+  }
+  __syncthreads();
+  double total[2] = {0.0, 0.0};
+  int count[2] = {0, 0};
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      total[k] += sums[k][w];
+      count[k] += counts[k][w];
+    }
+  float weight[2];
+  finish_pair(a, p, total, count, threadIdx.x == 0, weight);
+  if (!a.grad) return;
+  __threadfence_block();                                     // the wave's own rows' facts
+  for (int row = begin + wave; row < end; row += NW) {
+    Row<BF16> r;
+    r.init(a.logits, row * a.ld_row, a.C, a.labels[row]);
+    char* const d_row = (char*)a.grad + row * a.ld_grad * (16 / V);
+    const float w = row < middle ? weight[0] : weight[1];
+    if ((unsigned)r.label >= (unsigned)a.C || w == 0.f) {
+      r.template zero<64>(d_row, lane);
+      continue;
+    }
+    const PreferenceRow f = a.rows[row];
+    const RowGrad d{-w * f.share, 0.f, w * f.rest};
+    for_chunks<BF16, true, 1, 64>(r, lane, r.chunks, [&](float* z, int i) {
+      if (i < r.chunks) store_gradient<BF16, false>(r, d_row, i, z, f.top, a.s.hi, d);
+    });
   }
 }
 
 template <bool BF16, int NT>
 __global__ __launch_bounds__(NT) void preference_grad_kernel(PreferenceArgs a) {
   constexpr int V = Row<BF16>::V;
-  const int begin = offset_at(a, 2 * a.pair0), end = offset_at(a, 2 * a.pair1);
-  for (int k = blockIdx.y; k < end - begin; k += gridDim.y) {
-    const int row = end - 1 - k;                             // the last rows read are the likeliest to lie in a cache
+  const int end = offset_at(a, 2 * a.pairs);
+  for (int row = offset_at(a, 0) + blockIdx.y; row < end; row += gridDim.y) {
     const PreferenceRow f = a.rows[row];
     Row<BF16> r;
     r.init(a.logits, row * a.ld_row, a.C, a.labels[row]);
@@ -659,7 +758,7 @@ __global__ __launch_bounds__(NT) void preference_grad_kernel(PreferenceArgs a) {
       continue;
     }
     const RowGrad d{-f.weight * f.share, 0.f, f.weight * f.rest};
-    for_chunks<BF16, true, NT>(r, first, last, [&](float* z, int i) {
+    for_chunks<BF16, true, 1, NT>(r, first, last, [&](float* z, int i) {
       if (i < last) store_gradient<BF16, false>(r, d_row, i, z, f.top, a.s.hi, d);
     });
   }
@@ -667,14 +766,15 @@ __global__ __launch_bounds__(NT) void preference_grad_kernel(PreferenceArgs a) {
 
 // Workgroups of a launch's second axis, and rows that it takes at most.
 constexpr int kGridRows = 1 << 15;
+constexpr long long kFewBytes = 4 << 20;
 
-template <bool BF16, bool POLICY, bool ENT, int NT, int CH, int G>
+template <bool BF16, bool POLICY, bool ENT, int NT, int CH, int G, bool REST>
 hipError_t launch_loss_rows(const TokenLossArgs& args, hipStream_t s) {
   TokenLossArgs a = args;
   for (long long row = 0; row < args.n; row += (1 << 20) * G) {   // 2^20 workgroups a launch at most
     a.row0 = (int)row;
     const long long rows = std::min<long long>(args.n - row, (1 << 20) * G);
-    launch(token_loss_kernel<BF16, POLICY, ENT, NT, CH, G>, dim3((unsigned)((rows + G - 1) / G)), dim3(NT * G), s, a);
+    launch(token_loss_kernel<BF16, POLICY, ENT, NT, CH, G, REST>, dim3((unsigned)((rows + G - 1) / G)), dim3(NT * G), s, a);
     const hipError_t st = hipGetLastError();
     if (st != hipSuccess) return st;
   }
@@ -704,10 +804,14 @@ hipError_t launch_loss_by_length(const TokenLossArgs& args, hipStream_t s) {
   a.n_parts = parts_of(a.n, chunks);
   a.per_part = (chunks + a.n_parts - 1) / a.n_parts;
   if (a.n_parts > 1) return launch_loss_parts<BF16, POLICY, ENT>(a, s);
-  if (chunks <= 64 * 4) return launch_loss_rows<BF16, POLICY, ENT, 64, 4, 4>(a, s);
-  if (chunks <= 128 * 8) return launch_loss_rows<BF16, POLICY, ENT, 128, 8, 1>(a, s);
-  if (chunks <= 256 * 8) return launch_loss_rows<BF16, POLICY, ENT, 256, 8, 1>(a, s);
-  return launch_loss_rows<BF16, POLICY, ENT, 512, 0, 1>(a, s);
+  if (chunks <= 8 * 4) return launch_loss_rows<BF16, POLICY, ENT, 8, 4, 32, false>(a, s);
+  if (chunks <= 16 * 4) return launch_loss_rows<BF16, POLICY, ENT, 16, 4, 16, false>(a, s);
+  if (chunks <= 32 * 8) return launch_loss_rows<BF16, POLICY, ENT, 32, 8, 8, false>(a, s);
+  if (chunks <= 128 * 8) return launch_loss_rows<BF16, POLICY, ENT, 128, 8, 1, false>(a, s);
+  if (!a.grad) return launch_loss_rows<BF16, POLICY, ENT, 512, 0, 1, true>(a, s);
+  if (chunks <= 256 * 8) return launch_loss_rows<BF16, POLICY, ENT, 256, 8, 1, false>(a, s);
+  if (chunks <= 512 * 8) return launch_loss_rows<BF16, POLICY, ENT, 512, 4, 1, true>(a, s);
+  return launch_loss_rows<BF16, POLICY, ENT, 512, 8, 1, true>(a, s);
 }
 
 template <bool BF16>
@@ -723,16 +827,19 @@ hipError_t launch_preference_of(const PreferenceArgs& args, hipStream_t s) {
   const int chunks = (a.C + Row<BF16>::V - 1) / Row<BF16>::V;
   a.n_parts = parts_of(a.n, chunks);
   a.per_part = (chunks + a.n_parts - 1) / a.n_parts;
-  const dim3 grid(a.n_parts, std::min(a.n, kGridRows));
-  a.pair0 = 0;
-  a.pair1 = a.pairs;
-  launch(preference_sums_kernel<BF16, 256>, grid, dim3(256), s, a);
+  const long long turns = (a.n / a.pairs + 15) / 16;         // rows of a wave, as answers go on average
+  if (turns * (256 + chunks) <= 1024 && a.n * (chunks * 16LL) <= kFewBytes) {
+    launch(preference_few_kernel<BF16>, dim3(a.pairs), dim3(1024), s, a);
+    return hipGetLastError();
+  }
+  const unsigned rows = std::min(a.n, kGridRows);
+  launch(preference_sums_kernel<BF16, 256>, dim3(a.n_parts, rows), dim3(256), s, a);
   hipError_t st = hipGetLastError();
   if (st != hipSuccess) return st;
-  launch(preference_pairs_kernel<BF16>, dim3(a.pair1 - a.pair0), dim3(256), s, a);
+  launch(preference_pairs_kernel<BF16>, dim3(a.pairs), dim3(256), s, a);
   st = hipGetLastError();
   if (st != hipSuccess || !a.grad) return st;
-  launch(preference_grad_kernel<BF16, 256>, grid, dim3(256), s, a);
+  launch(preference_grad_kernel<BF16, 512>, dim3(a.n_parts, rows), dim3(512), s, a);
   return hipGetLastError();
 }
 

@@ -106,7 +106,6 @@ struct PreferenceArgs {
   const void* logits;
   long long ld_row;
   int n, C, pairs;
-  int pair0, pair1;           // the launch's pairs
   const int32_t* labels;
   const int32_t* offsets;
   const float* ref_logp;

@@ -800,25 +800,40 @@ def mx4_empty(n: int, c: int, device="cuda"):
     return torch.empty((n, 16 * blocks), dtype=torch.uint8, device=device), scale[:, :blocks]
 
 
-def _mx4_blocks(q, scale, name):
-    """Blocks a row of codes uint8 [n, 16 b] and scales uint8 [n, b]."""
+def _mx4_rows(q, scale, name):
+    """(rows, blocks a row, distances of the rows of codes and of scales) of codes uint8 [n, 16 b] and scales uint8
+    [n, b]; one row is as far from the next as it is long."""
     import torch
-    if not (q.is_cuda and scale.is_cuda and q.dtype == scale.dtype == torch.uint8 and q.dim() == scale.dim() == 2 and
-            q.shape[0] == scale.shape[0] and q.shape[1] == 16 * scale.shape[1]):
-        raise ValueError(f"{name}: expected device tensors of uint8, codes [n, 16 b] and scales [n, b], got "
-                         f"{tuple(q.shape)} {q.dtype} and {tuple(scale.shape)} {scale.dtype}")
-    return scale.shape[1]
+    u8 = torch.uint8
+    shape, blocks = q.shape, scale.shape[-1]
+    if shape != (scale.shape[0], 16 * blocks) or scale.dim() != 2 or q.dtype != u8 or scale.dtype != u8:
+        raise ValueError(f"{name}: expected codes [n, 16 b] and scales [n, b] of uint8, got {tuple(shape)} {q.dtype} and "
+                         f"{tuple(scale.shape)} {scale.dtype}")
+    (ld, unit), (ld_s, unit_s) = q.stride(), scale.stride()
+    if unit != 1 or (unit_s != 1 and blocks > 1):
+        raise ValueError(f"{name}: expected contiguous rows, got strides {q.stride()} and {scale.stride()}")
+    n = shape[0]
+    return (n, blocks, ld, ld_s) if n > 1 else (n, blocks, 16 * blocks, (blocks + 15) // 16 * 16)
+
+
+def _on_device(first, *others):
+    """Every tensor on the device of ``first`` (a device tensor)."""
+    index = first.get_device()
+    for t in others:
+        if t.get_device() != index:
+            raise ValueError(f"tensors on {first.device} and {t.device}")
 
 
 def quantize_rows_mx4(x, q, scale, stream=None):
     """Rows of x [n, c] (fp32 or bf16) in 4-bit floating point: codes q uint8 [n, 16 b] and scales uint8 [n, b], one for
     each of the b = ceil(c / 32) blocks of 32 values (mx4_empty makes both)."""
     code = _dtype_code(x, "x")
-    ld_x, ld_q, ld_s = _rows(x, "x"), _rows(q, "q"), _rows(scale, "scale")
+    ld_x = _rows(x, "x")
     n, c = x.shape
-    if _mx4_blocks(q, scale, "q") != (c + 31) // 32 or q.shape[0] != n:
+    rows, blocks, ld_q, ld_s = _mx4_rows(q, scale, "q")
+    if blocks != (c + 31) // 32 or rows != n:
         raise ValueError(f"q: expected codes [{n}, {(c + 31) // 32 * 16}], got {tuple(q.shape)}")
-    _same_device(x, q, scale)
+    _on_device(x, q, scale)
     _call(x, stream, None, None, load_library().rafiki_quantize_rows_mx4, x.data_ptr(), code, ld_x, n, c, q.data_ptr(), ld_q,
           scale.data_ptr(), ld_s)
 
@@ -837,21 +852,20 @@ def fc_mx4(x, x_scale, w, w_scale, y, bias=None, relu: bool = False, workspace=N
     boundaries, scales readable up to the next one (mx4_empty)."""
     import torch
     code = _dtype_code(y, "y")
-    blocks = _mx4_blocks(x, x_scale, "x")
-    n, c_out = x.shape[0], w.shape[0]
-    if _mx4_blocks(w, w_scale, "w") != blocks or y.shape != (n, c_out):
+    n, blocks, ld_x, ld_xs = _mx4_rows(x, x_scale, "x")
+    c_out, w_blocks, ld_w, ld_ws = _mx4_rows(w, w_scale, "w")
+    if w_blocks != blocks or y.shape != (n, c_out):
         raise ValueError("expected codes x [n, 16 b] and w [c_out, 16 b] and y [n, c_out]")
-    strides = []
-    b16 = (blocks + 15) // 16 * 16                           # rows of scales are read up to there
-    for t, least, name in ((x, 16 * blocks, "x"), (x_scale, b16, "x_scale"), (w, 16 * blocks, "w"), (w_scale, b16, "w_scale")):
-        ld = _rows(t, name) if t.shape[0] > 1 else least     # one row has no distance to the next
-        if t.storage_offset() + (t.shape[0] - 1) * ld + least > t.untyped_storage().nbytes():
-            raise ValueError(f"{name}: the last row is not readable up to the next multiple of 16")
-        strides += [t.data_ptr(), ld]
-    _same_device(y, x, x_scale, w, w_scale)
-    _call(y, stream, fc_mx4_workspace(n, 32 * blocks, c_out), workspace, load_library().rafiki_fc_mx4, *strides,
-          _vector(bias, c_out, torch.float32, y.device, "bias"), n, 32 * blocks, c_out, 1 if relu else 0, y.data_ptr(), code,
-          _rows(y, "y"))
+    pad = -blocks % 16                                       # rows of scales are read up to there
+    if pad:
+        for t, name in ((x_scale, "x_scale"), (w_scale, "w_scale")):
+            if t.storage_offset() + (t.shape[0] - 1) * t.stride(0) + blocks + pad > t.untyped_storage().nbytes():
+                raise ValueError(f"{name}: the last row is not readable up to the next multiple of 16")
+    _on_device(y, x, x_scale, w, w_scale)
+    _call(y, stream, fc_mx4_workspace(n, 32 * blocks, c_out), workspace, load_library().rafiki_fc_mx4, x.data_ptr(), ld_x,
+          x_scale.data_ptr(), ld_xs, w.data_ptr(), ld_w, w_scale.data_ptr(), ld_ws,
+          _vector(bias, c_out, torch.float32, y.device, "bias") if bias is not None else 0, n, 32 * blocks, c_out,
+          1 if relu else 0, y.data_ptr(), code, _rows(y, "y"))
 
 
 def tile_configs():

@@ -26,57 +26,71 @@ __device__ __forceinline__ float value(const void* p, long long i) {
   else return ((const float*)p)[i];
 }
 
-// The code of v (already over its scale): magnitudes are multiples of 1/2 below 2, of 1 below 4 and of 2 above, and rounding up
-// to the next such range gives its first code.
-__device__ __forceinline__ uint32_t code_of(float v) {
-  const float m = fminf(fabsf(v), 6.f);
-  const float code = m < 2.f ? __builtin_rintf(2.f * m) : m < 4.f ? 2.f + __builtin_rintf(m) : 4.f + __builtin_rintf(0.5f * m);
-  return (uint32_t)code | (__float_as_uint(v) >> 31 << 3);
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Two values over `scale` as codes in byte `at` of `codes`: to the nearest magnitude, ties to even, above 6 to 6, the sign kept.
+__device__ __forceinline__ uint32_t two_codes(uint32_t codes, bf16x2 v, float scale, int at) {
+  switch (at) {
+    case 0: return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, v, scale, 0);
+    case 1: return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, v, scale, 1);
+    case 2: return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, v, scale, 2);
+    default: return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, v, scale, 3);
+  }
+}
+__device__ __forceinline__ uint32_t two_codes(uint32_t codes, float lo, float hi, float scale, int at) {
+  switch (at) {
+    case 0: return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, lo, hi, scale, 0);
+    case 1: return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, lo, hi, scale, 1);
+    case 2: return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, lo, hi, scale, 2);
+    default: return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, lo, hi, scale, 3);
+  }
 }
 
-// A thread per 8 values of a block, 4 threads a block.
+// A thread per 8 values of a block, 4 threads a block.  Bits of magnitudes order as the magnitudes, NaN above +inf.
 template <bool BF16>
 __global__ __launch_bounds__(256) void quantize_mx4_kernel(const void* x, long long ld_x, int n, int c, uint8_t* q,
                                                            long long ld_q, uint8_t* scale, long long ld_scale) {
+  constexpr int W = BF16 ? 4 : 8;                            // registers of 8 values
   const int quarters = (c + 31) / 32 * 4;
   const long long total = (long long)n * quarters;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
-    const long long row = i / quarters;
+    const long long row = total >> 32 ? i / quarters : (uint32_t)i / (uint32_t)quarters;
     const int part = (int)(i - row * quarters), c0 = part * 8;
     const long long base = row * ld_x + c0;
-    float v[8];
+    uint32_t v[W];
     if (c0 + 8 <= c) {
-      if constexpr (BF16) {
-        const u32x4_any w = *(const u32x4_any*)((const bf16_t*)x + base);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v[2 * j] = __uint_as_float(w[j] << 16);
-          v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-        }
-      } else {
+      for (int h = 0; h < W / 4; ++h) {
+        const u32x4_any w = *(const u32x4_any*)((const char*)x + base * (BF16 ? 2 : 4) + 16 * h);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const u32x4_any w = *(const u32x4_any*)((const float*)x + base + 4 * h);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[4 * h + j] = __uint_as_float(w[j]);
-        }
+        for (int j = 0; j < 4; ++j) v[4 * h + j] = w[j];
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = c0 + j < c ? value<BF16>(x, base + j) : 0.f;
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t b = c0 + j < c ? __float_as_uint(value<BF16>(x, base + j)) : 0u;
+        if constexpr (!BF16) v[j] = b;
+        else v[j / 2] = j & 1 ? v[j / 2] | b : b >> 16;
+      }
     }
-    uint32_t top = 0;                                        // bits of magnitudes order as the magnitudes, NaN above +inf
+    uint32_t top = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+    for (int j = 0; j < W; ++j) {
+      if constexpr (BF16) top = max(top, max(v[j] << 16 & 0x7FFF0000u, v[j] & 0x7FFF0000u));
+      else top = max(top, v[j] & 0x7FFFFFFFu);
+    }
     top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
     top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
     const bool bad = top >= 0x7F800000u;
     const int e = max((int)(top >> 23) - 127 - 2, -127);     // of a value below 2^-126, at most -127 too
-    const float inverse = __uint_as_float((uint32_t)(127 - e) << 23);   // 2^-e: e is in [-127, 125]
+    const float s = e == -127 ? 0x1p-127f : __uint_as_float((uint32_t)(127 + e) << 23);
     uint32_t codes = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) codes |= (bad ? 0u : code_of(v[j] * inverse)) << (4 * j);
-    *(u32_byte*)(q + row * ld_q + part * 4) = codes;
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (BF16) codes = two_codes(codes, __builtin_bit_cast(bf16x2, v[j]), s, j);
+      else codes = two_codes(codes, __uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]), s, j);
+    }
+    *(u32_byte*)(q + row * ld_q + part * 4) = bad ? 0u : codes;
     if ((part & 3) == 0) scale[row * ld_scale + part / 4] = bad ? 255 : (uint8_t)(e + 127);
   }
 }
@@ -107,73 +121,48 @@ __device__ __forceinline__ f32x4 mfma16(i32x4 w, i32x4 x, f32x4 acc, int s, int 
   }
 }
 
-// Few rows (16 NB a workgroup): 16 rows of w and its WAVES waves the steps of 16 blocks in turn.  Lane l holds blocks
-// 4 (l / 16) .. + 3 of a step of row l % 16 of either operand; outputs are 4 (l / 16) .. + 3 of w's rows for row l % 16 of x,
-// and the waves' sums meet in LDS.
-template <int NB, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void fc_mx4_rows_kernel(FcMx4Args a) {
-  __shared__ f32x4 sums[WAVES][NB][64];
+// Up to 16 rows: 16 rows of w a workgroup, whose 8 waves take the steps of 16 blocks in turn.  Lane l holds blocks 4 (l / 16) ..
+// + 3 of a step of row l % 16 of either operand; outputs are 4 (l / 16) .. + 3 of w's rows for row l % 16 of x, and the
+// waves' sums meet in LDS.  Bound by w's bytes and the launch: 1 x 4096 x 4096 4.5 us, 1 x 25088 x 4096 12 us (4.5 TB/s; in 4 waves
+// 16).
+__global__ __launch_bounds__(512) void fc_mx4_rows_kernel(FcMx4Args a) {
+  constexpr int NW = 8;
+  __shared__ f32x4 sums[NW][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int o0 = blockIdx.x * 16, r = lane & 15, q = lane >> 4;
-  const long long wr = min(o0 + r, a.c_out - 1);
-  const uint8_t* wp = a.w + wr * a.ld_w;
-  const uint8_t* wsp = a.ws + wr * a.ld_ws;
-  const uint8_t* xp[NB];
-  const uint8_t* xsp[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const long long xr = min(b * 16 + r, a.n - 1);
-    xp[b] = a.x + xr * a.ld_x;
-    xsp[b] = a.xs + xr * a.ld_xs;
-  }
-  f32x4 acc[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const long long wr = min(o0 + r, a.c_out - 1), xr = min(r, a.n - 1);
+  const uint8_t *wp = a.w + wr * a.ld_w, *wsp = a.ws + wr * a.ld_ws, *xp = a.x + xr * a.ld_x, *xsp = a.xs + xr * a.ld_xs;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   const int steps = (a.blocks + 15) / 16;
-  for (int s = wave; s < steps; s += WAVES) {
+  for (int s = wave; s < steps; s += NW) {
     const int b0 = s * 16 + q * 4, left = a.blocks - b0;     // blocks of the row from this lane's first on
     // scales behind the row's blocks are 0 (2^-127), not what lies there: NaN times code 0 is NaN
     const uint32_t mask = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
-    i32x4 w[4], x[NB][4];
-    int sw, sx[NB];
-    sw = (int)(*(const uint32_t*)(wsp + b0) & mask);
+    i32x4 w[4], x[4];
+    const int sw = (int)(*(const uint32_t*)(wsp + b0) & mask), sx = (int)(*(const uint32_t*)(xsp + b0) & mask);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      w[i] = i32x4{0, 0, 0, 0};
+      w[i] = x[i] = i32x4{0, 0, 0, 0};
       if (i < left) w[i] = *(const i32x4*)(wp + (long long)(b0 + i) * 16);
+      if (i < left) x[i] = *(const i32x4*)(xp + (long long)(b0 + i) * 16);
     }
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      sx[b] = (int)(*(const uint32_t*)(xsp[b] + b0) & mask);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[b][i] = i32x4{0, 0, 0, 0};
-        if (i < left) x[b][i] = *(const i32x4*)(xp[b] + (long long)(b0 + i) * 16);
-      }
-    }
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[b] = mfma16(w[i], x[b][i], acc[b], i, sw, sx[b]);
-    }
+    for (int i = 0; i < 4; ++i) acc = mfma16(w[i], x[i], acc, i, sw, sx);
   }
-#pragma unroll
-  for (int b = 0; b < NB; ++b) sums[wave][b][lane] = acc[b];
+  sums[wave][lane] = acc;
   __syncthreads();
-  for (int t = threadIdx.x; t < NB * 64; t += WAVES * 64) {
-    const int b = t >> 6, l = t & 63;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (threadIdx.x >= 64) return;
+  f32x4 v = sums[0][lane];
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) v += sums[w][b][l];
-    const int row = b * 16 + (l & 15), o = o0 + 4 * (l >> 4);
-    if (row >= a.n) continue;
+  for (int w = 1; w < NW; ++w) v += sums[w][lane];
+  const int o = o0 + 4 * q;
+  if (r >= a.n) return;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (o + j >= a.c_out) continue;
-      const float f = finish(v[j], a.bias ? a.bias[o + j] : 0.f, a.relu);
-      if (a.out_bf16) ((__bf16*)a.y)[row * a.ld_y + o + j] = (__bf16)f;
-      else ((float*)a.y)[row * a.ld_y + o + j] = f;
-    }
+  for (int j = 0; j < 4; ++j) {
+    if (o + j >= a.c_out) continue;
+    const float f = finish(v[j], a.bias ? a.bias[o + j] : 0.f, a.relu);
+    if (a.out_bf16) ((__bf16*)a.y)[r * a.ld_y + o + j] = (__bf16)f;
+    else ((float*)a.y)[r * a.ld_y + o + j] = f;
   }
 }
 
@@ -472,13 +461,18 @@ __global__ __launch_bounds__(256) void fc_mx4_reduce_kernel(FcMx4Args a, int spl
 struct MxConfig {
   int bm, bn;
 };
-constexpr MxConfig kMxConfigs[] = {{256, 256}, {128, 128}, {64, 128}};
+constexpr MxConfig kMxConfigs[] = {{256, 256}, {128, 128}, {64, 64}};
 constexpr int kUnitsOfGpu = 256;
 
 struct MxPlan {
   int cfg, splits, kt_per_split;
 };
 
+// The largest tile that still gives every compute unit one (2048 x 1024 x 8192: 20.0 us in 256 x 256, 21.6 in 128 x 128; 1000 x
+// 4096 x 4096: 33, 17.7 and 19.5 in 64 x 64; 512 x 4096 x 4096: 32, 16.0 and 11.6), else the smallest, with K split
+// where two workgroups a unit leave room for it, in runs of at least 12 K tiles (64 x 25088 x 4096: 49 us unsplit,
+// 18.1 in 8; 300 x 25088 x 500: 52.8 unsplit, 16.8 in 8; 40 x 4096 x 4096: 10.8 unsplit, 13.8 in 2): the splits' sums go
+// through memory and a second launch.
 MxPlan plan_mx4(int n, int blocks, int c_out) {
   const int pairs = (blocks + 15) / 16;                      // of K tiles
   auto tiles = [&](int c) {
@@ -486,7 +480,7 @@ MxPlan plan_mx4(int n, int blocks, int c_out) {
   };
   int cfg = 0;
   while (cfg < 2 && tiles(cfg) < kUnitsOfGpu) ++cfg;
-  const int splits = (int)std::max<long long>(1, std::min<long long>(kUnitsOfGpu / tiles(cfg), pairs / 4));
+  const int splits = cfg < 2 ? 1 : (int)std::max<long long>(1, std::min<long long>(2 * kUnitsOfGpu / tiles(cfg), pairs / 6));
   const int per = (pairs + splits - 1) / splits;
   return MxPlan{cfg, (pairs + per - 1) / per, 2 * per};
 }
@@ -499,7 +493,10 @@ hipError_t launch_mx4_tile(const FcMx4Args& a, int splits, hipStream_t s) {
   return hipGetLastError();
 }
 
-bool few_rows_mx4(int n, int blocks, int c_out) { return n <= 32; }
+// What fc_mx4_rows_kernel takes: its workgroups read x again for every 16 outputs.  In us, and in tiles: 1 x 25088 x 4096 12.1 and
+// 14.7, 2 x 8192 x 8192 10.9 and 13.6, 1 x 25088 x 100 12.4 and 13.3; but 16 x 25088 x 4096 17.1 and 15.4, 1 x 4096 x
+// 30000 14.4 and 12.4, 16 x 4096 x 30000 21.6 and 12.5.
+bool few_rows_mx4(int n, int blocks, int c_out) { return n <= 16 && n * blocks <= 4096 && c_out <= 8192; }
 
 }  // namespace
 
@@ -521,9 +518,7 @@ long long fc_mx4_workspace_bytes(int n, int blocks, int c_out) {
 hipError_t launch_fc_mx4(const FcMx4Args& args, hipStream_t s) {
   FcMx4Args a = args;
   if (few_rows_mx4(a.n, a.blocks, a.c_out)) {
-    const dim3 grid((a.c_out + 15) / 16);
-    if (a.n <= 16) launch(fc_mx4_rows_kernel<1, 4>, grid, dim3(256), s, a);
-    else launch(fc_mx4_rows_kernel<2, 4>, grid, dim3(256), s, a);
+    launch(fc_mx4_rows_kernel, dim3((a.c_out + 15) / 16), dim3(512), s, a);
     return hipGetLastError();
   }
   const MxPlan p = plan_mx4(a.n, a.blocks, a.c_out);
@@ -532,7 +527,7 @@ hipError_t launch_fc_mx4(const FcMx4Args& args, hipStream_t s) {
   switch (p.cfg) {
     case 0: st = launch_mx4_tile<256, 256, 2, 4, 2>(a, p.splits, s); break;
     case 1: st = launch_mx4_tile<128, 128, 2, 2, 2>(a, p.splits, s); break;
-    default: st = launch_mx4_tile<64, 128, 1, 4, 2>(a, p.splits, s); break;
+    default: st = launch_mx4_tile<64, 64, 2, 2, 2>(a, p.splits, s); break;
   }
   if (st != hipSuccess || p.splits == 1) return st;
   const long long total = (long long)a.n * ((a.c_out + 3) / 4);

@@ -117,7 +117,7 @@ int rafiki_distill_loss(const void* logits, int dtype, long long ld_row, int n, 
  * (logit -inf) has log p = -inf, as has a log p beyond fp32; NaN, +inf or a row of only -inf gives NaN
  * in all outputs of the row.  Any output may be null, not all.  fp32 arithmetic; log p is exact to fp32 also
  * where p is near 1; each gradient is rounded once.  Scalars are 64 bits here, since what follows subtracts and sums
- * log-probabilities.  2^-20 <= T <= 2^20, n >= 1. */
+ * log-probabilities.  2^-20 <= T <= 2^20, 1 <= n <= 2^30. */
 int rafiki_token_logp(const void* logits, int dtype, long long ld_row, int n, int n_classes, const int32_t* labels,
                       double temperature, const float* grad_logp, const float* grad_entropy, float* out_logp,
                       float* out_entropy, void* grad_logits, long long ld_grad, void* workspace,

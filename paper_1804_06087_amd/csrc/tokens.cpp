@@ -33,7 +33,7 @@ long long combine_bytes(int n_models, int n, int n_classes) {
 bool fc_mx4_sizes(int n, int c_in, int c_out) {
   return n >= 1 && n <= (1 << 24) && c_out >= 1 && c_out <= (1 << 24) && c_in >= 32 && c_in <= (1 << 20) && c_in % 32 == 0;
 }
-bool row_sizes(int n, int n_classes) { return n >= 1 && n_classes >= 1 && n_classes <= kMaxTokenClasses; }
+bool row_sizes(int n, int n_classes) { return n >= 1 && n <= (1 << 30) && n_classes >= 1 && n_classes <= kMaxTokenClasses; }
 bool bad_workspace(const void* workspace, long long bytes, long long need) {
   return need && (!workspace || bytes < need || !aligned16(workspace));
 }
@@ -43,7 +43,7 @@ int check_rows(const void* logits, int dtype, long long ld_row, int n, int n_cla
                const void* grad_logits, long long ld_grad, const void* workspace, long long bytes, long long (*need)(int, int)) {
   if (!logits || !labels) return invalid("null pointer");
   if (!known(dtype)) return invalid("dtype must be RAFIKI_FP32 or RAFIKI_BF16");
-  if (!row_sizes(n, n_classes)) return invalid("n must be >= 1 and n_classes in [1, 2^20]");
+  if (!row_sizes(n, n_classes)) return invalid("n must be in [1, 2^30] and n_classes in [1, 2^20]");
   if (!(temperature >= 0x1p-20 && temperature <= 0x1p20)) return invalid("temperature must be in [2^-20, 2^20]");
   if (ld_row < 0 || (grad_logits && ld_grad < n_classes)) return invalid("row distances: ld_row >= 0, ld_grad >= n_classes");
   if (!aligned_to(logits, dtype) || !aligned_to(grad_logits, dtype)) return invalid("rows are not aligned to their type");
@@ -196,7 +196,7 @@ int rafiki_token_logp(const void* logits, int dtype, long long ld_row, int n, in
 
 int rafiki_token_workspace(int n, int n_classes, long long* bytes) {
   if (!bytes) return invalid("null pointer");
-  if (!row_sizes(n, n_classes)) return invalid("n must be >= 1 and n_classes in [1, 2^20]");
+  if (!row_sizes(n, n_classes)) return invalid("n must be in [1, 2^30] and n_classes in [1, 2^20]");
   *bytes = token_loss_workspace_bytes(n, n_classes);
   return RAFIKI_OK;
 }
@@ -234,7 +234,7 @@ int rafiki_policy_loss(const void* logits, int dtype, long long ld_row, int n, i
 
 int rafiki_preference_workspace(int n, int n_classes, long long* bytes) {
   if (!bytes) return invalid("null pointer");
-  if (!row_sizes(n, n_classes)) return invalid("n must be >= 1 and n_classes in [1, 2^20]");
+  if (!row_sizes(n, n_classes)) return invalid("n must be in [1, 2^30] and n_classes in [1, 2^20]");
   *bytes = preference_workspace_bytes(n, n_classes);
   return RAFIKI_OK;
 }

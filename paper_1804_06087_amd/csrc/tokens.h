@@ -99,7 +99,8 @@ struct TokenLossArgs {
 };
 
 struct PreferenceRow {        // of the workspace
-  float top, share, rest;     // the powers' reference, p there, 1 - p of the label
+  float top, shift, share;    // p of a class is 2^((z - top) s - shift) share
+  float rest;                 // 1 - p of the label
   float weight;               // dL / d log p over T
 };
 struct PreferenceArgs {

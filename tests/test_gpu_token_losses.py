@@ -221,6 +221,30 @@ def test_token_logp_of_a_sure_student():
         assert abs(float(grad[i, labels[i]]) + want) <= rel * abs(want) + abs(want) ** 2
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("C", [50, 900, 9000, 70001])
+def test_token_logp_of_unlikely_tokens(C, dtype):
+    """Labels up to e^-400 below the others, with weights down to 1e-30: the gradient of the likely classes keeps its
+    precision, whichever way the row is summed."""
+    below = (10.0, 20.0, 30.0, 33.0, 34.0, 60.0, 87.0, 88.0, 89.0, 104.0, 400.0)
+    n = len(below)
+    rng = np.random.default_rng(C)
+    z = torch.from_numpy(rng.standard_normal((n, C)).astype(np.float32))
+    labels = rng.integers(0, C, n).astype(np.int32)
+    for i, d in enumerate(below):
+        z[i, labels[i]] = -d
+    z = z.to(DT[dtype]).to(DEV)
+    for a in (1.0, 1e-8, 1e-30):
+        w = np.full(n, a, np.float32)
+        for h in (None, w):
+            check_logp(z, labels, 1.0, w, h, run_logp(z, labels, 1.0, w, h), dtype)
+    A, g = np.ones(n, np.float32), np.full(n, 1e-8, np.float32)
+    check_policy(z, labels, A, None, None, g, 1.0, 0.2, 0.2, 0.0, 0.01, run_policy(z, labels, A, None, None, g, ent=0.01), dtype)
+    offsets = [0, 5, n]
+    check_preference(z, labels, offsets, None, 1.0, 1e-3, 0.0, False, None,
+                     run_preference(z, labels, offsets, None, 1.0, 1e-3), dtype)
+
+
 def test_token_logp_strided_unaligned_broadcast():
     rng = np.random.default_rng(3)
     n, C = 7, 1001

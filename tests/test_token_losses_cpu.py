@@ -50,7 +50,7 @@ def _fc(**over):
     return pkg.load_library().rafiki_fc_mx4(*a.values())
 
 
-ROWS = ({"logits": None}, {"labels": None}, {"dtype": 2}, {"dtype": -1}, {"n": 0}, {"n": -1}, {"C": 0}, {"C": (1 << 20) + 1},
+ROWS = ({"logits": None}, {"labels": None}, {"dtype": 2}, {"dtype": -1}, {"n": 0}, {"n": -1}, {"n": (1 << 30) + 1}, {"C": 0}, {"C": (1 << 20) + 1},
         {"t": 0.0}, {"t": -1.0}, {"t": math.nan}, {"t": math.inf}, {"t": 2.0 ** -21}, {"t": 2.0 ** 21}, {"ld_row": -1},
         {"ld_grad": 9}, {"logits": P + 2}, {"grad": P + 2}, {"dtype": 1, "logits": P + 1})
 
@@ -84,7 +84,7 @@ def test_workspace_sizes():
     lib, b = pkg.load_library(), C.c_longlong(-1)
     for f in (lib.rafiki_preference_workspace, lib.rafiki_token_workspace):
         assert f(1, 1, None) == INVALID
-        for bad in ((0, 1), (1, 0), (1, (1 << 20) + 1)):
+        for bad in ((0, 1), (1, 0), (1, (1 << 20) + 1), ((1 << 30) + 1, 1)):
             assert f(*bad, C.byref(b)) == INVALID
     assert bd.preference_workspace(1 << 30, 1) > 1 << 32                 # 64-bit size
     assert bd.token_workspace(1 << 30, 1 << 20) >= 0

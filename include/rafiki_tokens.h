@@ -162,7 +162,7 @@ int rafiki_policy_loss(const void* logits, int dtype, long long ld_row, int n, i
  * tokens NaN.  Rows before offsets[0] and from offsets[2 n_pairs] on are not read and their gradient rows are left as
  * they were.  Offsets that decrease or leave [0, n] give wrong values but no access out of the
  * arrays.  log p, scores and the loss are summed in 64 bits.  beta > 0 and finite, 0 <= smoothing <= 0.5,
- * 1 <= n_pairs <= 2^24. */
+ * 1 <= n_pairs <= 2^20. */
 int rafiki_preference_loss(const void* logits, int dtype, long long ld_row, int n, int n_classes,
                            const int32_t* labels, const int32_t* offsets, int n_pairs, const float* ref_logp,
                            double temperature, double beta, double smoothing, int mean, const float* grad_loss,

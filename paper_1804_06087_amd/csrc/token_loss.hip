@@ -81,7 +81,6 @@ __device__ __forceinline__ T wave_add(T v) {
   return v;
 }
 
-
 // The maximum as a reference for powers: an empty row has none and takes 0.
 __device__ __forceinline__ float reference(float top) { return top == -INFINITY ? 0.f : top; }
 // Exponents of 2 as factors of a power that is 0 below here: -inf would make it NaN.
@@ -407,7 +406,7 @@ __device__ __forceinline__ void store_gradient(const Row<BF16>& r, char* row, in
   r.store(row, i, z, d.at_label);
 }
 
-// What a row needs before it is read: false if nothing of it is.
+// Opens a row: whether it has a token, and whether its gradient is 0 by its weights.
 template <bool BF16, bool POLICY>
 __device__ __forceinline__ bool open_row(const TokenLossArgs& a, int row, Row<BF16>& r, bool& weightless) {
   const int label = a.labels[row];
@@ -471,7 +470,7 @@ __global__ __launch_bounds__(NT * G) void token_loss_kernel(TokenLossArgs a) {
   float lost = 0.f;
   each(std::false_type{}, [&](const float* z, int) { add_chunk<V, ENT, false>(sums, lost, z, z_label, a.s); });
   sums = join<NT, ENT, false>(sums, a.s.hi, waves);
-  if (!bounded(sums)) {                                 // the same in all of the row's threads
+  if (!bounded(sums)) {                                      // the same in all of the row's threads
     if constexpr (NW > 1) __syncthreads();
     sums = Sums{0.0, 0.0, -INFINITY};
     each(std::false_type{}, [&](const float* z, int) { add_chunk_any<V, ENT>(sums, z, a.s.hi); });

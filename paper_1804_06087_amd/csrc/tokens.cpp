@@ -248,7 +248,7 @@ int rafiki_preference_loss(const void* logits, int dtype, long long ld_row, int 
                             workspace_bytes, preference_workspace_bytes);
   if (rc) return rc;
   if (!out_loss && !out_scores && !grad_logits) return invalid("no output is asked for");
-  if (n_pairs < 1 || n_pairs > (1 << 24)) return invalid("n_pairs must be in [1, 2^24]");
+  if (n_pairs < 1 || n_pairs > (1 << 20)) return invalid("n_pairs must be in [1, 2^20]");
   if (!offsets && n % (2LL * n_pairs)) return invalid("without offsets n must be a multiple of 2 n_pairs");
   if (!(beta > 0) || !std::isfinite(beta) || !(smoothing >= 0 && smoothing <= 0.5))
     return invalid("beta must be positive and finite, smoothing in [0, 0.5]");

@@ -581,6 +581,35 @@ def test_preference_special_rows(dtype):
     assert (out[2] == 0).all()
 
 
+@pytest.mark.parametrize("pairs", [70000, 1 << 20])
+def test_preference_of_many_pairs(pairs):
+    """More pairs than a grid's second axis takes, most of them without rows or with one."""
+    C, n = 5, 150000
+    g = torch.Generator(device="cuda").manual_seed(pairs)
+    z = torch.randn((n, C), device=DEV, generator=g)
+    labels = torch.randint(-1, C, (n,), dtype=torch.int32, device=DEV, generator=g)
+    offsets = torch.sort(torch.randint(0, n + 1, (2 * pairs + 1,), dtype=torch.int32, device=DEV, generator=g)).values
+    loss, scores, grad = full(pairs), full(pairs, 2), torch.full_like(z, -7)
+    bd.preference_loss(z, labels, loss, grad, offsets=offsets, out_scores=scores, beta=0.5)
+    rows = torch.log_softmax(z.double(), -1)
+    at = labels.clamp(min=0).long()[:, None]
+    valid = labels >= 0
+    logp = torch.where(valid, rows.gather(1, at)[:, 0], 0)
+    run = torch.cat([torch.zeros(1, dtype=torch.float64, device=DEV), logp.cumsum(0)])
+    first = offsets.long()
+    score = (0.5 * (run[first[1:]] - run[first[:-1]])).view(-1, 2)
+    u = score[:, 0] - score[:, 1]
+    # five terms: 2^-22 (|x| + 4) with |x| < 14 a row, at most some 20 rows an answer; the running sum is off by 1e-9
+    assert (scores.double() - score).abs().max() < 20 * 2.0 ** -17 and (loss.double() + torch.nn.functional.logsigmoid(u)).abs().max() < 40 * 2.0 ** -17
+    which = torch.searchsorted(first[1:], torch.arange(n, device=DEV), right=True).clamp(max=2 * pairs - 1)
+    a = -0.5 * torch.sigmoid(-u)[which // 2] * (1 - 2 * (which % 2)) * valid
+    want = -torch.exp(rows)
+    want.scatter_add_(1, at, torch.ones_like(want[:, :1]))
+    want *= a[:, None]
+    inside = (torch.arange(n, device=DEV) >= first[0]) & (torch.arange(n, device=DEV) < first[-1])
+    assert (grad.double() - want)[inside].abs().max() < 2.0 ** -13 and (grad[~inside] == -7).all()
+
+
 def test_preference_bad_offsets_stay_inside():
     """Decreasing offsets and such beyond the rows: wrong values, but nothing outside of the arrays is written."""
     n, C = 6, 300

@@ -63,7 +63,7 @@ ROWS = ({"logits": None}, {"labels": None}, {"dtype": 2}, {"dtype": -1}, {"n": 0
     *[(_policy, o) for o in ({"advantage": None}, {"loss": None, "logp": None, "out_kl": None, "entropy": None, "grad": None},
                              {"low": -0.1}, {"low": 1.1}, {"low": math.nan}, {"high": -0.1}, {"high": math.nan},
                              {"kl": math.inf}, {"kl": math.nan}, {"ent": math.inf}, {"ent": math.nan})],
-    *[(_preference, o) for o in ({"loss": None, "scores": None, "grad": None}, {"pairs": 0}, {"pairs": (1 << 24) + 1},
+    *[(_preference, o) for o in ({"loss": None, "scores": None, "grad": None}, {"pairs": 0}, {"pairs": (1 << 20) + 1},
                                  {"offsets": None, "pairs": 3}, {"beta": 0.0}, {"beta": -1.0}, {"beta": math.inf},
                                  {"beta": math.nan}, {"smoothing": -0.1}, {"smoothing": 0.6}, {"smoothing": math.nan},
                                  {"ws": None}, {"ws": P + 8}, {"ws_bytes": 8})],

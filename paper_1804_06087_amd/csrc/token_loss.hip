@@ -31,24 +31,26 @@ typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
+// BF16 as a template's parameter: 0 fp32 values, 1 bf16, 2 bf16 in rows that may start off 16-byte boundaries.
+
 __device__ __forceinline__ float power2(float t) { return __builtin_amdgcn_exp2f(t); }
 
-template <bool BF16>
+template <int BF16>
 __device__ __forceinline__ float element(const void* p, long long i) {
-  if constexpr (BF16) return __uint_as_float((uint32_t)((const bf16_t*)p)[i] << 16);
+  if constexpr (BF16 != 0) return __uint_as_float((uint32_t)((const bf16_t*)p)[i] << 16);
   else return ((const float*)p)[i];
 }
 // Rounded once, to nearest, ties to even; NaN stays NaN.
-template <bool BF16>
+template <int BF16>
 __device__ __forceinline__ void put(void* p, long long i, float v) {
-  if constexpr (BF16) ((__bf16*)p)[i] = (__bf16)v;
+  if constexpr (BF16 != 0) ((__bf16*)p)[i] = (__bf16)v;
   else ((float*)p)[i] = v;
 }
-template <bool BF16, int V>
+template <int BF16, int V>
 __device__ __forceinline__ void unpack(u32x4 q, float z[V]) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    if constexpr (BF16) {
+    if constexpr (BF16 != 0) {
       z[2 * j] = __uint_as_float(q[j] << 16);
       z[2 * j + 1] = __uint_as_float(q[j] & 0xFFFF0000u);
     } else {
@@ -56,12 +58,12 @@ __device__ __forceinline__ void unpack(u32x4 q, float z[V]) {
     }
   }
 }
-template <bool BF16, int V>
+template <int BF16, int V>
 __device__ __forceinline__ u32x4 pack(const float z[V]) {
   u32x4 q;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    if constexpr (BF16) q[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{z[2 * j], z[2 * j + 1]}, bf16x2));
+    if constexpr (BF16 != 0) q[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{z[2 * j], z[2 * j + 1]}, bf16x2));
     else q[j] = __float_as_uint(z[j]);
   }
   return q;
@@ -86,47 +88,47 @@ __device__ __forceinline__ float reference(float top) { return top == -INFINITY 
 // Exponents of 2 as factors of a power that is 0 below here: -inf would make it NaN.
 __device__ __forceinline__ float finite_log2(float x) { return fmaxf(x, -16384.f); }
 
-// A row of C values as chunks of 16 bytes, chunk i from class i V on; the last one, of fewer values, is read from
-// class C - V on.  Rows may start anywhere.
-template <bool BF16>
+// A row of C values as chunks of 16 bytes, chunk i from class i V - shift on.  Rows may start anywhere; unaligned chunks of bf16
+// values were a fifth slower (6000 x 131071 321 us, 6000 x 131072 257; fp32 rows take as long either way), so those are
+// taken on 16-byte boundaries of the logits.  The first and the last chunk may have fewer values, and are read from class
+// 0 or C - V on.
+template <int BF16>
 struct Row {
   static constexpr int V = BF16 ? 8 : 4;
   const char* x;
-  int C, chunks, label;
+  int C, shift, chunks, label;
 
   __device__ __forceinline__ void init(const void* logits, long long base, int C_, int label_) {
     x = (const char*)logits + base * (16 / V);
     C = C_;
-    chunks = (C + V - 1) / V;
+    shift = BF16 == 2 ? (int)((uintptr_t)x & 15) / 2 : 0;
+    chunks = (C + shift + V - 1) / V;
     label = label_;
   }
+  __device__ __forceinline__ float at(int c) const { return element<BF16>(x, c); }
   // Chunk i with -inf in the label's place and in those of classes that it does not have.
   template <bool STREAM>
   __device__ __forceinline__ u32x4 load(int i) const {
-    const int c0 = i * V;
-    const bool short_chunk = c0 + V > C;
+    const int c0 = i * V - shift, first = min(BF16 == 2 ? max(c0, 0) : c0, C - V);
     u32x4 q;
-    if (!short_chunk || C >= V) {
-      const u32x4_any* p = (const u32x4_any*)(x + (long long)(short_chunk ? C - V : c0) * (16 / V));
+    if (C >= V) {
+      const u32x4_any* p = (const u32x4_any*)(x + (long long)first * (16 / V));
       if constexpr (STREAM) q = __builtin_nontemporal_load(p);
       else q = *p;
     }
-    if (short_chunk || (unsigned)(label - c0) < (unsigned)V) {
+    if (c0 != first || (unsigned)(label - c0) < (unsigned)V) {
       float z[V];
-      if (short_chunk) {
-        const int n = C - c0;                                // its classes: the last n of the V that were read
-        float t[V];
-        if (C >= V) {
-          unpack<BF16, V>(q, t);
-        } else {
+      if (C < V) {
 #pragma unroll
-          for (int j = 0; j < V; ++j) t[j] = j >= V - n ? element<BF16>(x, j - (V - n)) : -INFINITY;
-        }
+        for (int j = 0; j < V; ++j) z[j] = (unsigned)(c0 + j) < (unsigned)C ? at(c0 + j) : -INFINITY;
+      } else if (c0 != first) {
+        float t[V];
+        unpack<BF16, V>(q, t);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           z[j] = -INFINITY;
 #pragma unroll
-          for (int k = 0; k < V; ++k) z[j] = k == j + V - n ? t[k] : z[j];
+          for (int k = 0; k < V; ++k) z[j] = k == j + c0 - first ? t[k] : z[j];
         }
       } else {
         unpack<BF16, V>(q, z);
@@ -139,17 +141,17 @@ struct Row {
   }
   // Chunk i of a row of values; the label's is `at_label`.
   __device__ __forceinline__ void store(char* row, int i, float d[V], float at_label) const {
-    const int c0 = i * V;
+    const int c0 = i * V - shift;
     if ((unsigned)(label - c0) < (unsigned)V) {
 #pragma unroll
       for (int j = 0; j < V; ++j) d[j] = c0 + j == label ? at_label : d[j];
     }
-    if (c0 + V <= C) {
+    if (c0 >= 0 && c0 + V <= C) {
       __builtin_nontemporal_store(pack<BF16, V>(d), (u32x4_any*)(row + (long long)c0 * (16 / V)));
     } else {
 #pragma unroll
       for (int j = 0; j < V; ++j)
-        if (c0 + j < C) put<BF16>(row, c0 + j, d[j]);
+        if ((unsigned)(c0 + j) < (unsigned)C) put<BF16>(row, c0 + j, d[j]);
     }
   }
   __device__ __forceinline__ void zero_chunk(char* row, int i) const {
@@ -176,22 +178,36 @@ __device__ __forceinline__ float tree_sum(const float v[V]) {
   if constexpr (V == 8) return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
   else return (v[0] + v[1]) + (v[2] + v[3]);
 }
-// The power of x = (z - ref) s; PRECISE: what is rounded off x, by s, the product and the difference (of fp32 values), into
-// `lost`, whose sum times ln 2 belongs to the sum of powers.
-template <bool PRECISE, bool EXACT_DIFFERENCE>
+// The power of x = (z - ref) s.  PRECISE (fp32 values): what is rounded off x, by the difference, s and the product, into `lost`,
+// whose sum times ln 2 belongs to the sum of powers.
+template <bool PRECISE>
 __device__ __forceinline__ float term(float z, float ref, const Scale& s, float& x, float& lost) {
   const float d = z - ref;
   x = d * s.hi;
   const float e = power2(x);
   if constexpr (PRECISE) {
-    float off = fmaf(d, s.lo, fmaf(d, s.hi, -x));
-    if constexpr (!EXACT_DIFFERENCE) {
-      const float back = d - z;
-      off = fmaf((z - (d - back)) - (ref + back), s.hi, off);
-    }
+    const float back = d - z;
+    const float off = fmaf((z - (d - back)) - (ref + back), s.hi, fmaf(d, s.lo, fmaf(d, s.hi, -x)));
     lost = fmaf(e, fminf(off, 1.f), lost);                   // NaN where d = -inf and e = 0: 1
   }
   return e;
+}
+// Precise sums of bf16 values, in fewer instructions: with s = s16 + rest16, s16 of 16 bits, and a reference that is a multiple of
+// 1/8, z s16 - ref s16 is exact for the values that count, and 2^(d rest16) = 1 + ln 2 d rest16 to 1e-7, whose sum comes from
+// that of 2^x z.  Where T is so low that 1/16 would be more than a few powers of 2, the label's logit stays the reference: x is
+// rounded then, but the few classes that such a T leaves have no bias to add up.
+__device__ __forceinline__ float coarse(float z, float s16) {
+  return s16 <= 64.f && fabsf(z) < 16.f ? 0.125f * __builtin_rintf(8.f * z) : z;
+}
+template <int V>
+__device__ __forceinline__ void add_chunk_bf16(Sums& a, float& weighted, const float z[V], float at, float s16) {
+  float e[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    e[j] = power2(fmaf(z[j], s16, -at));
+    weighted = fmaf(e[j], fmaxf(z[j], -0x1.fffffep127f), weighted);   // 0 for -inf
+  }
+  a.sum += (double)tree_sum<V>(e);
 }
 // Relative to the label's logit, which needs no maximum: what underflows beside the label's own 1 does not count, and while p_l
 // is above 2^-40 the powers that matter are below 2^40, whose exponents are rounded by 2^-19 at most.  A row of a less
@@ -202,7 +218,7 @@ __device__ __forceinline__ void add_chunk(Sums& a, float& lost, const float z[V]
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     float x;
-    e[j] = term<PRECISE, V == 8>(z[j], ref, s, x, lost);
+    e[j] = term<PRECISE>(z[j], ref, s, x, lost);
     if constexpr (ENT) m = fmaf(e[j], finite_log2(x), m);
   }
   a.sum += (double)tree_sum<V>(e);
@@ -289,16 +305,21 @@ __device__ __forceinline__ RowFacts row_facts(const Sums& r, float z, float s, d
   const double inv = 1.0 / total;
   f.rest = (float)(part * inv);
   f.p = (float)(e_y * inv);
-  const double ln_total = log(total), log2_p = (double)down - ln_total * 1.4426950408889634;
-  f.shift = (float)-rint(log2_p);
-  f.log2_share = (float)(log2_p + (double)f.shift);
-  f.share = (float)(inv * exp2((double)down + (double)f.shift));
-  f.entropy = ENT ? (float)(ln_total - 0.6931471805599453 * ((r.moment + r.sum * (double)down) * e_r + e_y * (double)x) * inv) : 0.f;
   // log p in 64 bits: the difference of two logits may exceed fp32, and what follows subtracts it
   const double D = ((double)z - (double)top) * inv_t;
   if (r.sum == 0.0) f.logp = 0.0;
   else if (D >= 0) f.logp = -log1p(r.sum * (D > 0 ? exp(-D) : 1.0));
   else f.logp = D - log(r.sum + exp(D));
+  const float log2_total = log2f((float)total), log2_p = down - log2_total;
+  f.shift = -__builtin_rintf(log2_p);
+  f.log2_share = log2_p + f.shift;
+  f.share = (float)inv * power2(down + f.shift);
+  f.entropy = 0.f;
+  if (ENT) {
+    const double ln_total = D >= 0 ? -f.logp : log(total);   // D >= 0: t = z
+    f.entropy = (float)(ln_total - 0.6931471805599453 * ((r.moment + r.sum * (double)down) * e_r + e_y * (double)x) * inv);
+    f.log2_share = (float)((double)down - ln_total * 1.4426950408889634 + (double)f.shift);
+  }
   if (!f.defined) {
     f.logp = NAN;
     f.entropy = NAN;
@@ -367,7 +388,7 @@ __device__ __forceinline__ RowGrad finish_row(const TokenLossArgs& a, int row, c
   return row_grad<ENT>(f, da, dh, (float)a.inv_t);
 }
 
-template <bool BF16>
+template <int BF16>
 __device__ __forceinline__ u32x4 masked_chunk() {
   constexpr uint32_t m = BF16 ? 0xFF80FF80u : 0xFF800000u;   // -inf in every place
   return u32x4{m, m, m, m};
@@ -375,7 +396,7 @@ __device__ __forceinline__ u32x4 masked_chunk() {
 
 // f(a chunk's values) for the chunks first, first + NT, .. below `last` of a row that is read for it, UN in flight (LAST: for the
 // last time, one chunk after another).
-template <bool BF16, bool LAST, int UN, int NT, typename F>
+template <int BF16, bool LAST, int UN, int NT, typename F>
 __device__ __forceinline__ void for_chunks(const Row<BF16>& r, int first, int last, F&& f) {
   constexpr int V = Row<BF16>::V;
   for (int i0 = first; i0 < last; i0 += NT * UN) {
@@ -395,7 +416,7 @@ __device__ __forceinline__ void for_chunks(const Row<BF16>& r, int first, int la
 }
 
 // Chunk i's gradient from its values.
-template <bool BF16, bool ENT>
+template <int BF16, bool ENT>
 __device__ __forceinline__ void store_gradient(const Row<BF16>& r, char* row, int i, float z[Row<BF16>::V], float top, float s,
                                                const RowGrad& d) {
 #pragma unroll
@@ -407,7 +428,7 @@ __device__ __forceinline__ void store_gradient(const Row<BF16>& r, char* row, in
 }
 
 // Opens a row: whether it has a token, and whether its gradient is 0 by its weights.
-template <bool BF16, bool POLICY>
+template <int BF16, bool POLICY>
 __device__ __forceinline__ bool open_row(const TokenLossArgs& a, int row, Row<BF16>& r, bool& weightless) {
   const int label = a.labels[row];
   r.init(a.logits, row * a.ld_row, a.C, label);
@@ -424,7 +445,7 @@ __device__ __forceinline__ void no_token(const TokenLossArgs& a, int row) {
 
 // NT threads per row, G rows a workgroup (G > 1: up to a wave each).  CH > 0: the row, of at most NT CH chunks, stays in registers
 // from its sums to its gradient, so that it is read once; CH = 0: any length, read again for the gradient.
-template <bool BF16, bool POLICY, bool ENT, int NT, int CH, int G, bool REST>
+template <int BF16, bool POLICY, bool ENT, int NT, int CH, int G, bool REST>
 __global__ __launch_bounds__(NT * G) void token_loss_kernel(TokenLossArgs a) {
   constexpr int V = Row<BF16>::V, NW = (NT + 63) / 64;
   static_assert(G == 1 || NT <= 64, "rows that share a workgroup have no barrier");
@@ -451,7 +472,7 @@ __global__ __launch_bounds__(NT * G) void token_loss_kernel(TokenLossArgs a) {
       if (i * NT + tid < r.chunks) held[i] = r.template load<true>(i * NT + tid);
     }
   }
-  const float z_label = element<BF16>(r.x, r.label);
+  const float z_label = r.at(r.label);
   auto each = [&](auto last, auto&& f) {
     if constexpr (CH > 0) {
 #pragma unroll
@@ -495,13 +516,25 @@ __global__ __launch_bounds__(NT * G) void token_loss_kernel(TokenLossArgs a) {
 // ---------------------------------------------------------------- rows in parts
 
 // The sums over a row's chunks first, first + NT, .. below `last`, joined over NT threads.
-template <bool BF16, bool ENT, bool PRECISE, int NT>
+template <int BF16, bool ENT, bool PRECISE, int NT>
 __device__ __forceinline__ Sums row_sums(const Row<BF16>& r, int first, int last, float z_label, const Scale& s, Sums* waves) {
   constexpr int V = Row<BF16>::V;
   Sums sums{0.0, 0.0, z_label};
   float lost = 0.f;
-  for_chunks<BF16, false, 4, NT>(r, first, last, [&](const float* z, int) { add_chunk<V, ENT, PRECISE>(sums, lost, z, z_label, s); });
-  if (PRECISE) sums.sum += (double)(kLn2 * lost);
+  if constexpr (BF16 != 0 && PRECISE) {
+    static_assert(!ENT, "without entropy");
+    sums.top = coarse(z_label, s.s16);
+    const float at = sums.top * s.s16;                       // exact
+    if (fabsf(at) <= 0x1p20f) {
+      for_chunks<BF16, false, 4, NT>(r, first, last, [&](const float* z, int) { add_chunk_bf16<V>(sums, lost, z, at, s.s16); });
+      sums.sum += (double)(kLn2 * s.rest16) * ((double)lost - (double)sums.top * sums.sum);
+    } else {
+      sums.sum = INFINITY;
+    }
+  } else {
+    for_chunks<BF16, false, 4, NT>(r, first, last, [&](const float* z, int) { add_chunk<V, ENT, PRECISE>(sums, lost, z, z_label, s); });
+    if (PRECISE) sums.sum += (double)(kLn2 * lost);
+  }
   sums = join<NT, ENT, false>(sums, s.hi, waves);
   if (!bounded(sums)) {
     if (NT > 64) __syncthreads();
@@ -512,11 +545,11 @@ __device__ __forceinline__ Sums row_sums(const Row<BF16>& r, int first, int last
   return sums;
 }
 // The sums of a row's part p, chunks p per .. + per - 1, into *out.
-template <bool BF16, bool ENT, bool PRECISE, int NT>
+template <int BF16, bool ENT, bool PRECISE, int NT>
 __device__ __forceinline__ void part_sums(const Row<BF16>& r, int p, int per, const Scale& s, Sums* out) {
   __shared__ Sums waves[NT / 64];
   const Sums sums = row_sums<BF16, ENT, PRECISE, NT>(r, p * per + threadIdx.x, min(r.chunks, (p + 1) * per),
-                                                     element<BF16>(r.x, r.label), s, waves);
+                                                     r.at(r.label), s, waves);
   if (threadIdx.x == 0) *out = sums;
 }
 // A row's sums from its parts', in every lane of a wave.
@@ -535,7 +568,7 @@ __device__ __forceinline__ Sums join_parts(const Sums* parts, int n, float s) {
   return join<64, ENT, true>(a, s, nullptr);
 }
 
-template <bool BF16, bool POLICY, bool ENT, int NT>
+template <int BF16, bool POLICY, bool ENT, int NT>
 __global__ __launch_bounds__(NT) void token_parts_kernel(TokenLossArgs a) {
   const int row = a.row0 + blockIdx.y;
   Row<BF16> r;
@@ -546,7 +579,7 @@ __global__ __launch_bounds__(NT) void token_parts_kernel(TokenLossArgs a) {
 }
 
 // The outputs (by the first part) and a part's gradient.
-template <bool BF16, bool POLICY, bool ENT, int NT>
+template <int BF16, bool POLICY, bool ENT, int NT>
 __global__ __launch_bounds__(NT) void token_parts_grad_kernel(TokenLossArgs a) {
   constexpr int V = Row<BF16>::V;
   __shared__ RowGrad shared_grad;
@@ -568,7 +601,7 @@ __global__ __launch_bounds__(NT) void token_parts_grad_kernel(TokenLossArgs a) {
   }
   if (threadIdx.x < 64) {
     const Sums sums = join_parts<ENT>((const Sums*)a.parts + (long long)row * a.n_parts, a.n_parts, a.s.hi);
-    const float z_label = element<BF16>(r.x, r.label);
+    const float z_label = r.at(r.label);
     const RowGrad d = finish_row<POLICY, ENT>(a, row, row_facts<ENT>(sums, z_label, a.s.hi, a.inv_t), p == 0 && threadIdx.x == 0);
     if (threadIdx.x == 0) {
       shared_grad = d;
@@ -593,8 +626,8 @@ __device__ __forceinline__ int offset_at(const PreferenceArgs& a, int i) {
 }
 
 // The sums of all rows, a workgroup a part of a row in turn.
-template <bool BF16, int NT>
-__global__ __launch_bounds__(NT, 6) void preference_sums_kernel(PreferenceArgs a) {
+template <int BF16, int NT>
+__global__ __launch_bounds__(NT) void preference_sums_kernel(PreferenceArgs a) {
   const int end = offset_at(a, 2 * a.pairs);
   for (int row = offset_at(a, 0) + blockIdx.y; row < end; row += gridDim.y) {
     const int label = a.labels[row];
@@ -645,7 +678,7 @@ __device__ __forceinline__ void finish_pair(const PreferenceArgs& a, int p, cons
 // One workgroup per pair: its rows' log p from their sums, its answers' sums in 64 bits (a thread's rows in their order, then
 // a tree, the same every time), the loss, and every row's weight.  A chain of a few dependent loads and 64-bit logarithms
 // for each 1024 rows: 7 us for 8 pairs of 470 rows, 13 us for 3 of 1760 (11 and 25 in 256 threads).
-template <bool BF16>
+template <int BF16>
 __global__ __launch_bounds__(1024) void preference_pairs_kernel(PreferenceArgs a) {
   constexpr int NW = 16;
   __shared__ double sums[2][NW];
@@ -696,7 +729,7 @@ __global__ __launch_bounds__(1024) void preference_pairs_kernel(PreferenceArgs a
 }
 
 // Small problems in one launch: a workgroup per pair, a wave a row in turn, whose logits it reads again for the gradient.
-template <bool BF16>
+template <int BF16>
 __global__ __launch_bounds__(1024) void preference_few_kernel(PreferenceArgs a) {
   constexpr int V = Row<BF16>::V, NW = 16;
   __shared__ double sums[2][NW];
@@ -709,7 +742,7 @@ __global__ __launch_bounds__(1024) void preference_few_kernel(PreferenceArgs a) 
     Row<BF16> r;
     r.init(a.logits, row * a.ld_row, a.C, a.labels[row]);
     if ((unsigned)r.label >= (unsigned)a.C) continue;
-    const float z_label = element<BF16>(r.x, r.label);
+    const float z_label = r.at(r.label);
     const Sums all = row_sums<BF16, false, true, 64>(r, lane, r.chunks, z_label, a.s, nullptr);
     const RowFacts f = row_facts<false>(all, z_label, a.s.hi, a.inv_t);
     if (lane == 0) {
@@ -749,7 +782,7 @@ __global__ __launch_bounds__(1024) void preference_few_kernel(PreferenceArgs a) 
   }
 }
 
-template <bool BF16, int NT>
+template <int BF16, int NT>
 __global__ __launch_bounds__(NT) void preference_grad_kernel(PreferenceArgs a) {
   constexpr int V = Row<BF16>::V;
   const int end = offset_at(a, 2 * a.pairs);
@@ -774,7 +807,7 @@ __global__ __launch_bounds__(NT) void preference_grad_kernel(PreferenceArgs a) {
 constexpr int kGridRows = 1 << 15;
 constexpr long long kFewBytes = 4 << 20;                     // bounds what uneven answers leave to one workgroup
 
-template <bool BF16, bool POLICY, bool ENT, int NT, int CH, int G, bool REST>
+template <int BF16, bool POLICY, bool ENT, int NT, int CH, int G, bool REST>
 hipError_t launch_loss_rows(const TokenLossArgs& args, hipStream_t s) {
   TokenLossArgs a = args;
   for (long long row = 0; row < args.n; row += (1 << 20) * G) {   // 2^20 workgroups a launch at most
@@ -794,7 +827,15 @@ int parts_of(long long n, int chunks) {
   return (int)std::max<long long>(1, std::min<long long>(kGroups / std::max<long long>(n, 1), chunks / kLeast));
 }
 
-template <bool BF16, bool POLICY, bool ENT>
+// Chunks of the longest row: one more where bf16 rows may start off 16-byte boundaries.
+template <int BF16>
+int most_chunks(int C) {
+  constexpr int V = Row<BF16>::V;
+  return (C + (BF16 == 2 ? 2 * V - 2 : V - 1)) / V;
+}
+bool on_boundaries(const void* logits, long long ld_row) { return ((uintptr_t)logits & 15) == 0 && ld_row % 8 == 0; }
+
+template <int BF16, bool POLICY, bool ENT>
 hipError_t launch_loss_parts(const TokenLossArgs& a, hipStream_t s) {
   constexpr int NT = 256;
   launch(token_parts_kernel<BF16, POLICY, ENT, NT>, dim3(a.n_parts, a.n), dim3(NT), s, a);
@@ -809,10 +850,10 @@ hipError_t launch_loss_parts(const TokenLossArgs& a, hipStream_t s) {
 // a cache: 4096 x 30000 bf16 102 us with 2048 of 3750 chunks held, 128 with all in 256 threads (106 in 512), 107 with
 // none; 1500 x 50021 fp32 127 us with 4096 of 12506 held, 132 with 2048, 140 with none, 145 with all; 2047 x 131071 bf16
 // 270, 271, 284, 291.  Without a gradient a row is read once: 4096 x 30000 52 us in 512 threads, 88 in 1024.
-template <bool BF16, bool POLICY, bool ENT>
+template <int BF16, bool POLICY, bool ENT>
 hipError_t launch_loss_by_length(const TokenLossArgs& args, hipStream_t s) {
   TokenLossArgs a = args;
-  const int chunks = (a.C + Row<BF16>::V - 1) / Row<BF16>::V;
+  const int chunks = most_chunks<BF16>(a.C);
   a.n_parts = parts_of(a.n, chunks);
   a.per_part = (chunks + a.n_parts - 1) / a.n_parts;
   if (a.n_parts > 1) return launch_loss_parts<BF16, POLICY, ENT>(a, s);
@@ -826,17 +867,17 @@ hipError_t launch_loss_by_length(const TokenLossArgs& args, hipStream_t s) {
   return launch_loss_rows<BF16, POLICY, ENT, 512, 8, 1, true>(a, s);
 }
 
-template <bool BF16>
+template <int BF16>
 hipError_t launch_loss(const TokenLossArgs& a, hipStream_t s) {
   const bool ent = a.entropy || a.grad_entropy || a.entropy_coef != 0.0;
   if (a.policy) return ent ? launch_loss_by_length<BF16, true, true>(a, s) : launch_loss_by_length<BF16, true, false>(a, s);
   return ent ? launch_loss_by_length<BF16, false, true>(a, s) : launch_loss_by_length<BF16, false, false>(a, s);
 }
 
-template <bool BF16>
+template <int BF16>
 hipError_t launch_preference_of(const PreferenceArgs& args, hipStream_t s) {
   PreferenceArgs a = args;
-  const int chunks = (a.C + Row<BF16>::V - 1) / Row<BF16>::V;
+  const int chunks = most_chunks<BF16>(a.C);
   a.n_parts = parts_of(a.n, chunks);
   a.per_part = (chunks + a.n_parts - 1) / a.n_parts;
   // One launch for few short rows.  In us, and in three launches: 2 pairs of 2 x 5 rows of 1000 fp32 8.9 and 15.2, 64 of 2 x 4
@@ -857,26 +898,30 @@ hipError_t launch_preference_of(const PreferenceArgs& args, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Parts of a row at most: of fp32 values, which has more chunks.
+int most_parts(int n, int n_classes) { return parts_of(n, (n_classes + 3) / 4); }
+
 }  // namespace
 
 long long token_loss_workspace_bytes(int n, int n_classes) {
-  // the parts of a row of fp32 values, which has more chunks
-  const int parts = parts_of(n, (n_classes + 3) / 4);
+  const int parts = most_parts(n, n_classes);
   return parts > 1 ? ((long long)n * parts * (long long)sizeof(Sums) + 15) / 16 * 16 : 0;
 }
 long long preference_workspace_bytes(int n, int n_classes) {
   return ((long long)n * (long long)sizeof(PreferenceRow) + 15) / 16 * 16 +
-         ((long long)n * parts_of(n, (n_classes + 3) / 4) * (long long)sizeof(Sums) + 15) / 16 * 16;
+         ((long long)n * most_parts(n, n_classes) * (long long)sizeof(Sums) + 15) / 16 * 16;
 }
 
 hipError_t launch_token_loss(const TokenLossArgs& a, bool bf16, hipStream_t s) {
-  return bf16 ? launch_loss<true>(a, s) : launch_loss<false>(a, s);
+  if (!bf16) return launch_loss<0>(a, s);
+  return on_boundaries(a.logits, a.ld_row) ? launch_loss<1>(a, s) : launch_loss<2>(a, s);
 }
 
 hipError_t launch_preference(const PreferenceArgs& args, bool bf16, hipStream_t s) {
   PreferenceArgs a = args;
   a.parts = (char*)a.rows + ((long long)a.n * (long long)sizeof(PreferenceRow) + 15) / 16 * 16;
-  return bf16 ? launch_preference_of<true>(a, s) : launch_preference_of<false>(a, s);
+  if (!bf16) return launch_preference_of<0>(a, s);
+  return on_boundaries(a.logits, a.ld_row) ? launch_preference_of<1>(a, s) : launch_preference_of<2>(a, s);
 }
 
 }  // namespace rafiki

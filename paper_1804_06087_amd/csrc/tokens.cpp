@@ -65,6 +65,10 @@ Args row_args(const void* logits, long long ld_row, int n, int n_classes, const 
   const double s = 1.4426950408889634 / temperature;
   a.s.hi = (float)s;
   a.s.lo = (float)(s - (double)a.s.hi);
+  int exponent;
+  const double bits = std::frexp(s, &exponent);              // in [1/2, 1)
+  a.s.s16 = (float)std::ldexp(std::rint(std::ldexp(bits, 16)), exponent - 16);
+  a.s.rest16 = (float)(s - (double)a.s.s16);
   a.grad = grad_logits;
   a.ld_grad = ld_grad;
   return a;

@@ -69,9 +69,9 @@ struct FcI8Args {
   int* partial;               // [splits][n][c_out] int32 sums (splits > 1)
 };
 
-// log2(e) / T, and what fp32 leaves of it.
+// log2(e) / T in fp32 and what that leaves of it; the first 16 bits of it and the rest.
 struct Scale {
-  float hi, lo;
+  float hi, lo, s16, rest16;
 };
 struct TokenLossArgs {
   const void* logits;

@@ -544,6 +544,24 @@ def test_preference(C, t, lengths, mean, dtype):
         assert torch.equal(alone[k], out[k])
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("t", [2.0 ** -20, 2.0 ** -12, 2.0 ** -8, 0.02, 0.03, 50.0, 2.0 ** 20])
+def test_preference_at_low_and_high_temperatures(t, dtype):
+    """Logits near 0, whose label is just above or below the others: what a low temperature makes large differences of."""
+    rng = np.random.default_rng(int(math.log2(t)) + 40)
+    for C in (2, 9, 700, 40001):
+        z = (rng.standard_normal((7, C)) * 0.05).astype(np.float32)
+        labels = rng.integers(0, C, 7).astype(np.int32)
+        z[1, labels[1]] = z[1].max() + np.float32(0.01)       # the likeliest class
+        z[2, labels[2]] = z[2].min() - np.float32(0.01)       # the least likely one
+        z[3] -= z[3].max() + np.float32(0.01)                 # all below 0, the label's below the others
+        z[3, labels[3]] = -0.0625
+        z[4] += 16 - z[4].mean()
+        z = torch.from_numpy(z).to(DT[dtype]).to(DEV)
+        out = run_preference(z, labels, [0, 2, 4, 5, 7], None, t, min(t, 1.0) * 0.3, 0.1)
+        check_preference(z, labels, [0, 2, 4, 5, 7], None, t, min(t, 1.0) * 0.3, 0.1, False, None, out, dtype)
+
+
 def test_preference_equal_lengths_and_padding():
     rng = np.random.default_rng(12)
     n, C = 24, 500

@@ -10,10 +10,10 @@
 //
 // Bound by bytes: logits read once and the gradient written once, where the factors f are the row's own; a preference loss
 // has them from all rows of a pair and reads the logits twice.  Measured on an MI355X (a device copy moves 4.8 TB/s): 8192 x
-// 131072 bf16 log p and entropy 310 us (5.9 TB/s of what has a token), 4096 x 30000 bf16 policy loss with entropy and
-// gradient 104 us (4.4 TB/s; with a maximum that the sums follow 133), 1500 x 50021 fp32 125 us (4.5), 3 pairs of 2 x 880 rows
-// of 131071 bf16 840 us, of which the sums take 273 (4.5 TB/s; vector instructions, of which PRECISE is a third) and the
-// gradient 551 (4.8 TB/s).  Pairs in groups that a cache might hold until their gradient is taken were slower (8
+// 131072 bf16 log p and entropy 316 us (5.9 TB/s of what has a token), 4096 x 30000 bf16 policy loss with entropy and
+// gradient 102 us (4.5 TB/s; with a maximum that the sums follow 133), 1500 x 50021 fp32 125 us (4.5), 3 pairs of 2 x 880 rows
+// of 131071 bf16 738 us, of which the sums take 219 (5.6 TB/s; 273 with the exponents of fp32 rows) and the
+// gradient 516 (4.8 TB/s).  Pairs in groups that a cache might hold until their gradient is taken were slower (8
 // groups of 2 pairs of 2 x 500 x 30000 663 us, all at once 557).
 #include "tokens.h"
 
@@ -845,11 +845,11 @@ hipError_t launch_loss_parts(const TokenLossArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Rows of up to 256 chunks share a wave (100000 x 1000 bf16: 231 us with 128 threads a row, 150 with 64, 110 with 32), up to 2048 stay
+// Rows of up to 256 chunks share a wave (100000 x 1000 bf16: 236 us with 128 threads a row, 129 with 64, 115 with 32), up to 2048 stay
 // in registers.  Of longer ones a part does, which leaves room for more rows a compute unit, and the rest is read again from
-// a cache: 4096 x 30000 bf16 102 us with 2048 of 3750 chunks held, 128 with all in 256 threads (106 in 512), 107 with
-// none; 1500 x 50021 fp32 127 us with 4096 of 12506 held, 132 with 2048, 140 with none, 145 with all; 2047 x 131071 bf16
-// 270, 271, 284, 291.  Without a gradient a row is read once: 4096 x 30000 52 us in 512 threads, 88 in 1024.
+// a cache: 4096 x 30000 bf16 103 us with 2048 of 3750 chunks held, 108 with all, 105 with
+// none; 1500 x 50021 fp32 127 us with 4096 of 12506 held, 132 with 2048, 140 with none, 139 with all; 2047 x 131071 bf16
+// 243, 240, 249, 285.  Without a gradient a row is read once: 4096 x 30000 52 us in 512 threads, 88 in 1024.
 template <int BF16, bool POLICY, bool ENT>
 hipError_t launch_loss_by_length(const TokenLossArgs& args, hipStream_t s) {
   TokenLossArgs a = args;

@@ -651,6 +651,8 @@ def _grad_rows(grad_logits, logits):
         return 0
     if grad_logits.shape != logits.shape or grad_logits.dtype != logits.dtype:
         raise ValueError("grad_logits: expected the shape and dtype of the logits")
+    if grad_logits.data_ptr() == logits.data_ptr():
+        raise ValueError("grad_logits: the logits are read again for it")
     _same_device(logits, grad_logits)
     return _rows(grad_logits, "grad_logits")
 

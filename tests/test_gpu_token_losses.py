@@ -804,3 +804,11 @@ def test_refusals_on_the_device():
                  lambda: bd.token_logp(z[:0], i[:0], f[:0])):
         with pytest.raises(RafikiError):
             call()
+
+
+def test_gradient_in_the_logits_place_is_refused():
+    z, i, f = torch.zeros(4, 6, device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV), torch.zeros(4, device=DEV)
+    for call in (lambda: bd.token_logp(z, i, None, None, z, f), lambda: bd.policy_loss(z, i, f, None, z),
+                 lambda: bd.preference_loss(z, i, None, z, n_pairs=2)):
+        with pytest.raises(ValueError, match="read again"):
+            call()

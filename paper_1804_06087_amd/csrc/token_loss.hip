@@ -445,8 +445,8 @@ __device__ __forceinline__ void no_token(const TokenLossArgs& a, int row) {
 
 // NT threads per row, G rows a workgroup (G > 1: up to a wave each).  CH > 0: the row, of at most NT CH chunks, stays in registers
 // from its sums to its gradient, so that it is read once; CH = 0: any length, read again for the gradient.
-template <int BF16, bool POLICY, bool ENT, int NT, int CH, int G, bool REST>
-__global__ __launch_bounds__(NT * G) void token_loss_kernel(TokenLossArgs a) {
+template <int BF16, bool POLICY, bool ENT, int NT, int CH, int G, bool REST, int OCC>
+__global__ __launch_bounds__(NT * G, OCC) void token_loss_kernel(TokenLossArgs a) {
   constexpr int V = Row<BF16>::V, NW = (NT + 63) / 64;
   static_assert(G == 1 || NT <= 64, "rows that share a workgroup have no barrier");
   __shared__ Sums waves[NW];
@@ -804,16 +804,16 @@ __global__ __launch_bounds__(NT) void preference_grad_kernel(PreferenceArgs a) {
 }
 
 // Workgroups of a launch's second axis at most.
-constexpr int kGridRows = 1 << 15;
+constexpr int kGridRows = 1 << 15, kUnits = 256;
 constexpr long long kFewBytes = 4 << 20;                     // bounds what uneven answers leave to one workgroup
 
-template <int BF16, bool POLICY, bool ENT, int NT, int CH, int G, bool REST>
+template <int BF16, bool POLICY, bool ENT, int NT, int CH, int G, bool REST, int OCC = 1>
 hipError_t launch_loss_rows(const TokenLossArgs& args, hipStream_t s) {
   TokenLossArgs a = args;
   for (long long row = 0; row < args.n; row += (1 << 20) * G) {   // 2^20 workgroups a launch at most
     a.row0 = (int)row;
     const long long rows = std::min<long long>(args.n - row, (1 << 20) * G);
-    launch(token_loss_kernel<BF16, POLICY, ENT, NT, CH, G, REST>, dim3((unsigned)((rows + G - 1) / G)), dim3(NT * G), s, a);
+    launch(token_loss_kernel<BF16, POLICY, ENT, NT, CH, G, REST, OCC>, dim3((unsigned)((rows + G - 1) / G)), dim3(NT * G), s, a);
     const hipError_t st = hipGetLastError();
     if (st != hipSuccess) return st;
   }
@@ -845,11 +845,19 @@ hipError_t launch_loss_parts(const TokenLossArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Rows of up to 256 chunks share a wave (100000 x 1000 bf16: 236 us with 128 threads a row, 129 with 64, 115 with 32), up to 2048 stay
-// in registers.  Of longer ones a part does, which leaves room for more rows a compute unit, and the rest is read again from
-// a cache: 4096 x 30000 bf16 103 us with 2048 of 3750 chunks held, 108 with all, 105 with
-// none; 1500 x 50021 fp32 127 us with 4096 of 12506 held, 132 with 2048, 140 with none, 139 with all; 2047 x 131071 bf16
-// 243, 240, 249, 285.  Without a gradient a row is read once: 4096 x 30000 52 us in 512 threads, 88 in 1024.
+// Short rows share a wave, up to 256 chunks stay in registers; of longer ones a part does, so that more rows run at once, and
+// the rest is read again from a cache.  What bounds all of these is how many bytes are on their way, so registers are given
+// to the threads up to 8 or 6 waves a SIMD (OCC).  In us, taken and otherwise (threads a row x chunks held in each):
+//   40000 x 1000 bf16, 125 chunks     with entropy 16 x 8 46.9, 32 x 4 53.7, 32 x 8 56.3; without 32 x 4 41.5, 16 x 8 49.0
+//   40000 x 3200 bf16, 400 chunks     64 x 8 112, 128 x 4 114, 128 x 8 (all) 141; of 4096 rows 128 x 4 17.7, 64 x 8 18.4
+//   40000 x 8000 bf16, 1000 chunks    128 x 4 226, 64 x 8 239, 128 x 8 (all) 231
+//   8000 x 12000 bf16, 1500 chunks    256 x 4 83.7, 256 x 8 (all) 85.6
+//   8000 x 20000 bf16, 2500 chunks    256 x 8 128, 256 x 4 130, 512 x 4 154
+//   4096 x 30000 bf16, 3750 chunks    256 x 8 96.4, 512 x 4 95.7, 256 x 4 107
+//   4096 x 64000 bf16, 8000 chunks    512 x 6 200, 512 x 4 205, 512 x 8 in 5 waves a SIMD 215
+//   2000 x 30001 fp32, 7501 chunks    512 x 8 91.3, 512 x 6 94.7, in 5 waves a SIMD 101; 1500 x 50021 126, 128, 128
+//   900 x 30001 fp32                  512 x 3 49.2 (in 8 waves: four rows a unit at once, so all of them), 512 x 8 51.2
+// Without a gradient a row is read once: 20000 x 20000 133 us in 256 threads, 142 in 512; 4096 x 30000 52 in 512, 88 in 1024.
 template <int BF16, bool POLICY, bool ENT>
 hipError_t launch_loss_by_length(const TokenLossArgs& args, hipStream_t s) {
   TokenLossArgs a = args;
@@ -859,12 +867,19 @@ hipError_t launch_loss_by_length(const TokenLossArgs& args, hipStream_t s) {
   if (a.n_parts > 1) return launch_loss_parts<BF16, POLICY, ENT>(a, s);
   if (chunks <= 8 * 4) return launch_loss_rows<BF16, POLICY, ENT, 8, 4, 32, false>(a, s);
   if (chunks <= 16 * 4) return launch_loss_rows<BF16, POLICY, ENT, 16, 4, 16, false>(a, s);
-  if (chunks <= 32 * 8) return launch_loss_rows<BF16, POLICY, ENT, 32, 8, 8, false>(a, s);
-  if (chunks <= 128 * 8) return launch_loss_rows<BF16, POLICY, ENT, 128, 8, 1, false>(a, s);
+  if (chunks <= 16 * 8) {
+    if constexpr (ENT) return launch_loss_rows<BF16, POLICY, ENT, 16, 8, 16, false, 6>(a, s);
+    else return launch_loss_rows<BF16, POLICY, ENT, 32, 4, 8, false, 8>(a, s);
+  }
+  if (chunks <= 32 * 8) return launch_loss_rows<BF16, POLICY, ENT, 32, 8, 8, false, ENT ? 6 : 1>(a, s);
+  if (chunks <= 64 * 12 && a.n >= 32 * kUnits) return launch_loss_rows<BF16, POLICY, ENT, 64, 8, 1, true, 6>(a, s);
+  if (chunks <= 128 * 8) return launch_loss_rows<BF16, POLICY, ENT, 128, 4, 1, true, 8>(a, s);
+  if (!a.grad && chunks <= 256 * 12) return launch_loss_rows<BF16, POLICY, ENT, 256, 0, 1, true, 8>(a, s);
   if (!a.grad) return launch_loss_rows<BF16, POLICY, ENT, 512, 0, 1, true>(a, s);
-  if (chunks <= 256 * 8) return launch_loss_rows<BF16, POLICY, ENT, 256, 8, 1, false>(a, s);
-  if (chunks <= 512 * 8) return launch_loss_rows<BF16, POLICY, ENT, 512, 4, 1, true>(a, s);
-  return launch_loss_rows<BF16, POLICY, ENT, 512, 8, 1, true>(a, s);
+  if (chunks <= 256 * 8) return launch_loss_rows<BF16, POLICY, ENT, 256, 4, 1, true, 8>(a, s);
+  if (chunks <= 256 * 16) return launch_loss_rows<BF16, POLICY, ENT, 256, 8, 1, true, 6>(a, s);
+  if (a.n > 3 * kUnits && a.n <= 4 * kUnits) return launch_loss_rows<BF16, POLICY, ENT, 512, 3, 1, true, 8>(a, s);
+  return launch_loss_rows<BF16, POLICY, ENT, 512, BF16 ? 6 : 8, 1, true, 6>(a, s);
 }
 
 template <int BF16>

@@ -173,6 +173,36 @@ def test_token_logp_at_every_row_length(chunks, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,chunks", [(8195, 257), (8195, 768), (8195, 769), (600, 257), (600, 768), (600, 1024), (600, 1025), (600, 2048), (600, 2049), (600, 3071),
+                                      (600, 3073), (600, 4096), (600, 4097), (770, 4097), (1024, 5000), (1025, 4200), (600, 9000)])
+def test_whole_rows_of_many(n, chunks, dtype):
+    """Enough rows that none goes in parts, at both sides of the numbers of 16-byte chunks and of rows at which a row takes
+    other threads or registers; the rows repeat ten that differ, and equal rows on equal boundaries have equal results."""
+    V = 8 if dtype == "bf16" else 4
+    rng = np.random.default_rng(chunks)
+    for C in (chunks * V, chunks * V - 5):
+        rows, labels = lm_rows(rng, 10, C, dtype)
+        labels[:3] = (C - 1, 0, C - V)                       # in the last chunk, the first, and on their border
+        A, old, ref, g = policy_inputs(rng, rows, labels, 0.9, 0.2, 0.28)
+        at = np.arange(n) % 10
+        z = rows.to(DEV)[torch.from_numpy(at).to(DEV)]
+        sel = list(range(10)) + list(range(n - 10, n))
+        for ent in (0.02, 0.0):
+            h = g[at] * np.float32(ent) if ent else None
+            for grad in (True, False):
+                out = run_logp(z, labels[at], 0.9, A[at] if grad else None, h if grad else None, entropy=bool(ent), grad=grad)
+                check_logp(z[sel], labels[at][sel], 0.9, A[at][sel], None if h is None else h[sel],
+                           [o if o is None else o[sel] for o in out], dtype)
+                if C % V == 0:
+                    for o in out:
+                        assert o is None or torch.equal(o[10:n // 10 * 10].reshape(n // 10 - 1, -1),
+                                                        o[:10].reshape(1, -1).expand(n // 10 - 1, -1))
+            o = run_policy(z, labels[at], A[at], old[at], ref[at], g[at], 0.9, 0.2, 0.28, 0.05, ent)
+            check_policy(z[sel], labels[at][sel], A[at][sel], old[at][sel], ref[at][sel], g[at][sel], 0.9, 0.2, 0.28, 0.05, ent,
+                         {k: v[sel] for k, v in o.items()}, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("C", [5, 700, 90001, 200003])
 def test_token_logp_special_rows(C, dtype):
     low, high = float(torch.finfo(DT[dtype]).min), float(torch.finfo(DT[dtype]).max)

@@ -545,10 +545,10 @@ __device__ __forceinline__ Sums row_sums(const Row<BF16>& r, int first, int last
   return sums;
 }
 // The sums of a row's part p, chunks p per .. + per - 1, into *out.
-template <int BF16, bool ENT, bool PRECISE, int NT>
+template <int BF16, bool ENT, int NT>
 __device__ __forceinline__ void part_sums(const Row<BF16>& r, int p, int per, const Scale& s, Sums* out) {
   __shared__ Sums waves[NT / 64];
-  const Sums sums = row_sums<BF16, ENT, PRECISE, NT>(r, p * per + threadIdx.x, min(r.chunks, (p + 1) * per),
+  const Sums sums = row_sums<BF16, ENT, false, NT>(r, p * per + threadIdx.x, min(r.chunks, (p + 1) * per),
                                                      r.at(r.label), s, waves);
   if (threadIdx.x == 0) *out = sums;
 }
@@ -575,7 +575,7 @@ __global__ __launch_bounds__(NT) void token_parts_kernel(TokenLossArgs a) {
   bool weightless;
   const bool token = open_row<BF16, POLICY>(a, row, r, weightless);
   if (!token || (weightless && !(a.loss || a.logp || a.kl || a.entropy))) return;
-  part_sums<BF16, ENT, false, NT>(r, blockIdx.x, a.per_part, a.s, (Sums*)a.parts + (long long)row * a.n_parts + blockIdx.x);
+  part_sums<BF16, ENT, NT>(r, blockIdx.x, a.per_part, a.s, (Sums*)a.parts + (long long)row * a.n_parts + blockIdx.x);
 }
 
 // The outputs (by the first part) and a part's gradient.
@@ -625,17 +625,21 @@ __device__ __forceinline__ int offset_at(const PreferenceArgs& a, int i) {
   return (int)(at < 0 ? 0 : at > a.n ? a.n : at);
 }
 
-// The sums of all rows, a workgroup a part of a row in turn.
-template <int BF16, int NT>
-__global__ __launch_bounds__(NT) void preference_sums_kernel(PreferenceArgs a) {
-  const int end = offset_at(a, 2 * a.pairs);
-  for (int row = offset_at(a, 0) + blockIdx.y; row < end; row += gridDim.y) {
+// The sums of all rows, NT threads a part of a row in turn, G rows a workgroup (G > 1: up to a wave each).
+template <int BF16, int NT, int G>
+__global__ __launch_bounds__(NT * G) void preference_sums_kernel(PreferenceArgs a) {
+  static_assert(G == 1 || NT <= 64, "rows that share a workgroup have no barrier");
+  __shared__ Sums waves[NT > 64 ? NT / 64 : 1];
+  const int end = offset_at(a, 2 * a.pairs), tid = threadIdx.x % NT, p = blockIdx.x;
+  for (int row = offset_at(a, 0) + blockIdx.y * G + threadIdx.x / NT; row < end; row += gridDim.y * G) {
     const int label = a.labels[row];
     if ((unsigned)label >= (unsigned)a.C) continue;
     Row<BF16> r;
     r.init(a.logits, row * a.ld_row, a.C, label);
-    part_sums<BF16, false, true, NT>(r, blockIdx.x, a.per_part, a.s, (Sums*)a.parts + (long long)row * a.n_parts + blockIdx.x);
-    __syncthreads();
+    const Sums sums = row_sums<BF16, false, true, NT>(r, p * a.per_part + tid, min(r.chunks, (p + 1) * a.per_part), r.at(label), a.s,
+                                                      waves);
+    if (tid == 0) ((Sums*)a.parts)[(long long)row * a.n_parts + p] = sums;
+    if (NT > 64) __syncthreads();
   }
 }
 
@@ -782,16 +786,16 @@ __global__ __launch_bounds__(1024) void preference_few_kernel(PreferenceArgs a) 
   }
 }
 
-template <int BF16, int NT>
-__global__ __launch_bounds__(NT) void preference_grad_kernel(PreferenceArgs a) {
+template <int BF16, int NT, int G>
+__global__ __launch_bounds__(NT * G) void preference_grad_kernel(PreferenceArgs a) {
   constexpr int V = Row<BF16>::V;
-  const int end = offset_at(a, 2 * a.pairs);
-  for (int row = offset_at(a, 0) + blockIdx.y; row < end; row += gridDim.y) {
+  const int end = offset_at(a, 2 * a.pairs), tid = threadIdx.x % NT;
+  for (int row = offset_at(a, 0) + blockIdx.y * G + threadIdx.x / NT; row < end; row += gridDim.y * G) {
     const PreferenceRow f = a.rows[row];
     Row<BF16> r;
     r.init(a.logits, row * a.ld_row, a.C, a.labels[row]);
     char* const d_row = (char*)a.grad + row * a.ld_grad * (16 / V);
-    const int first = blockIdx.x * a.per_part + threadIdx.x, last = min(r.chunks, ((int)blockIdx.x + 1) * a.per_part);
+    const int first = blockIdx.x * a.per_part + tid, last = min(r.chunks, ((int)blockIdx.x + 1) * a.per_part);
     if (f.weight == 0.f) {
       for (int i = first; i < last; i += NT) r.zero_chunk(d_row, i);
       continue;
@@ -889,6 +893,17 @@ hipError_t launch_loss(const TokenLossArgs& a, hipStream_t s) {
   return ent ? launch_loss_by_length<BF16, false, true>(a, s) : launch_loss_by_length<BF16, false, false>(a, s);
 }
 
+template <int BF16, int NT, int G>
+hipError_t launch_preference_sums(const PreferenceArgs& a, hipStream_t s) {
+  launch(preference_sums_kernel<BF16, NT, G>, dim3(a.n_parts, std::min((a.n + G - 1) / G, kGridRows)), dim3(NT * G), s, a);
+  return hipGetLastError();
+}
+template <int BF16, int NT, int G>
+hipError_t launch_preference_grad(const PreferenceArgs& a, hipStream_t s) {
+  launch(preference_grad_kernel<BF16, NT, G>, dim3(a.n_parts, std::min((a.n + G - 1) / G, kGridRows)), dim3(NT * G), s, a);
+  return hipGetLastError();
+}
+
 template <int BF16>
 hipError_t launch_preference_of(const PreferenceArgs& args, hipStream_t s) {
   PreferenceArgs a = args;
@@ -902,15 +917,18 @@ hipError_t launch_preference_of(const PreferenceArgs& args, hipStream_t s) {
     launch(preference_few_kernel<BF16>, dim3(a.pairs), dim3(1024), s, a);
     return hipGetLastError();
   }
-  const unsigned rows = std::min(a.n, kGridRows);
-  launch(preference_sums_kernel<BF16, 256>, dim3(a.n_parts, rows), dim3(256), s, a);
-  hipError_t st = hipGetLastError();
+  // Threads of a row (and rows a workgroup) by its chunks.  Sums and gradient, in us for all three kernels, taken and otherwise:
+  // 64 pairs of 2 x 250 rows of 1000 bf16 52, with 256 and 512 threads 128; 32 of 5000 99 and 124, 16 of 10000 92 and 105, 16 of 2 x
+  // 100 of 10000 45 and 49; 16 of 8000 fp32 129, with 64 and 256 threads 134; 8 of 30000 bf16 132, with 64 threads for sums 135 and for both 140.
+  const bool short_rows = a.n_parts == 1 && chunks <= 1536;
+  hipError_t st = !short_rows ? launch_preference_sums<BF16, 256, 1>(a, s)
+                  : chunks <= 256 ? launch_preference_sums<BF16, 32, 8>(a, s) : launch_preference_sums<BF16, 64, 1>(a, s);
   if (st != hipSuccess) return st;
   launch(preference_pairs_kernel<BF16>, dim3(a.pairs), dim3(1024), s, a);
   st = hipGetLastError();
   if (st != hipSuccess || !a.grad) return st;
-  launch(preference_grad_kernel<BF16, 512>, dim3(a.n_parts, rows), dim3(512), s, a);
-  return hipGetLastError();
+  if (!short_rows) return launch_preference_grad<BF16, 512, 1>(a, s);
+  return chunks <= 1024 ? launch_preference_grad<BF16, 64, 4>(a, s) : launch_preference_grad<BF16, 256, 1>(a, s);
 }
 
 // Parts of a row at most: of fp32 values, which has more chunks.

@@ -575,6 +575,33 @@ def test_preference(C, t, lengths, mean, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("chunks", [30, 255, 257, 1024, 1025, 1536, 1537, 2049])
+def test_preference_of_many_rows(chunks, dtype):
+    """Enough rows for three launches and none in parts, at both sides of the numbers of 16-byte chunks at which a row takes
+    other threads; the pairs repeat one whose answers are checked, in rows on other boundaries."""
+    V = 8 if dtype == "bf16" else 4
+    rng = np.random.default_rng(chunks)
+    for C in (chunks * V, chunks * V - 5):
+        rows, labels = lm_rows(rng, 11, C, dtype)
+        labels[:3] = (C - 1, 0, C - V)
+        ref = np.array([ot.token_facts(host(rows[i]), y, 0.9)[0] if 0 <= y < C else 0.0 for i, y in enumerate(labels)])
+        ref = (ref + rng.standard_normal(11)).astype(np.float32)
+        pairs = 60
+        at = np.concatenate([[0], np.tile(np.arange(11), pairs), [0, 0]])
+        offsets = np.concatenate([[1], 1 + np.cumsum(np.tile([4, 7], pairs))])
+        z = rows.to(DEV)[torch.from_numpy(at).to(DEV)]
+        g = rng.standard_normal(pairs).astype(np.float32)
+        loss, scores, grad = run_preference(z, labels[at], offsets, ref[at], 0.9, 0.3, 0.1, True, g)
+        for p in (0, 1, pairs - 1):
+            r = slice(1 + 11 * p, 12 + 11 * p)
+            check_preference(z[r], labels, [0, 4, 11], ref, 0.9, 0.3, 0.1, True, g[p:p + 1],
+                             (loss[p:p + 1], scores[p:p + 1], grad[r]), dtype)
+        if C % V == 0:                                       # equal rows on equal boundaries
+            assert (loss == loss[0]).all() and (scores == scores[0]).all()
+        assert (grad[0] == -7).all() and (grad[-2:] == -7).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("t", [2.0 ** -20, 2.0 ** -12, 2.0 ** -8, 0.02, 0.03, 50.0, 2.0 ** 20])
 def test_preference_at_low_and_high_temperatures(t, dtype):
     """Logits near 0, whose label is just above or below the others: what a low temperature makes large differences of."""

@@ -12,8 +12,8 @@
 // has them from all rows of a pair and reads the logits twice.  Measured on an MI355X (a device copy moves 4.8 TB/s): 8192 x
 // 131072 bf16 log p and entropy 316 us (5.9 TB/s of what has a token), 4096 x 30000 bf16 policy loss with entropy and
 // gradient 102 us (4.5 TB/s; with a maximum that the sums follow 133), 1500 x 50021 fp32 125 us (4.5), 3 pairs of 2 x 880 rows
-// of 131071 bf16 738 us, of which the sums take 219 (5.6 TB/s; 273 with the exponents of fp32 rows) and the
-// gradient 516 (4.8 TB/s).  Pairs in groups that a cache might hold until their gradient is taken were slower (8
+// of 131071 bf16 738 us, of which the sums take 219 (5.5 TB/s; 273 with the exponents of fp32 rows) and the
+// gradient 516 (5.1 TB/s).  Pairs in groups that a cache might hold until their gradient is taken were slower (8
 // groups of 2 pairs of 2 x 500 x 30000 663 us, all at once 557).
 #include "tokens.h"
 
@@ -919,7 +919,8 @@ hipError_t launch_preference_of(const PreferenceArgs& args, hipStream_t s) {
   }
   // Threads of a row (and rows a workgroup) by its chunks.  Sums and gradient, in us for all three kernels, taken and otherwise:
   // 64 pairs of 2 x 250 rows of 1000 bf16 52, with 256 and 512 threads 128; 32 of 5000 99 and 124, 16 of 10000 92 and 105, 16 of 2 x
-  // 100 of 10000 45 and 49; 16 of 8000 fp32 129, with 64 and 256 threads 134; 8 of 30000 bf16 132, with 64 threads for sums 135 and for both 140.
+  // 100 of 10000 45 and 49; 16 of 8000 fp32 129, with 64 and 256 threads 134; 8 of 30000 bf16 132, with 64 threads for sums
+  // 135 and for both 140.
   const bool short_rows = a.n_parts == 1 && chunks <= 1536;
   hipError_t st = !short_rows ? launch_preference_sums<BF16, 256, 1>(a, s)
                   : chunks <= 256 ? launch_preference_sums<BF16, 32, 8>(a, s) : launch_preference_sums<BF16, 64, 1>(a, s);

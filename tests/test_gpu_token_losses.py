@@ -173,8 +173,9 @@ def test_token_logp_at_every_row_length(chunks, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
-@pytest.mark.parametrize("n,chunks", [(8195, 257), (8195, 768), (8195, 769), (600, 257), (600, 768), (600, 1024), (600, 1025), (600, 2048), (600, 2049), (600, 3071),
-                                      (600, 3073), (600, 4096), (600, 4097), (770, 4097), (1024, 5000), (1025, 4200), (600, 9000)])
+@pytest.mark.parametrize("n,chunks", [(8195, 257), (8195, 768), (8195, 769), (600, 257), (600, 768), (600, 1024), (600, 1025),
+                                      (600, 2048), (600, 2049), (600, 3071), (600, 3073), (600, 4096), (600, 4097), (770, 4097),
+                                      (1024, 5000), (1025, 4200), (600, 9000)])
 def test_whole_rows_of_many(n, chunks, dtype):
     """Enough rows that none goes in parts, at both sides of the numbers of 16-byte chunks and of rows at which a row takes
     other threads or registers; the rows repeat ten that differ, and equal rows on equal boundaries have equal results."""

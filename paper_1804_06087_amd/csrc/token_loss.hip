@@ -1,12 +1,11 @@
 // Log-probabilities of given tokens, the clipped policy loss and the preference loss with their
 // gradients (rafiki_tokens.h).
 //
-// With y_c = z_c s, s = log2(e) / T, l the row's label and the sums over all classes but l:
-//     R = sum 2^(y_c - r),  r any reference,   S = R 2^(r - t) + 2^(y_l - t),  t = max(r, y_l),
-//     1 - p_l = R 2^(r - t) / S,   log p_l = - log(1 + R 2^(r - y_l))  (y_l >= r; otherwise y_l - r - log(R + 2^(y_l - r))),
+// With x_c = (z_c - top) log2(e) / T, l the row's label, top the row's maximum and the sum over all classes but l:
+//     R = sum 2^x_c,   S = R + 2^x_l,   1 - p_l = R / S,   log p_l = ln 2 x_l - log S   (- log(1 + R) where the label is the maximum),
 // which keeps 1 - p_l and log p_l exact where p_l is near 1: a sum over all classes would have lost the others'.
-// The gradient is affine in log p under p:  dz_c = 2^(y_c - r) (f + f' (y_c - r)) for c != l, with f' = 0 without entropy.
-// With r = y_l, known before the row is read, the sums need no maximum and no second look at the row.
+// The gradient is affine in log p under p:  dz_c = 2^x_c (f + f' x_c) for c != l, with f' = 0 without entropy.
+// The maximum is the largest logit so far, the same in a wave: it grows a few times in a row, and the sums move with it.
 //
 // Bound by bytes: logits read once and the gradient written once, where the factors f are the row's own; a preference loss
 // has them from all rows of a pair and reads the logits twice.  Measured on an MI355X (a device copy moves 4.8 TB/s): 8192 x
@@ -23,8 +22,6 @@
 namespace rafiki {
 
 namespace {
-
-constexpr float kLn2 = 0.693147180559945f, kLog2e = 1.44269504088896f;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
@@ -83,8 +80,6 @@ __device__ __forceinline__ T wave_add(T v) {
   return v;
 }
 
-// The maximum as a reference for powers: an empty row has none and takes 0.
-__device__ __forceinline__ float reference(float top) { return top == -INFINITY ? 0.f : top; }
 // Exponents of 2 as factors of a power that is 0 below here: -inf would make it NaN.
 __device__ __forceinline__ float finite_log2(float x) { return fmaxf(x, -16384.f); }
 
@@ -166,187 +161,172 @@ struct Row {
   }
 };
 
-// Sums over classes, the label's apart: 2^x with x = (z - top) s, and of those times x.  A thread adds a chunk's in 32 bits and
+// The exponents x = (z - top) log2(e) / T of a row's classes, with roundings that go either way: log2(e) / T is a number of
+// fewer bits and a rest, since a scale rounded to fp32 would move every log p the same way.  log p is off by 1.5e-8 (fp32) to 3e-8
+// (bf16 logits) rms, 7e-8 at most; with x relative to the label's logit, up to 40 and in a rounded scale, a label 24 T below
+// the top was off by 8e-7 on average and up to 2.4e-6 (T = 0.71, 100 to 200003 classes).
+//   fp32: d = z - top,  x = d hi + d lo.
+//   bf16: x = y + y rest, y = z hi - top hi, which for hi of 16 bits are exact products.
+// lo and rest are positive, so that -inf stays -inf.  Classes 2^80 and more below `top` have no power with any scale.
+template <int BF16>
+struct Exponent {
+  float hi, lo, at;
+  __device__ __forceinline__ void relative_to(float top, const Scale& s) {
+    if constexpr (BF16 != 0) {
+      hi = fabsf(top) > 0x1p100f ? fminf(s.hi16, 1.f) : s.hi16;   // no overflow
+      lo = s.rest16;
+      at = top * hi;
+    } else {
+      hi = s.hi;
+      lo = s.lo;
+      at = top;
+    }
+  }
+  __device__ __forceinline__ float of(float z) const {
+    if constexpr (BF16 != 0) {
+      const float y = fmaf(z, hi, -at);
+      return fmaf(y, lo, y);
+    } else {
+      const float d = z - at;
+      return fmaf(d, hi, d * lo);
+    }
+  }
+};
+
+// Sums over classes, the label's apart: 2^x and of those times x.  A thread adds a chunk's in 32 bits and
 // the chunks in 64: unlikely classes by the thousand, each below the last bit of a likely one's sum, would be lost in 32
 // (log p of 131071 classes off by 1.4e-6 on average; the additions cost nothing that the loads do not hide).
 struct Sums {
   double sum, moment;
-  float top;
+  float top;                  // finite: with no class and no label above -inf, the least number
 };
+constexpr float kLeast = -0x1.fffffep127f;
+
 template <int V>
 __device__ __forceinline__ float tree_sum(const float v[V]) {
   if constexpr (V == 8) return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
   else return (v[0] + v[1]) + (v[2] + v[3]);
 }
-// The power of x = (z - ref) s.  PRECISE (fp32 values): what is rounded off x, by the difference, s and the product, into `lost`,
-// whose sum times ln 2 belongs to the sum of powers.
-template <bool PRECISE>
-__device__ __forceinline__ float term(float z, float ref, const Scale& s, float& x, float& lost) {
-  const float d = z - ref;
-  x = d * s.hi;
-  const float e = power2(x);
-  if constexpr (PRECISE) {
-    const float back = d - z;
-    const float off = fmaf((z - (d - back)) - (ref + back), s.hi, fmaf(d, s.lo, fmaf(d, s.hi, -x)));
-    lost = fmaf(e, fminf(off, 1.f), lost);                   // NaN where d = -inf and e = 0: 1
-  }
-  return e;
-}
-// Precise sums of bf16 values, in fewer instructions: with s = s16 + rest16, s16 of 16 bits, and a reference that is a multiple of
-// 1/8, z s16 - ref s16 is exact for the values that count, and 2^(d rest16) = 1 + ln 2 d rest16 to 1e-7, whose sum comes from
-// that of 2^x z.  Where T is so low that 1/16 would be more than a few powers of 2, the label's logit stays the reference: x is
-// rounded then, but the few classes that such a T leaves have no bias to add up.
-__device__ __forceinline__ float coarse(float z, float s16) {
-  return s16 <= 64.f && fabsf(z) < 16.f ? 0.125f * __builtin_rintf(8.f * z) : z;
+// The compiler's maximum makes NaN of loaded values quiet first, an instruction each.  A row with NaN may have any reference.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  asm("v_max3_f32 %0, %0, %1, %2" : "+v"(a) : "v"(b), "v"(c));
+  return a;
 }
 template <int V>
-__device__ __forceinline__ void add_chunk_bf16(Sums& a, float& weighted, const float z[V], float at, float s16) {
-  float e[V];
+__device__ __forceinline__ float chunk_max(const float v[V]) {
+  float top = v[0];
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    e[j] = power2(fmaf(z[j], s16, -at));
-    weighted = fmaf(e[j], fmaxf(z[j], -0x1.fffffep127f), weighted);   // 0 for -inf
-  }
-  a.sum += (double)tree_sum<V>(e);
+  for (int j = 1; j < V; j += 2) top = max3(top, v[j], v[j + 1 < V ? j + 1 : j]);
+  return top;
 }
-// Relative to the label's logit, which needs no maximum: what underflows beside the label's own 1 does not count, and while p_l
-// is above 2^-40 the powers that matter are below 2^40, whose exponents are rounded by 2^-19 at most.  A row of a less
-// likely label is summed again by add_chunk_any.
-template <int V, bool ENT, bool PRECISE>
-__device__ __forceinline__ void add_chunk(Sums& a, float& lost, const float z[V], float ref, const Scale& s) {
-  float e[V], m = 0.f;
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    float x;
-    e[j] = term<PRECISE>(z[j], ref, s, x, lost);
-    if constexpr (ENT) m = fmaf(e[j], finite_log2(x), m);
-  }
-  a.sum += (double)tree_sum<V>(e);
-  if constexpr (ENT) a.moment += (double)m;
-}
-__device__ __forceinline__ bool bounded(const Sums& a) { return a.sum < 0x1p40; }   // not NaN either
-// The same sums relative to `ref`.
+// The same sums relative to `top`, at least their own.  The step's power keeps what is rounded off its exponent.
 template <bool ENT>
-__device__ __forceinline__ Sums moved(Sums v, float ref, float s) {
-  const float step = (v.top - ref) * s;
-  const double grown = v.sum == 0.0 ? 0.0 : (double)power2(step);
-  if (ENT) v.moment = (v.moment + v.sum * (double)finite_log2(step)) * grown;
-  v.sum *= grown;
-  return v;
+__device__ __forceinline__ Sums moved(const Sums& v, float top, double s) {
+  if (v.sum == 0.0) return Sums{0.0, 0.0, top};
+  const double step = fmax(((double)v.top - (double)top) * s, -16384.0);
+  const float x = (float)step;
+  const double grown = (double)power2(x) * (1.0 + 0.6931471805599453 * (step - (double)x));
+  return Sums{v.sum * grown, ENT ? (v.moment + v.sum * step) * grown : 0.0, top};
 }
-// For any values: relative to the largest so far.
-template <int V, bool ENT>
-__device__ __forceinline__ void add_chunk_any(Sums& a, const float z[V], float s) {
-  float now = a.top;
-#pragma unroll
-  for (int j = 0; j < V; ++j) now = fmaxf(now, z[j]);
-  a = moved<ENT>(a, reference(now), s);
-  float e[V], m = 0.f;
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const float x = (z[j] - reference(now)) * s;
-    e[j] = power2(x);
-    if constexpr (ENT) m = fmaf(e[j], finite_log2(x), m);
+// A row's sums in W neighbouring lanes, which have the same `top`: the largest logit so far.
+template <int BF16, int W, bool ENT>
+struct RowSums {
+  static constexpr int V = Row<BF16>::V;
+  Sums a;
+  Exponent<BF16> x;
+  __device__ __forceinline__ void start(float top, const Scale& s) {
+    a = Sums{0.0, 0.0, top};
+    x.relative_to(top, s);
   }
-  a.sum += (double)tree_sum<V>(e);
-  if constexpr (ENT) a.moment += (double)m;
-  a.top = now;
-}
-// The sums of NT threads in each of them; a barrier if NT > 64, and before `waves` is used again.  With ANY the threads'
-// references differ.
-template <int NT, bool ENT, bool ANY>
-__device__ __forceinline__ Sums join(Sums a, float s, Sums* waves) {
-  constexpr int NW = NT / 64, W = NT < 64 ? NT : 64;
-  if constexpr (ANY) {
-    const float all = wave_max<W>(a.top);
-    a = moved<ENT>(a, reference(all), s);
-    a.top = all;
+  // A chunk in each lane.
+  __device__ __forceinline__ void add_any(const float z[V], const Scale& s) {
+    const float top = chunk_max<V>(z);
+    if (__any(top > a.top)) {
+      a = moved<ENT>(a, fmaxf(a.top, wave_max<W>(top)), s.s);
+      x.relative_to(a.top, s);
+    }
+    add(z);
   }
+  // The same of classes up to `top`.
+  __device__ __forceinline__ void add(const float z[V]) {
+    float e[V], m = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float t = x.of(z[j]);
+      e[j] = power2(t);
+      if constexpr (ENT) m = fmaf(e[j], finite_log2(t), m);
+    }
+    a.sum += (double)tree_sum<V>(e);
+    if constexpr (ENT) a.moment += (double)m;
+  }
+};
+// The sums of W lanes with tops of their own, in each of them.
+template <int W, bool ENT>
+__device__ __forceinline__ Sums join_any(Sums a, const Scale& s) {
+  a = moved<ENT>(a, wave_max<W>(a.top), s.s);
   a.sum = wave_add<W>(a.sum);
   if (ENT) a.moment = wave_add<W>(a.moment);
-  if constexpr (NW > 1) {
+  return a;
+}
+// The sums of NT threads, the same top in a wave: in each of them (NT <= 64), else in the first wave, behind a barrier.
+template <int NT, bool ENT>
+__device__ __forceinline__ Sums join(Sums a, const Scale& s, Sums* waves) {
+  constexpr int W = NT < 64 ? NT : 64;
+  a.sum = wave_add<W>(a.sum);
+  if (ENT) a.moment = wave_add<W>(a.moment);
+  if constexpr (NT > 64) {
+    constexpr int NW = NT / 64;
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = a;
     __syncthreads();
-    float top = a.top;
-    if constexpr (ANY) {
-#pragma unroll
-      for (int w = 0; w < NW; ++w) top = fmaxf(top, waves[w].top);
-    }
-    Sums r{0.0, 0.0, top};
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const Sums v = ANY ? moved<ENT>(waves[w], reference(top), s) : waves[w];
-      r.sum += v.sum;
-      r.moment += v.moment;
-    }
-    return r;
+    if (threadIdx.x < 64) a = join_any<NW, ENT>(waves[threadIdx.x % NW], s);
   }
   return a;
 }
 
-// What a row's sums and its label's logit say.
+// What a row's sums and its label's logit say.  64 bits: the difference of two logits may exceed fp32, and what follows
+// subtracts log p and H.
 struct RowFacts {
-  double logp;
-  float entropy;
-  float rest, p;              // 1 - p of the label, p of the label
-  // p of any class is 2^(x - shift) share, x as in the sums: shift is whole and share within 2^-1/2 .. 2^1/2, so that no
-  // factor of the gradient is smaller than a weight
-  float shift, share, log2_share;
+  double logp, entropy, ln_total;
+  double rest, p;             // 1 - p of the label, p of the label
+  double share;               // p of any class is 2^x share, x as in the sums; at least 1 / C
   bool defined;
 };
 template <bool ENT>
-__device__ __forceinline__ RowFacts row_facts(const Sums& r, float z, float s, double inv_t) {
+__device__ __forceinline__ RowFacts row_facts(const Sums& r, float z, double inv_t) {
   RowFacts f;
-  const float top = reference(r.top), t = reference(fmaxf(r.top, z));
-  const float down = finite_log2((top - t) * s), x = finite_log2((z - t) * s);
-  const double e_r = r.sum == 0.0 ? 0.0 : (double)power2(down), e_y = (double)power2((z - t) * s);
-  const double part = r.sum * e_r, total = part + e_y;
-  f.defined = total > 0.0 && total < INFINITY && t < INFINITY;
-  const double inv = 1.0 / total;
-  f.rest = (float)(part * inv);
-  f.p = (float)(e_y * inv);
-  // log p in 64 bits: the difference of two logits may exceed fp32, and what follows subtracts it
-  const double D = ((double)z - (double)top) * inv_t;
-  if (r.sum == 0.0) f.logp = 0.0;
-  else if (D >= 0) f.logp = -log1p(r.sum * (D > 0 ? exp(-D) : 1.0));
-  else f.logp = D - log(r.sum + exp(D));
-  const float log2_total = log2f((float)total), log2_p = down - log2_total;
-  f.shift = -__builtin_rintf(log2_p);
-  f.log2_share = log2_p + f.shift;
-  f.share = (float)inv * power2(down + f.shift);
-  f.entropy = 0.f;
+  const double D = ((double)z - (double)r.top) * inv_t, e_y = exp(D), total = r.sum + e_y;
+  f.defined = total > 0.0 && total < INFINITY;
+  f.share = 1.0 / total;
+  f.rest = r.sum * f.share;
+  f.p = e_y * f.share;
+  f.ln_total = D == 0.0 ? log1p(r.sum) : log(total);
+  f.logp = f.defined ? D - f.ln_total : NAN;
+  f.entropy = 0.0;
   if (ENT) {
-    const double ln_total = D >= 0 ? -f.logp : log(total);   // D >= 0: t = z
-    f.entropy = (float)(ln_total - 0.6931471805599453 * ((r.moment + r.sum * (double)down) * e_r + e_y * (double)x) * inv);
-    f.log2_share = (float)((double)down - ln_total * 1.4426950408889634 + (double)f.shift);
-  }
-  if (!f.defined) {
-    f.logp = NAN;
-    f.entropy = NAN;
+    const double own = e_y > 0.0 ? e_y * D : 0.0;
+    f.entropy = f.defined ? f.ln_total - (0.6931471805599453 * r.moment + own) * f.share : NAN;
   }
   return f;
 }
 
-// What the gradient pass needs: dz = 2^x (f0 + f1 x) with x = (z - top) s - shift, and the label's.
+// What the gradient pass needs: dz = 2^x (f0 + f1 x) with x = (z - top) s, and the label's.
 struct RowGrad {
-  float f0, f1, at_label, shift;
+  float f0, f1, at_label, top;
 };
 template <bool ENT>
-__device__ __forceinline__ RowGrad row_grad(const RowFacts& f, float a, float h, float inv_t) {
+__device__ __forceinline__ RowGrad row_grad(const RowFacts& f, float a, float h, float top, double inv_t) {
   if (!f.defined || !(fabsf(a) < INFINITY) || h != h) return RowGrad{NAN, 0.f, NAN, 0.f};
-  const float share = f.share * inv_t;
-  RowGrad g{share * -a, 0.f, a * f.rest * inv_t, f.shift};
-  if (ENT) {
-    g.f0 = share * (-a - h * (kLn2 * f.log2_share + f.entropy));
-    g.f1 = -share * h * kLn2;
-    if (f.p > 0.f) g.at_label -= h * f.p * ((float)f.logp + f.entropy) * inv_t;
-  }
-  return g;
+  const double share = f.share * inv_t;
+  if (!ENT) return RowGrad{(float)(-a * share), 0.f, (float)(a * f.rest * inv_t), top};
+  double at_label = a * f.rest;
+  if (f.p > 0.0) at_label -= h * f.p * (f.logp + f.entropy);
+  return RowGrad{(float)(share * (-a - h * (f.entropy - f.ln_total))), (float)(share * h * -0.6931471805599453),
+                 (float)(at_label * inv_t), top};
 }
 
 // What a loss makes of a row's facts: its outputs and the gradient's factors (in every thread that calls it).
 template <bool POLICY, bool ENT>
-__device__ __forceinline__ RowGrad finish_row(const TokenLossArgs& a, int row, const RowFacts& f, bool writes) {
+__device__ __forceinline__ RowGrad finish_row(const TokenLossArgs& a, int row, const RowFacts& f, float top, bool writes) {
   float da, dh;
   if constexpr (POLICY) {
     // 64 bits: r and exp(d) are powers of differences, and kl is what is left of them
@@ -368,7 +348,7 @@ __device__ __forceinline__ RowGrad finish_row(const TokenLossArgs& a, int row, c
         slope -= a.kl_coef * (beyond ? INFINITY : e);
       }
     }
-    if (a.entropy_coef != 0.0) loss -= a.entropy_coef * (double)f.entropy;
+    if (a.entropy_coef != 0.0) loss -= a.entropy_coef * f.entropy;
     if (!f.defined) loss = kl = NAN;
     if (writes) {
       if (a.loss) a.loss[row] = (float)loss;
@@ -383,9 +363,9 @@ __device__ __forceinline__ RowGrad finish_row(const TokenLossArgs& a, int row, c
   }
   if (writes) {
     if (a.logp) a.logp[row] = (float)f.logp;
-    if (a.entropy) a.entropy[row] = f.entropy;
+    if (a.entropy) a.entropy[row] = (float)f.entropy;
   }
-  return row_grad<ENT>(f, da, dh, (float)a.inv_t);
+  return row_grad<ENT>(f, da, dh, top, a.inv_t);
 }
 
 template <int BF16>
@@ -394,35 +374,38 @@ __device__ __forceinline__ u32x4 masked_chunk() {
   return u32x4{m, m, m, m};
 }
 
-// f(a chunk's values) for the chunks first, first + NT, .. below `last` of a row that is read for it, UN in flight (LAST: for the
-// last time, one chunk after another).
+// f(a chunk's values) for the chunks begin .. last - 1 of a row that is read for it, by NT threads, UN of each in flight (LAST: for
+// the last time, one chunk after another).  A wave's lanes call f together, some for a chunk of -inf behind the last.
 template <int BF16, bool LAST, int UN, int NT, typename F>
-__device__ __forceinline__ void for_chunks(const Row<BF16>& r, int first, int last, F&& f) {
+__device__ __forceinline__ void for_chunks(const Row<BF16>& r, int begin, int last, F&& f) {
   constexpr int V = Row<BF16>::V;
-  for (int i0 = first; i0 < last; i0 += NT * UN) {
+  const int lane = threadIdx.x % (NT < 64 ? NT : 64);
+  const int wave = NT > 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0;
+  for (int b = begin + wave * 64; b < last; b += NT * UN) {
     u32x4 q[UN];
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
       q[u] = masked_chunk<BF16>();
-      if (i0 + u * NT < last) q[u] = r.template load<LAST>(i0 + u * NT);
+      if (b + u * NT + lane < last) q[u] = r.template load<LAST>(b + u * NT + lane);
     }
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
+      if (u > 0 && b + u * NT >= last) break;
       float z[V];
       unpack<BF16, V>(q[u], z);
-      f(z, i0 + u * NT);
+      f(z, b + u * NT + lane);
     }
   }
 }
 
 // Chunk i's gradient from its values.
 template <int BF16, bool ENT>
-__device__ __forceinline__ void store_gradient(const Row<BF16>& r, char* row, int i, float z[Row<BF16>::V], float top, float s,
+__device__ __forceinline__ void store_gradient(const Row<BF16>& r, char* row, int i, float z[Row<BF16>::V], const Exponent<BF16>& x,
                                                const RowGrad& d) {
 #pragma unroll
   for (int j = 0; j < Row<BF16>::V; ++j) {
-    const float x = fmaf(z[j] - top, s, -d.shift);
-    z[j] = power2(x) * (ENT ? fmaf(d.f1, finite_log2(x), d.f0) : d.f0);
+    const float t = x.of(z[j]);
+    z[j] = power2(t) * (ENT ? fmaf(d.f1, finite_log2(t), d.f0) : d.f0);
   }
   r.store(row, i, z, d.at_label);
 }
@@ -447,7 +430,7 @@ __device__ __forceinline__ void no_token(const TokenLossArgs& a, int row) {
 // from its sums to its gradient, so that it is read once; CH = 0: any length, read again for the gradient.
 template <int BF16, bool POLICY, bool ENT, int NT, int CH, int G, bool REST, int OCC>
 __global__ __launch_bounds__(NT * G, OCC) void token_loss_kernel(TokenLossArgs a) {
-  constexpr int V = Row<BF16>::V, NW = (NT + 63) / 64;
+  constexpr int V = Row<BF16>::V, NW = (NT + 63) / 64, W = NT < 64 ? NT : 64;
   static_assert(G == 1 || NT <= 64, "rows that share a workgroup have no barrier");
   __shared__ Sums waves[NW];
   __shared__ RowGrad shared_grad;
@@ -481,25 +464,35 @@ __global__ __launch_bounds__(NT * G, OCC) void token_loss_kernel(TokenLossArgs a
         // opaque here, or the compiler keeps every pass's unpacked values for the next one
         asm volatile("" : "+v"(held[i][0]), "+v"(held[i][1]), "+v"(held[i][2]), "+v"(held[i][3]));
         unpack<BF16, V>(held[i], z);
-        f(z, i * NT + tid);
+        f(z, i * NT + tid, std::true_type{});
         __builtin_amdgcn_sched_barrier(0);                   // one chunk's values at a time in registers
       }
     }
-    if constexpr (REST) for_chunks<BF16, decltype(last)::value, (decltype(last)::value && CH != 0 ? 1 : 4), NT>(r, NT * CH + tid, r.chunks, f);
+    if constexpr (REST) {
+      for_chunks<BF16, decltype(last)::value, (decltype(last)::value && CH != 0 ? 1 : 4), NT>(
+          r, NT * CH, r.chunks, [&](float* z, int i) { f(z, i, std::false_type{}); });
+    }
   };
-  Sums sums{0.0, 0.0, z_label};
-  float lost = 0.f;
-  each(std::false_type{}, [&](const float* z, int) { add_chunk<V, ENT, false>(sums, lost, z, z_label, a.s); });
-  sums = join<NT, ENT, false>(sums, a.s.hi, waves);
-  if (!bounded(sums)) {                                      // the same in all of the row's threads
-    if constexpr (NW > 1) __syncthreads();
-    sums = Sums{0.0, 0.0, -INFINITY};
-    each(std::false_type{}, [&](const float* z, int) { add_chunk_any<V, ENT>(sums, z, a.s.hi); });
-    sums = join<NT, ENT, true>(sums, a.s.hi, waves);
+  RowSums<BF16, W, ENT> sum;
+  float top = fmaxf(z_label, kLeast);
+  if constexpr (CH > 0) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      float z[V];
+      unpack<BF16, V>(held[i], z);
+      top = fmaxf(top, chunk_max<V>(z));
+    }
+    top = wave_max<W>(top);
   }
+  sum.start(top, a.s);
+  each(std::false_type{}, [&](const float* z, int, auto in_registers) {
+    if constexpr (decltype(in_registers)::value) sum.add(z);
+    else sum.add_any(z, a.s);
+  });
+  const Sums sums = join<NT, ENT>(sum.a, a.s, waves);
   RowGrad d{};
   if (NW == 1 || threadIdx.x < 64) {
-    d = finish_row<POLICY, ENT>(a, row, row_facts<ENT>(sums, z_label, a.s.hi, a.inv_t), tid == 0);
+    d = finish_row<POLICY, ENT>(a, row, row_facts<ENT>(sums, z_label, a.inv_t), sums.top, tid == 0);
     if (NW > 1 && tid == 0) shared_grad = d;
   }
   if (!a.grad || weightless) return;
@@ -507,65 +500,42 @@ __global__ __launch_bounds__(NT * G, OCC) void token_loss_kernel(TokenLossArgs a
     __syncthreads();
     d = shared_grad;
   }
-  const float top = reference(sums.top);
-  each(std::true_type{}, [&](float* z, int i) {
-    if (i < r.chunks) store_gradient<BF16, ENT>(r, d_row, i, z, top, a.s.hi, d);
+  Exponent<BF16> x;
+  x.relative_to(d.top, a.s);
+  each(std::true_type{}, [&](float* z, int i, auto) {
+    if (i < r.chunks) store_gradient<BF16, ENT>(r, d_row, i, z, x, d);
   });
 }
 
 // ---------------------------------------------------------------- rows in parts
 
-// The sums over a row's chunks first, first + NT, .. below `last`, joined over NT threads.
-template <int BF16, bool ENT, bool PRECISE, int NT>
-__device__ __forceinline__ Sums row_sums(const Row<BF16>& r, int first, int last, float z_label, const Scale& s, Sums* waves) {
-  constexpr int V = Row<BF16>::V;
-  Sums sums{0.0, 0.0, z_label};
-  float lost = 0.f;
-  if constexpr (BF16 != 0 && PRECISE) {
-    static_assert(!ENT, "without entropy");
-    sums.top = coarse(z_label, s.s16);
-    const float at = sums.top * s.s16;                       // exact
-    if (fabsf(at) <= 0x1p20f) {
-      for_chunks<BF16, false, 4, NT>(r, first, last, [&](const float* z, int) { add_chunk_bf16<V>(sums, lost, z, at, s.s16); });
-      sums.sum += (double)(kLn2 * s.rest16) * ((double)lost - (double)sums.top * sums.sum);
-    } else {
-      sums.sum = INFINITY;
-    }
-  } else {
-    for_chunks<BF16, false, 4, NT>(r, first, last, [&](const float* z, int) { add_chunk<V, ENT, PRECISE>(sums, lost, z, z_label, s); });
-    if (PRECISE) sums.sum += (double)(kLn2 * lost);
-  }
-  sums = join<NT, ENT, false>(sums, s.hi, waves);
-  if (!bounded(sums)) {
-    if (NT > 64) __syncthreads();
-    sums = Sums{0.0, 0.0, -INFINITY};
-    for_chunks<BF16, false, 4, NT>(r, first, last, [&](const float* z, int) { add_chunk_any<V, ENT>(sums, z, s.hi); });
-    sums = join<NT, ENT, true>(sums, s.hi, waves);
-  }
-  return sums;
+// The sums over a row's chunks begin .. last - 1, joined over NT threads.
+template <int BF16, bool ENT, int NT>
+__device__ __forceinline__ Sums row_sums(const Row<BF16>& r, int begin, int last, float z_label, const Scale& s, Sums* waves) {
+  RowSums<BF16, (NT < 64 ? NT : 64), ENT> sum;
+  sum.start(fmaxf(z_label, kLeast), s);
+  for_chunks<BF16, false, 4, NT>(r, begin, last, [&](const float* z, int) { sum.add_any(z, s); });
+  return join<NT, ENT>(sum.a, s, waves);
 }
 // The sums of a row's part p, chunks p per .. + per - 1, into *out.
 template <int BF16, bool ENT, int NT>
 __device__ __forceinline__ void part_sums(const Row<BF16>& r, int p, int per, const Scale& s, Sums* out) {
   __shared__ Sums waves[NT / 64];
-  const Sums sums = row_sums<BF16, ENT, false, NT>(r, p * per + threadIdx.x, min(r.chunks, (p + 1) * per),
-                                                     r.at(r.label), s, waves);
+  const Sums sums = row_sums<BF16, ENT, NT>(r, p * per, min(r.chunks, (p + 1) * per), r.at(r.label), s, waves);
   if (threadIdx.x == 0) *out = sums;
 }
 // A row's sums from its parts', in every lane of a wave.
 template <bool ENT>
-__device__ __forceinline__ Sums join_parts(const Sums* parts, int n, float s) {
-  const int lane = threadIdx.x & 63;
-  Sums a{0.0, 0.0, -INFINITY};
-  for (int p = lane; p < n; p += 64) {
-    Sums b = parts[p];
-    const float top = fmaxf(a.top, b.top);
-    const float ref = reference(top);
-    a = moved<ENT>(a, ref, s);
-    b = moved<ENT>(b, ref, s);
-    a = Sums{a.sum + b.sum, a.moment + b.moment, top};
+__device__ __forceinline__ Sums join_parts(const Sums* parts, int n, const Scale& s) {
+  Sums a{0.0, 0.0, kLeast};
+  for (int p = threadIdx.x & 63; p < n; p += 64) {
+    const float top = fmaxf(a.top, parts[p].top);
+    const Sums b = moved<ENT>(parts[p], top, s.s);
+    a = moved<ENT>(a, top, s.s);
+    a.sum += b.sum;
+    a.moment += b.moment;
   }
-  return join<64, ENT, true>(a, s, nullptr);
+  return join_any<64, ENT>(a, s);
 }
 
 template <int BF16, bool POLICY, bool ENT, int NT>
@@ -583,16 +553,15 @@ template <int BF16, bool POLICY, bool ENT, int NT>
 __global__ __launch_bounds__(NT) void token_parts_grad_kernel(TokenLossArgs a) {
   constexpr int V = Row<BF16>::V;
   __shared__ RowGrad shared_grad;
-  __shared__ float shared_top;
   const int row = a.row0 + blockIdx.y, p = blockIdx.x;
   Row<BF16> r;
   bool weightless;
   const bool token = open_row<BF16, POLICY>(a, row, r, weightless);
-  const int first = p * a.per_part + threadIdx.x, last = min(r.chunks, (p + 1) * a.per_part);
+  const int begin = p * a.per_part, last = min(r.chunks, begin + a.per_part);
   char* const d_row = (char*)a.grad + row * a.ld_grad * (16 / V);
   if (!token || weightless) {
     if (a.grad)
-      for (int i = first; i < last; i += NT) r.zero_chunk(d_row, i);
+      for (int i = begin + threadIdx.x; i < last; i += NT) r.zero_chunk(d_row, i);
     if (!token) {
       if (p == 0 && threadIdx.x == 0) no_token(a, row);
       return;
@@ -600,20 +569,18 @@ __global__ __launch_bounds__(NT) void token_parts_grad_kernel(TokenLossArgs a) {
     if (p > 0 || !(a.loss || a.logp || a.kl || a.entropy)) return;
   }
   if (threadIdx.x < 64) {
-    const Sums sums = join_parts<ENT>((const Sums*)a.parts + (long long)row * a.n_parts, a.n_parts, a.s.hi);
-    const float z_label = r.at(r.label);
-    const RowGrad d = finish_row<POLICY, ENT>(a, row, row_facts<ENT>(sums, z_label, a.s.hi, a.inv_t), p == 0 && threadIdx.x == 0);
-    if (threadIdx.x == 0) {
-      shared_grad = d;
-      shared_top = reference(sums.top);
-    }
+    const Sums sums = join_parts<ENT>((const Sums*)a.parts + (long long)row * a.n_parts, a.n_parts, a.s);
+    const RowFacts f = row_facts<ENT>(sums, r.at(r.label), a.inv_t);
+    const RowGrad d = finish_row<POLICY, ENT>(a, row, f, sums.top, p == 0 && threadIdx.x == 0);
+    if (threadIdx.x == 0) shared_grad = d;
   }
   if (!a.grad || weightless) return;
   __syncthreads();
   const RowGrad d = shared_grad;
-  const float top = shared_top;
-  for_chunks<BF16, true, 1, NT>(r, first, last, [&](float* z, int i) {
-    if (i < last) store_gradient<BF16, ENT>(r, d_row, i, z, top, a.s.hi, d);
+  Exponent<BF16> x;
+  x.relative_to(d.top, a.s);
+  for_chunks<BF16, true, 1, NT>(r, begin, last, [&](float* z, int i) {
+    if (i < last) store_gradient<BF16, ENT>(r, d_row, i, z, x, d);
   });
 }
 
@@ -636,11 +603,14 @@ __global__ __launch_bounds__(NT * G) void preference_sums_kernel(PreferenceArgs 
     if ((unsigned)label >= (unsigned)a.C) continue;
     Row<BF16> r;
     r.init(a.logits, row * a.ld_row, a.C, label);
-    const Sums sums = row_sums<BF16, false, true, NT>(r, p * a.per_part + tid, min(r.chunks, (p + 1) * a.per_part), r.at(label), a.s,
-                                                      waves);
+    const Sums sums = row_sums<BF16, false, NT>(r, p * a.per_part, min(r.chunks, (p + 1) * a.per_part), r.at(label), a.s, waves);
     if (tid == 0) ((Sums*)a.parts)[(long long)row * a.n_parts + p] = sums;
     if (NT > 64) __syncthreads();
   }
+}
+
+__device__ __forceinline__ PreferenceRow preference_row(const Sums& sums, const RowFacts& f) {
+  return PreferenceRow{sums.top, f.defined ? (float)f.share : NAN, f.defined ? (float)f.rest : NAN, 0.f};
 }
 
 // A pair's outputs (where `writes`) and its answers' weights, dL / d log p of a token over T, from NW waves' sums of
@@ -698,19 +668,15 @@ __global__ __launch_bounds__(1024) void preference_pairs_kernel(PreferenceArgs a
     const float z = element<BF16>((const char*)a.logits + row * a.ld_row * (BF16 ? 2 : 4), label);
     const Sums* parts = (const Sums*)a.parts + (long long)row * a.n_parts;
     Sums all = parts[0];
-    for (int q = 1; q < a.n_parts; ++q) {
-      Sums b = parts[q];
-      const float top = fmaxf(all.top, b.top), ref = reference(top);
-      all = moved<false>(all, ref, a.s.hi);
-      b = moved<false>(b, ref, a.s.hi);
-      all = Sums{all.sum + b.sum, 0.0, top};
+    if (a.n_parts > 1) {
+#pragma unroll 8
+      for (int q = 1; q < a.n_parts; ++q) all.top = fmaxf(all.top, parts[q].top);
+      all.sum = 0.0;
+#pragma unroll 8
+      for (int q = 0; q < a.n_parts; ++q) all.sum += moved<false>(parts[q], all.top, a.s.s).sum;
     }
-    const RowFacts f = row_facts<false>(all, z, a.s.hi, a.inv_t);
-    PreferenceRow& out = a.rows[row];
-    out.top = reference(all.top);
-    out.shift = f.shift;
-    out.share = f.defined ? f.share : NAN;
-    out.rest = f.defined ? f.rest : NAN;
+    const RowFacts f = row_facts<false>(all, z, a.inv_t);
+    a.rows[row] = preference_row(all, f);
     const double delta = f.logp - (a.ref_logp ? (double)a.ref_logp[row] : 0.0);
     if (row < middle) sum[0] += delta, ++tokens[0];
     else sum[1] += delta, ++tokens[1];
@@ -747,15 +713,9 @@ __global__ __launch_bounds__(1024) void preference_few_kernel(PreferenceArgs a) 
     r.init(a.logits, row * a.ld_row, a.C, a.labels[row]);
     if ((unsigned)r.label >= (unsigned)a.C) continue;
     const float z_label = r.at(r.label);
-    const Sums all = row_sums<BF16, false, true, 64>(r, lane, r.chunks, z_label, a.s, nullptr);
-    const RowFacts f = row_facts<false>(all, z_label, a.s.hi, a.inv_t);
-    if (lane == 0) {
-      PreferenceRow& out = a.rows[row];
-      out.top = reference(all.top);
-      out.shift = f.shift;
-      out.share = f.defined ? f.share : NAN;
-      out.rest = f.defined ? f.rest : NAN;
-    }
+    const Sums all = row_sums<BF16, false, 64>(r, 0, r.chunks, z_label, a.s, nullptr);
+    const RowFacts f = row_facts<false>(all, z_label, a.inv_t);
+    if (lane == 0) a.rows[row] = preference_row(all, f);
     const double delta = f.logp - (a.ref_logp ? (double)a.ref_logp[row] : 0.0);
     if (row < middle) sum[0] += delta, ++tokens[0];
     else sum[1] += delta, ++tokens[1];
@@ -779,9 +739,11 @@ __global__ __launch_bounds__(1024) void preference_few_kernel(PreferenceArgs a) 
       continue;
     }
     const PreferenceRow f = a.rows[row];
-    const RowGrad d{-w * f.share, 0.f, w * f.rest, f.shift};
-    for_chunks<BF16, true, 1, 64>(r, lane, r.chunks, [&](float* z, int i) {
-      if (i < r.chunks) store_gradient<BF16, false>(r, d_row, i, z, f.top, a.s.hi, d);
+    const RowGrad d{-w * f.share, 0.f, w * f.rest, f.top};
+    Exponent<BF16> x;
+    x.relative_to(f.top, a.s);
+    for_chunks<BF16, true, 1, 64>(r, 0, r.chunks, [&](float* z, int i) {
+      if (i < r.chunks) store_gradient<BF16, false>(r, d_row, i, z, x, d);
     });
   }
 }
@@ -795,14 +757,16 @@ __global__ __launch_bounds__(NT * G) void preference_grad_kernel(PreferenceArgs 
     Row<BF16> r;
     r.init(a.logits, row * a.ld_row, a.C, a.labels[row]);
     char* const d_row = (char*)a.grad + row * a.ld_grad * (16 / V);
-    const int first = blockIdx.x * a.per_part + tid, last = min(r.chunks, ((int)blockIdx.x + 1) * a.per_part);
+    const int begin = blockIdx.x * a.per_part, last = min(r.chunks, begin + a.per_part);
     if (f.weight == 0.f) {
-      for (int i = first; i < last; i += NT) r.zero_chunk(d_row, i);
+      for (int i = begin + tid; i < last; i += NT) r.zero_chunk(d_row, i);
       continue;
     }
-    const RowGrad d{-f.weight * f.share, 0.f, f.weight * f.rest, f.shift};
-    for_chunks<BF16, true, 1, NT>(r, first, last, [&](float* z, int i) {
-      if (i < last) store_gradient<BF16, false>(r, d_row, i, z, f.top, a.s.hi, d);
+    const RowGrad d{-f.weight * f.share, 0.f, f.weight * f.rest, f.top};
+    Exponent<BF16> x;
+    x.relative_to(f.top, a.s);
+    for_chunks<BF16, true, 1, NT>(r, begin, last, [&](float* z, int i) {
+      if (i < last) store_gradient<BF16, false>(r, d_row, i, z, x, d);
     });
   }
 }

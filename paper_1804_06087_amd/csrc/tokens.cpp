@@ -4,6 +4,7 @@
 #include "greedy.h"
 #include "tokens.h"
 
+#include <algorithm>
 #include <cmath>
 #include <string>
 
@@ -62,13 +63,15 @@ Args row_args(const void* logits, long long ld_row, int n, int n_classes, const 
   a.C = n_classes;
   a.labels = labels;
   a.inv_t = 1.0 / temperature;
-  const double s = 1.4426950408889634 / temperature;
-  a.s.hi = (float)s;
-  a.s.lo = (float)(s - (double)a.s.hi);
+  a.s.s = 1.4426950408889634 / temperature;
   int exponent;
-  const double bits = std::frexp(s, &exponent);              // in [1/2, 1)
-  a.s.s16 = (float)std::ldexp(std::rint(std::ldexp(bits, 16)), exponent - 16);
-  a.s.rest16 = (float)(s - (double)a.s.s16);
+  const double bits = std::frexp(a.s.s, &exponent);          // in [1/2, 1)
+  auto first = [&](int n) { return std::ldexp(std::floor(std::ldexp(bits, n)), exponent - n); };
+  const double tiny = 0x1p-60;                               // the rests are positive (see token_loss.hip)
+  a.s.hi = (float)first(24);
+  a.s.lo = (float)std::max(a.s.s - (double)a.s.hi, tiny * a.s.s);
+  a.s.hi16 = (float)first(16);
+  a.s.rest16 = (float)std::max((a.s.s - (double)a.s.hi16) / (double)a.s.hi16, tiny);
   a.grad = grad_logits;
   a.ld_grad = ld_grad;
   return a;

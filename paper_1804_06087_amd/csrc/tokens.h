@@ -69,9 +69,10 @@ struct FcI8Args {
   int* partial;               // [splits][n][c_out] int32 sums (splits > 1)
 };
 
-// log2(e) / T in fp32 and what that leaves of it; the first 16 bits of it and the rest.
+// log2(e) / T in 64 bits; its first 24 bits and the rest; its first 16 bits and the rest relative to them.
 struct Scale {
-  float hi, lo, s16, rest16;
+  double s;
+  float hi, lo, hi16, rest16;
 };
 struct TokenLossArgs {
   const void* logits;
@@ -99,7 +100,7 @@ struct TokenLossArgs {
 };
 
 struct PreferenceRow {        // of the workspace
-  float top, shift, share;    // p of a class is 2^((z - top) s - shift) share
+  float top, share;           // p of a class is 2^((z - top) s) share
   float rest;                 // 1 - p of the label
   float weight;               // dL / d log p over T
 };

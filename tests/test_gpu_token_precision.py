@@ -1,0 +1,107 @@
+"""How precise the losses over given tokens are, on the GPU against 64 bits: log-probabilities without a bias and a KL term that
+keeps its digits next to the reference.
+
+What 32 bits lose here, relative to a class's power 2^x, x = (z - the row's maximum) log2(e) / T in units of powers: the
+difference and the product are rounded, 2^-24 |x| ln 2 each; the power is off by one unit, 2^-23; a chunk's additions by 2^-24 each,
+three in a row; a move of a sum to another maximum, in a row and where its parts are joined, by a unit each.  Together
+2^-23 (4.5 + |ln of the power|)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_1804_06087_amd import binding as bd
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+DT = {"fp32": torch.float32, "bf16": torch.bfloat16}
+T = 0.71                                                     # log2(e) / T is 3e-8 of itself away from an fp32 number
+
+
+def full(*shape, dtype=torch.float32):
+    return torch.full(shape, -7, dtype=dtype, device=DEV)
+
+
+def rows_of(n, C, dtype, gap, seed):
+    """Logits [n, C] of a language model, and labels about `gap` T below the row's likeliest class."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    z = torch.randn((n, C), device=DEV, generator=g) * 1.5
+    at = torch.randint(0, C, (n, 40), device=DEV, generator=g)
+    z.scatter_(1, at, 8 + 8 * torch.rand((n, 40), device=DEV, generator=g))
+    labels = torch.randint(0, C, (n,), device=DEV, generator=g)
+    z.scatter_(1, labels[:, None], z.amax(1, keepdim=True) - gap * T - torch.rand((n, 1), device=DEV, generator=g))
+    return z.to(DT[dtype]), labels.int()
+
+
+class Exact:
+    """log p [n] of the labels in 64 bits, and the bound of a row's error by the rule above."""
+
+    def __init__(self, z, labels, t=T):
+        n = z.shape[0]
+        self.logp, self.bound = (torch.empty(n, dtype=torch.float64, device=DEV) for _ in range(2))
+        step = max(1, (1 << 26) // z.shape[1])
+        for i in range(0, n, step):
+            x = z[i:i + step].double() / t
+            log_p = torch.log_softmax(x, 1)
+            self.logp[i:i + step] = log_p.gather(1, labels[i:i + step, None].long())[:, 0]
+            below = log_p.amax(1, keepdim=True) - log_p
+            self.bound[i:i + step] = 2.0 ** -23 * (4.5 + (log_p.exp() * below.clamp(max=1e4)).sum(1))
+
+    def check(self, delta):
+        """Errors delta [n] of log p: every one within its row's bound; on average, since roundings go either way, within half a
+        unit of the power (which may have a side) and four deviations of that average."""
+        assert (delta.abs() <= self.bound).all(), (delta / self.bound).abs().max()
+        deviation = self.bound.square().mean().sqrt().item() / math.sqrt(3 * delta.numel())
+        assert abs(delta.mean().item()) <= 2.0 ** -24 + 4 * deviation, (delta.mean().item(), deviation)
+
+
+# rows in a wave, in several, in many with the rest read again, and in parts
+KINDS = [(500, 100), (500, 1000), (500, 2300), (300, 9000), (300, 30001), (64, 131071), (600, 50021), (600, 131072), (9, 200003)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,C", KINDS)
+@pytest.mark.parametrize("gap", [0.0, 4.0, 24.0])
+def test_kl_next_to_the_reference(n, C, gap, dtype):
+    """kl = exp(d) - d - 1 with d near 0.01: log p off by delta changes it by (exp(d) - 1) delta, and the fp32 result is rounded
+    by 2^-24 of 5e-5, 3e-10 of log p."""
+    z, labels = rows_of(n, C, dtype, gap, n + C)
+    exact = Exact(z, labels)
+    ref = (exact.logp + 0.01 * (1 + torch.rand(n, device=DEV, dtype=torch.float64))).float()
+    d = ref.double() - exact.logp
+    want = torch.expm1(d) - d
+    for ent in (0.0, 0.01):
+        for grad in (True, False):
+            kl, loss = full(n), full(n)
+            bd.policy_loss(z, labels, torch.ones(n, device=DEV), loss, torch.empty_like(z) if grad else None, ref_logp=ref,
+                           out_kl=kl, temperature=T, kl_coef=0.1, entropy_coef=ent)
+            exact.check((want - kl.double()) / torch.expm1(d))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,C", KINDS)
+def test_log_p_has_no_bias(n, C, dtype):
+    z, labels = rows_of(n, C, dtype, 24.0, n + C + 1)
+    exact = Exact(z, labels)
+    for entropy in (True, False):
+        logp = full(n)
+        bd.token_logp(z, labels, logp, full(n) if entropy else None, temperature=T)
+        rounded = exact.logp.abs().max().item() * 2.0 ** -24
+        delta = logp.double() - exact.logp
+        exact.bound += rounded
+        exact.check(delta)
+        exact.bound -= rounded
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,C", KINDS)
+def test_preference_scores_next_to_the_reference(n, C, dtype):
+    """Scores of one token each: beta (log p - ref), whose fp32 rounding is 2^-24 of the difference."""
+    n -= n % 2
+    z, labels = rows_of(n, C, dtype, 24.0, n + C + 2)
+    exact = Exact(z, labels)
+    ref = exact.logp.float()
+    scores = full(n // 2, 2)
+    bd.preference_loss(z, labels, None, None, n_pairs=n // 2, ref_logp=ref, out_scores=scores, temperature=T, beta=0.5)
+    exact.check(scores.double().view(-1) / 0.5 - (exact.logp - ref.double()))

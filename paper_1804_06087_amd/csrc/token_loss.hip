@@ -196,9 +196,14 @@ struct Exponent {
 // Sums over classes, the label's apart: 2^x and of those times x.  A thread adds a chunk's in 32 bits and
 // the chunks in 64: unlikely classes by the thousand, each below the last bit of a likely one's sum, would be lost in 32
 // (log p of 131071 classes off by 1.4e-6 on average; the additions cost nothing that the loads do not hide).
+//
+// The entropy of a row that is nearly sure, H = log S - ln 2 sum 2^x x / S, is all in the classes below the maximum, whose power is
+// 1 and whose x is 0.  With entropy (ENT) those powers are counted apart, so that nothing is lost beside them: both terms are
+// positive, log S = log(1 + the rest), and H keeps its digits however small it is.
 struct Sums {
   double sum, moment;
   float top;                  // finite: with no class and no label above -inf, the least number
+  float ones;                 // ENT: classes at the top, which `sum` leaves out; otherwise 0
 };
 constexpr float kLeast = -0x1.fffffep127f;
 
@@ -222,11 +227,13 @@ __device__ __forceinline__ float chunk_max(const float v[V]) {
 // The same sums relative to `top`, at least their own.  The step's power keeps what is rounded off its exponent.
 template <bool ENT>
 __device__ __forceinline__ Sums moved(const Sums& v, float top, double s) {
-  if (v.sum == 0.0) return Sums{0.0, 0.0, top};
+  if (top == v.top) return v;
+  const double sum = v.sum + (ENT ? (double)v.ones : 0.0);
+  if (sum == 0.0) return Sums{0.0, 0.0, top, 0.f};
   const double step = fmax(((double)v.top - (double)top) * s, -16384.0);
   const float x = (float)step;
   const double grown = (double)power2(x) * (1.0 + 0.6931471805599453 * (step - (double)x));
-  return Sums{v.sum * grown, ENT ? (v.moment + v.sum * step) * grown : 0.0, top};
+  return Sums{sum * grown, ENT ? (v.moment + sum * step) * grown : 0.0, top, 0.f};
 }
 // A row's sums in W neighbouring lanes, which have the same `top`: the largest logit so far.
 template <int BF16, int W, bool ENT>
@@ -235,7 +242,7 @@ struct RowSums {
   Sums a;
   Exponent<BF16> x;
   __device__ __forceinline__ void start(float top, const Scale& s) {
-    a = Sums{0.0, 0.0, top};
+    a = Sums{0.0, 0.0, top, 0.f};
     x.relative_to(top, s);
   }
   // A chunk in each lane.
@@ -256,8 +263,20 @@ struct RowSums {
       e[j] = power2(t);
       if constexpr (ENT) m = fmaf(e[j], finite_log2(t), m);
     }
-    a.sum += (double)tree_sum<V>(e);
-    if constexpr (ENT) a.moment += (double)m;
+    float sum = tree_sum<V>(e);
+    if constexpr (ENT) {
+      a.moment += (double)m;
+      asm volatile("" : "+v"(a.moment));                     // or the compiler sinks it behind the branches, with all of its terms
+      if (__any(sum >= 1.f)) {                               // else none of them is 1
+        float below[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) below[j] = __builtin_amdgcn_fractf(e[j]);   // 0 of 1, else e[j]
+        const float rest = tree_sum<V>(below);
+        a.ones += __builtin_rintf(sum - rest);
+        sum = rest;
+      }
+    }
+    a.sum += (double)sum;
   }
 };
 // The sums of W lanes with tops of their own, in each of them.
@@ -265,7 +284,7 @@ template <int W, bool ENT>
 __device__ __forceinline__ Sums join_any(Sums a, const Scale& s) {
   a = moved<ENT>(a, wave_max<W>(a.top), s.s);
   a.sum = wave_add<W>(a.sum);
-  if (ENT) a.moment = wave_add<W>(a.moment);
+  if (ENT) a.moment = wave_add<W>(a.moment), a.ones = wave_add<W>(a.ones);
   return a;
 }
 // The sums of NT threads, the same top in a wave: in each of them (NT <= 64), else in the first wave, behind a barrier.
@@ -273,7 +292,7 @@ template <int NT, bool ENT>
 __device__ __forceinline__ Sums join(Sums a, const Scale& s, Sums* waves) {
   constexpr int W = NT < 64 ? NT : 64;
   a.sum = wave_add<W>(a.sum);
-  if (ENT) a.moment = wave_add<W>(a.moment);
+  if (ENT) a.moment = wave_add<W>(a.moment), a.ones = wave_add<W>(a.ones);
   if constexpr (NT > 64) {
     constexpr int NW = NT / 64;
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = a;
@@ -294,12 +313,17 @@ struct RowFacts {
 template <bool ENT>
 __device__ __forceinline__ RowFacts row_facts(const Sums& r, float z, double inv_t) {
   RowFacts f;
-  const double D = ((double)z - (double)r.top) * inv_t, e_y = exp(D), total = r.sum + e_y;
+  const double D = ((double)z - (double)r.top) * inv_t, e_y = exp(D), sum = r.sum + (double)r.ones, total = sum + e_y;
   f.defined = total > 0.0 && total < INFINITY;
   f.share = 1.0 / total;
-  f.rest = r.sum * f.share;
+  f.rest = sum * f.share;
   f.p = e_y * f.share;
-  f.ln_total = D == 0.0 ? log1p(r.sum) : log(total);
+  // S - 1, the power of one class at the top apart: the label's, or one of those that are counted
+  const double others = D == 0.0 ? sum : ENT ? r.sum + e_y + ((double)r.ones - 1.0) : total - 1.0;
+  // log(1 + others) by the logarithm of the rounded sum and what the rounding left (Kahan); the library's log1p takes longer
+  // in one wave (4096 x 30000 bf16 107.5 us, 104.5)
+  const double w = 1.0 + others;
+  f.ln_total = w == 1.0 ? others : log(w) * (others / (w - 1.0));
   f.logp = f.defined ? D - f.ln_total : NAN;
   f.entropy = 0.0;
   if (ENT) {
@@ -527,13 +551,14 @@ __device__ __forceinline__ void part_sums(const Row<BF16>& r, int p, int per, co
 // A row's sums from its parts', in every lane of a wave.
 template <bool ENT>
 __device__ __forceinline__ Sums join_parts(const Sums* parts, int n, const Scale& s) {
-  Sums a{0.0, 0.0, kLeast};
+  Sums a{0.0, 0.0, kLeast, 0.f};
   for (int p = threadIdx.x & 63; p < n; p += 64) {
     const float top = fmaxf(a.top, parts[p].top);
     const Sums b = moved<ENT>(parts[p], top, s.s);
     a = moved<ENT>(a, top, s.s);
     a.sum += b.sum;
     a.moment += b.moment;
+    a.ones += b.ones;
   }
   return join_any<64, ENT>(a, s);
 }
@@ -815,7 +840,7 @@ hipError_t launch_loss_parts(const TokenLossArgs& a, hipStream_t s) {
 
 // Short rows share a wave, up to 256 chunks stay in registers; of longer ones a part does, so that more rows run at once, and
 // the rest is read again from a cache.  What bounds all of these is how many bytes are on their way, so registers are given
-// to the threads up to 8 or 6 waves a SIMD (OCC).  In us, taken and otherwise (threads a row x chunks held in each):
+// to the threads up to 8, 6 or 5 waves a SIMD (OCC).  In us, taken and otherwise (threads a row x chunks held in each):
 //   40000 x 1000 bf16, 125 chunks     with entropy 16 x 8 46.9, 32 x 4 53.7, 32 x 8 56.3; without 32 x 4 41.5, 16 x 8 49.0
 //   40000 x 3200 bf16, 400 chunks     64 x 8 112, 128 x 4 114, 128 x 8 (all) 141; of 4096 rows 128 x 4 17.7, 64 x 8 18.4
 //   40000 x 8000 bf16, 1000 chunks    128 x 4 226, 64 x 8 239, 128 x 8 (all) 231
@@ -836,10 +861,10 @@ hipError_t launch_loss_by_length(const TokenLossArgs& args, hipStream_t s) {
   if (chunks <= 8 * 4) return launch_loss_rows<BF16, POLICY, ENT, 8, 4, 32, false>(a, s);
   if (chunks <= 16 * 4) return launch_loss_rows<BF16, POLICY, ENT, 16, 4, 16, false>(a, s);
   if (chunks <= 16 * 8) {
-    if constexpr (ENT) return launch_loss_rows<BF16, POLICY, ENT, 16, 8, 16, false, 6>(a, s);
+    if constexpr (ENT) return launch_loss_rows<BF16, POLICY, ENT, 16, 8, 16, false, 5>(a, s);
     else return launch_loss_rows<BF16, POLICY, ENT, 32, 4, 8, false, 8>(a, s);
   }
-  if (chunks <= 32 * 8) return launch_loss_rows<BF16, POLICY, ENT, 32, 8, 8, false, ENT ? 6 : 1>(a, s);
+  if (chunks <= 32 * 8) return launch_loss_rows<BF16, POLICY, ENT, 32, 8, 8, false, ENT ? 5 : 1>(a, s);
   if (chunks <= 64 * 12 && a.n >= 32 * kUnits) return launch_loss_rows<BF16, POLICY, ENT, 64, 8, 1, true, 6>(a, s);
   if (chunks <= 128 * 8) return launch_loss_rows<BF16, POLICY, ENT, 128, 4, 1, true, 8>(a, s);
   if (!a.grad && chunks <= 256 * 12) return launch_loss_rows<BF16, POLICY, ENT, 256, 0, 1, true, 8>(a, s);

@@ -105,3 +105,96 @@ def test_preference_scores_next_to_the_reference(n, C, dtype):
     scores = full(n // 2, 2)
     bd.preference_loss(z, labels, None, None, n_pairs=n // 2, ref_logp=ref, out_scores=scores, temperature=T, beta=0.5)
     exact.check(scores.double().view(-1) / 0.5 - (exact.logp - ref.double()))
+
+
+# ---------------------------------------------------------------- entropy
+
+HALF_STEP = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8}
+
+
+class ExactEntropy:
+    """H [n] and its gradient [n, C] in 64 bits with their bounds.
+
+    With weights w_c = 2^x_c off by rho_c relatively (the rule above; the maximum's x is 0, its power 1 and nothing of it is
+    lost), H = ln sum w - sum w x ln 2 / sum w moves by sum p_c rho_c |1 - ln p_c - H|, ln sum w by sum p_c rho_c.  A chunk's
+    moment is summed in fp32, at most 9 roundings of 2^-24 of what is a sum of one sign; H is rounded once.
+    dH / dz_c = - p_c (log p_c + H) / T: a factor of two fp32 terms of the size of log p_c and H, and p_c with rho_c."""
+
+    def __init__(self, z, t):
+        x = z.double() / t
+        top = x.amax(1, keepdim=True)
+        e = torch.exp(x - top)
+        is_top = torch.zeros_like(x, dtype=torch.bool).scatter_(1, x.argmax(1, keepdim=True), True)
+        rest = e.masked_fill(is_top, 0).sum(1, keepdim=True)
+        log_p = (x - top) - torch.log1p(rest)
+        p = log_p.exp()
+        finite = torch.where(p > 0, log_p, 0)
+        self.H = -(p * finite).sum(1)
+        below = torch.where(p > 0, top - x, 0)
+        rho = (2.0 ** -23 * (4.5 + below)).masked_fill(is_top, 0)
+        lost = p * rho
+        H = self.H[:, None]
+        self.d_H = (lost * (1 + finite.abs() + H)).sum(1) + 9 * 2.0 ** -24 * (p * below).sum(1) + 2.0 ** -23 * self.H
+        self.grad = torch.where(p > 0, -p * (finite + H), 0) / t
+        shift = (self.d_H + lost.sum(1))[:, None]
+        self.d_grad = p * ((rho + 2.0 ** -22) * (finite.abs() + H) + shift) / t
+
+    def check(self, H, grad, dtype):
+        assert (H >= 0).all()
+        off = (H.double() - self.H).abs()
+        assert (off <= self.d_H).all(), ((off / self.d_H).max(), self.H[(off / self.d_H).argmax()])
+        off = (grad.double() - self.grad).abs()
+        limit = self.d_grad * 1.01 + self.grad.abs() * HALF_STEP[dtype] + 1e-37
+        assert (off <= limit).all(), ((off / limit).max(), (off / limit).argmax())
+
+
+def check_entropy(z, labels, t, dtype):
+    n = z.shape[0]
+    exact = ExactEntropy(z, t)
+    one = torch.ones(n, device=DEV)
+    H, grad = full(n), torch.empty_like(z)
+    bd.token_logp(z, labels, None, H, grad, None, one, temperature=t)
+    exact.check(H, grad, dtype)
+    bd.token_logp(z, labels, None, H, temperature=t)           # without a gradient
+    exact.check(H, grad, dtype)
+    # the policy loss takes the same: - H, without an advantage
+    loss = full(n)
+    bd.policy_loss(z, labels, 0 * one, loss, grad, out_entropy=H, temperature=t, entropy_coef=-1.0)
+    exact.check(H, grad, dtype)
+    assert torch.equal(loss, H)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,C", [(64, 2), (64, 5), (64, 9), (64, 100), (48, 1000), (48, 2300), (300, 9000), (300, 30001), (600, 60000),
+                                 (8, 131071), (3, 200003)])
+def test_entropy_of_sure_rows(n, C, dtype):
+    """One class far above a bulk, with the label that class, in the bulk, the first and the last one: H does not
+    depend on it, is never negative and keeps its digits however small it is."""
+    g = torch.Generator(device=DEV).manual_seed(C)
+    base = torch.randn((n, C), device=DEV, generator=g)
+    at = torch.randint(0, C, (n,), device=DEV, generator=g)
+    at[0], at[-1] = 0, C - 1
+    for gap in (6.0, 10.0, 14.0, 18.0, 22.0, 26.0, 28.0, 40.0):
+        z = base.scatter(1, at[:, None], gap).to(DT[dtype])
+        for labels in (at, torch.randint(0, C, (n,), device=DEV, generator=g), 0 * at, 0 * at + C - 1):
+            check_entropy(z, labels.int(), 1.0, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,C", KINDS)
+def test_entropy(n, C, dtype):
+    n = min(n, 150_000_000 // (C * 8) + 1) if n < 600 else n // 4
+    z, labels = rows_of(n, C, dtype, 6.0, n + C + 3)
+    check_entropy(z, labels, T, dtype)
+    check_entropy(torch.zeros_like(z) + z[:, :1], labels, T, dtype)      # classes that are all alike
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_entropy_of_many_sure_rows(dtype):
+    """Enough rows of each length that none goes in parts."""
+    for n, C in ((9000, 700), (9000, 2000), (600, 5000), (600, 12000), (600, 30000), (800, 30001)):
+        g = torch.Generator(device=DEV).manual_seed(C)
+        z = torch.randn((n, C), device=DEV, generator=g)
+        at = torch.randint(0, C, (n, 1), device=DEV, generator=g)
+        z = z.scatter_(1, at, 6 + 30 * torch.rand((n, 1), device=DEV, generator=g)).to(DT[dtype])
+        check_entropy(z, torch.randint(0, C, (n,), device=DEV, generator=g).int(), 1.0, dtype)

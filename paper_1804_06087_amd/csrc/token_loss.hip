@@ -357,7 +357,8 @@ __device__ __forceinline__ RowGrad finish_row(const TokenLossArgs& a, int row, c
     double loss = 0.0, kl = 0.0, slope = 0.0;
     const double A = a.advantage[row];
     if (A != 0.0) {
-      const double ratio = a.old_logp ? (double)(float)exp(f.logp - (double)a.old_logp[row]) : f.logp == f.logp ? 1.0 : f.logp;
+      double ratio = a.old_logp ? exp(f.logp - (double)a.old_logp[row]) : f.logp == f.logp ? 1.0 : f.logp;
+      if ((float)ratio == INFINITY) ratio = INFINITY;
       const double kept = fmin(fmax(ratio, 1.0 - a.clip_low), 1.0 + a.clip_high);
       const double plain = ratio * A, cut = kept * A;
       loss = plain != plain ? plain : -fmin(plain, cut);

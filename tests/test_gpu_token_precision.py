@@ -198,3 +198,24 @@ def test_entropy_of_many_sure_rows(dtype):
         at = torch.randint(0, C, (n, 1), device=DEV, generator=g)
         z = z.scatter_(1, at, 6 + 30 * torch.rand((n, 1), device=DEV, generator=g)).to(DT[dtype])
         check_entropy(z, torch.randint(0, C, (n,), device=DEV, generator=g).int(), 1.0, dtype)
+
+
+# ---------------------------------------------------------------- ratio
+
+def test_ratio_next_to_the_clip():
+    """Rows of C equal classes: log p = - ln C to 1e-15, and old that rounded to fp32, so that r - 1 is up to 1e-7.  With a clip
+    on either side of it, r is clipped, and the gradient 0, or it is not."""
+    for C in range(2, 60):
+        logp = -math.log(C)
+        old = np.float32(logp)
+        step = math.expm1(logp - float(old))
+        if abs(step) < 1e-9:
+            continue
+        z = torch.zeros((2, C), device=DEV)
+        labels = torch.tensor([0, C - 1], dtype=torch.int32, device=DEV)
+        A = torch.full((2,), math.copysign(1.0, step), device=DEV)
+        for width, clipped in ((abs(step) / 2, True), (abs(step) * 2, False)):
+            loss, grad = full(2), torch.empty_like(z)
+            bd.policy_loss(z, labels, A, loss, grad, old_logp=torch.full((2,), float(old), device=DEV), clip_low=width,
+                           clip_high=width)
+            assert (grad == 0).all() if clipped else (grad != 0).all(), (C, step, width)

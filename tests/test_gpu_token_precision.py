@@ -219,3 +219,21 @@ def test_ratio_next_to_the_clip():
             bd.policy_loss(z, labels, A, loss, grad, old_logp=torch.full((2,), float(old), device=DEV), clip_low=width,
                            clip_high=width)
             assert (grad == 0).all() if clipped else (grad != 0).all(), (C, step, width)
+
+
+# ---------------------------------------------------------------- more rows than a launch takes
+
+@pytest.mark.parametrize("n,C,dtype", [((1 << 20) + 5, 1100, "fp32"), ((1 << 20) + 5, 9001, "bf16"), ((1 << 25) + 37, 3, "fp32")])
+def test_rows_of_a_second_launch(n, C, dtype):
+    """A launch takes 2^20 workgroups: of one row each, or of 32 short ones.  All rows are one row of logits."""
+    g = torch.Generator(device=DEV).manual_seed(C)
+    z = (3 * torch.randn((1, C), device=DEV, generator=g)).to(DT[dtype])
+    log_p = torch.log_softmax(z[0].double(), 0)
+    H = -(log_p.exp() * log_p).sum()
+    labels = torch.randint(-1, C, (n,), dtype=torch.int32, device=DEV, generator=g)
+    logp, entropy = full(n), full(n)
+    bd.token_logp(z.expand(n, C), labels, logp, entropy)
+    want = torch.where(labels >= 0, log_p[labels.clamp(min=0).long()], 0)
+    # the rule above with powers down to e^-40, and the results' own rounding, 2^-24 of 40
+    assert (logp.double() - want).abs().max() <= 2.0 ** -23 * (4.5 + 40) + 2.0 ** -24 * 40
+    assert (entropy.double() - torch.where(labels >= 0, H, 0)).abs().max() <= 2.0 ** -23 * (4.5 + 40) * (2 + H) * 2

@@ -113,7 +113,8 @@ int rafiki_distill_loss(const void* logits, int dtype, long long ld_row, int n, 
  *     out_entropy[i] = H = - sum_c p_c log p_c           (a term with p = 0 is 0),
  *     dz_c = 1/T [ a_i (1[c = y] - p_c) - h_i p_c (log p_c + H) ]
  * with a = grad_logp = dL / d logp and h = grad_entropy = dL / dH (fp32 [n]; null: 0; grad_logits
- * needs one of them).  A row with a_i = h_i = 0 has gradient 0 whatever it holds.  A masked label
+ * needs one of them); here and below grad_logits shares no element with the logits, which are read again for it (the
+ * binding refuses such a call).  A row with a_i = h_i = 0 has gradient 0 whatever it holds.  A masked label
  * (logit -inf) has log p = -inf, as has a log p beyond fp32; NaN, +inf or a row of only -inf gives NaN
  * in all outputs of the row.  Any output may be null, not all.  fp32 arithmetic; log p is exact to fp32 also
  * where p is near 1; each gradient is rounded once.  Scalars are 64 bits here, since what follows subtracts and sums

@@ -645,16 +645,39 @@ def distill_loss(logits, teacher_labels, teacher_logp, out_loss=None, grad_logit
           _ptr(grad_logits), ld_grad)
 
 
-def _grad_rows(grad_logits, logits):
-    """Distance between the rows of a gradient of the logits (0 for None)."""
+def _rows_overlap(p: int, ld_p: int, q: int, ld_q: int, n: int, width: int) -> bool:
+    """Whether two matrices of n rows of ``width`` bytes, ld bytes apart, at addresses p and q share a byte."""
+    if not n or p + (n - 1) * ld_p + width <= q or q + (n - 1) * ld_q + width <= p:
+        return False
+    if n == 1 or ld_p == ld_q == 0:
+        return True
+    if ld_p == ld_q:                                         # rows between each other's
+        between = (q - p) % ld_p
+        return between < width or between > ld_p - width
+    import numpy as np
+    if ld_p < ld_q:
+        p, ld_p, q, ld_q = q, ld_q, p, ld_p
+    for first in range(0, n, 1 << 20):                       # each row of q against the rows of p next to it
+        at = q - p + ld_q * np.arange(first, min(n, first + (1 << 20)), dtype=np.int64)
+        below = np.clip(at // ld_p, 0, n - 1)
+        above = np.minimum(below + 1, n - 1)
+        if any((np.abs(at - i * ld_p) < width).any() for i in (below, above)):
+            return True
+    return False
+
+
+def _grad_rows(grad_logits, logits, ld_row):
+    """Distance between the rows of a gradient of the logits (0 for None), which shares no element with them."""
     if grad_logits is None:
         return 0
     if grad_logits.shape != logits.shape or grad_logits.dtype != logits.dtype:
         raise ValueError("grad_logits: expected the shape and dtype of the logits")
-    if grad_logits.data_ptr() == logits.data_ptr():
-        raise ValueError("grad_logits: the logits are read again for it")
     _same_device(logits, grad_logits)
-    return _rows(grad_logits, "grad_logits")
+    ld = _rows(grad_logits, "grad_logits")
+    item, (n, c) = logits.element_size(), logits.shape
+    if _rows_overlap(logits.data_ptr(), ld_row * item, grad_logits.data_ptr(), ld * item, n, c * item):
+        raise ValueError("grad_logits: the logits are read again for it")
+    return ld
 
 
 @functools.lru_cache(maxsize=4096)
@@ -672,7 +695,8 @@ def token_logp(logits, labels, out_logp=None, out_entropy=None, grad_logits=None
     are grad_logp and grad_entropy fp32 [n] (None: 0).  Any output may be None."""
     import torch
     code = _dtype_code(logits, "logits")
-    ld_row, ld_grad = _rows(logits, "logits"), _grad_rows(grad_logits, logits)
+    ld_row = _rows(logits, "logits")
+    ld_grad = _grad_rows(grad_logits, logits, ld_row)
     n, nc = logits.shape
     f32, dev = torch.float32, logits.device
     if labels is None:
@@ -692,7 +716,8 @@ def policy_loss(logits, labels, advantage, out_loss=None, grad_logits=None, old_
     None: no KL term) fp32 [n]; in grad_logits its gradient times grad_loss [n] (None: 1).  Any output may be None."""
     import torch
     code = _dtype_code(logits, "logits")
-    ld_row, ld_grad = _rows(logits, "logits"), _grad_rows(grad_logits, logits)
+    ld_row = _rows(logits, "logits")
+    ld_grad = _grad_rows(grad_logits, logits, ld_row)
     n, nc = logits.shape
     if labels is None or advantage is None:
         raise ValueError("labels and advantage are required")
@@ -722,7 +747,8 @@ def preference_loss(logits, labels, out_loss=None, grad_logits=None, offsets=Non
     (None: 1); out_scores fp32 [pairs, 2].  Any output may be None."""
     import torch
     code = _dtype_code(logits, "logits")
-    ld_row, ld_grad = _rows(logits, "logits"), _grad_rows(grad_logits, logits)
+    ld_row = _rows(logits, "logits")
+    ld_grad = _grad_rows(grad_logits, logits, ld_row)
     n, nc = logits.shape
     f32, dev = torch.float32, logits.device
     if labels is None:

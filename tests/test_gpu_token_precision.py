@@ -237,3 +237,26 @@ def test_rows_of_a_second_launch(n, C, dtype):
     # the rule above with powers down to e^-40, and the results' own rounding, 2^-24 of 40
     assert (logp.double() - want).abs().max() <= 2.0 ** -23 * (4.5 + 40) + 2.0 ** -24 * 40
     assert (entropy.double() - torch.where(labels >= 0, H, 0)).abs().max() <= 2.0 ** -23 * (4.5 + 40) * (2 + H) * 2
+
+
+# ---------------------------------------------------------------- gradients beside the logits
+
+def test_gradient_over_the_logits_is_refused():
+    """Rows of the gradient that share elements with rows of the logits: refused, however they meet; rows that lie between
+    them are written."""
+    n, C = 6, 40
+    buf = torch.randn(4 * n * 100, device=DEV)
+    at = lambda first, ld: buf.as_strided((n, C), (ld, 1), first)  # noqa: E731
+    labels, f = torch.arange(n, dtype=torch.int32, device=DEV), torch.ones(n, device=DEV)
+    for z, grad in ((at(0, 40), at(40, 40)), (at(40, 40), at(0, 40)), (at(0, 100), at(39, 100)), (at(0, 100), at(61, 100)),
+                    (at(0, 100), at(500, 40)), (at(500, 40), at(0, 100)), (at(0, 0), at(39, 40)), (at(500, 17), at(0, 100))):
+        for call in (lambda: bd.token_logp(z, labels, None, None, grad, f), lambda: bd.policy_loss(z, labels, f, None, grad),
+                     lambda: bd.preference_loss(z, labels, None, grad, n_pairs=3)):
+            with pytest.raises(ValueError, match="read again"):
+                call()
+    for z, grad in ((at(0, 100), at(40, 100)), (at(60, 100), at(0, 100)), (at(0, 40), at(240, 40)), (at(0, 0), at(40, 40)),
+                    (at(0, 200), at(50, 400)), (at(0, 400), at(50, 200))):
+        apart = torch.empty((n, C), device=DEV)
+        bd.token_logp(z, labels, None, None, apart, f)
+        bd.token_logp(z, labels, None, None, grad, f)
+        assert torch.equal(grad, apart)

@@ -236,8 +236,11 @@ __device__ __forceinline__ Sums moved(const Sums& v, float top, double s) {
   return Sums{sum * grown, ENT ? (v.moment + sum * step) * grown : 0.0, top, 0.f};
 }
 // A row's sums in W neighbouring lanes, which have the same `top`: the largest logit so far.
-template <int BF16, int W, bool ENT>
+// FINE (without entropy): the few chunks of a likely class are added in 64 bits throughout.  Beside it unlikely classes lose more
+// than they gain by rounding: log p of bf16 rows of 30000 is 2.5e-8 above its value on average, 1.2e-8 with FINE.
+template <int BF16, int W, bool ENT, bool FINE>
 struct RowSums {
+  static_assert(!(ENT && FINE), "without entropy");
   static constexpr int V = Row<BF16>::V;
   Sums a;
   Exponent<BF16> x;
@@ -264,6 +267,15 @@ struct RowSums {
       if constexpr (ENT) m = fmaf(e[j], finite_log2(t), m);
     }
     float sum = tree_sum<V>(e);
+    if constexpr (FINE) {
+      if (__any(sum >= 0.25f)) {
+        double all[2] = {(double)e[0], (double)e[1]};
+#pragma unroll
+        for (int j = 2; j < V; ++j) all[j & 1] += (double)e[j];
+        a.sum += all[0] + all[1];
+        return;
+      }
+    }
     if constexpr (ENT) {
       a.moment += (double)m;
       asm volatile("" : "+v"(a.moment));                     // or the compiler sinks it behind the branches, with all of its terms
@@ -498,7 +510,7 @@ __global__ __launch_bounds__(NT * G, OCC) void token_loss_kernel(TokenLossArgs a
           r, NT * CH, r.chunks, [&](float* z, int i) { f(z, i, std::false_type{}); });
     }
   };
-  RowSums<BF16, W, ENT> sum;
+  RowSums<BF16, W, ENT, false> sum;
   float top = fmaxf(z_label, kLeast);
   if constexpr (CH > 0) {
 #pragma unroll
@@ -535,9 +547,9 @@ __global__ __launch_bounds__(NT * G, OCC) void token_loss_kernel(TokenLossArgs a
 // ---------------------------------------------------------------- rows in parts
 
 // The sums over a row's chunks begin .. last - 1, joined over NT threads.
-template <int BF16, bool ENT, int NT>
+template <int BF16, bool ENT, bool FINE, int NT>
 __device__ __forceinline__ Sums row_sums(const Row<BF16>& r, int begin, int last, float z_label, const Scale& s, Sums* waves) {
-  RowSums<BF16, (NT < 64 ? NT : 64), ENT> sum;
+  RowSums<BF16, (NT < 64 ? NT : 64), ENT, FINE> sum;
   sum.start(fmaxf(z_label, kLeast), s);
   for_chunks<BF16, false, 4, NT>(r, begin, last, [&](const float* z, int) { sum.add_any(z, s); });
   return join<NT, ENT>(sum.a, s, waves);
@@ -546,7 +558,7 @@ __device__ __forceinline__ Sums row_sums(const Row<BF16>& r, int begin, int last
 template <int BF16, bool ENT, int NT>
 __device__ __forceinline__ void part_sums(const Row<BF16>& r, int p, int per, const Scale& s, Sums* out) {
   __shared__ Sums waves[NT / 64];
-  const Sums sums = row_sums<BF16, ENT, NT>(r, p * per, min(r.chunks, (p + 1) * per), r.at(r.label), s, waves);
+  const Sums sums = row_sums<BF16, ENT, false, NT>(r, p * per, min(r.chunks, (p + 1) * per), r.at(r.label), s, waves);
   if (threadIdx.x == 0) *out = sums;
 }
 // A row's sums from its parts', in every lane of a wave.
@@ -629,7 +641,7 @@ __global__ __launch_bounds__(NT * G) void preference_sums_kernel(PreferenceArgs 
     if ((unsigned)label >= (unsigned)a.C) continue;
     Row<BF16> r;
     r.init(a.logits, row * a.ld_row, a.C, label);
-    const Sums sums = row_sums<BF16, false, NT>(r, p * a.per_part, min(r.chunks, (p + 1) * a.per_part), r.at(label), a.s, waves);
+    const Sums sums = row_sums<BF16, false, true, NT>(r, p * a.per_part, min(r.chunks, (p + 1) * a.per_part), r.at(label), a.s, waves);
     if (tid == 0) ((Sums*)a.parts)[(long long)row * a.n_parts + p] = sums;
     if (NT > 64) __syncthreads();
   }
@@ -739,7 +751,7 @@ __global__ __launch_bounds__(1024) void preference_few_kernel(PreferenceArgs a) 
     r.init(a.logits, row * a.ld_row, a.C, a.labels[row]);
     if ((unsigned)r.label >= (unsigned)a.C) continue;
     const float z_label = r.at(r.label);
-    const Sums all = row_sums<BF16, false, 64>(r, 0, r.chunks, z_label, a.s, nullptr);
+    const Sums all = row_sums<BF16, false, true, 64>(r, 0, r.chunks, z_label, a.s, nullptr);
     const RowFacts f = row_facts<false>(all, z_label, a.inv_t);
     if (lane == 0) a.rows[row] = preference_row(all, f);
     const double delta = f.logp - (a.ref_logp ? (double)a.ref_logp[row] : 0.0);

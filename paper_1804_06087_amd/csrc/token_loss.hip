@@ -224,16 +224,20 @@ __device__ __forceinline__ float chunk_max(const float v[V]) {
   for (int j = 1; j < V; j += 2) top = max3(top, v[j], v[j + 1 < V ? j + 1 : j]);
   return top;
 }
-// The same sums relative to `top`, at least their own.  The step's power keeps what is rounded off its exponent.
+// 2^step, step <= 0, with what is rounded off the exponent.
+__device__ __forceinline__ double grown(double step) {
+  const float x = (float)step;
+  return (double)power2(x) * (1.0 + 0.6931471805599453 * (step - (double)x));
+}
+__device__ __forceinline__ double step_between(float from, float to, double s) { return fmax(((double)from - (double)to) * s, -16384.0); }
+// The same sums relative to `top`, at least their own.
 template <bool ENT>
 __device__ __forceinline__ Sums moved(const Sums& v, float top, double s) {
   if (top == v.top) return v;
   const double sum = v.sum + (ENT ? (double)v.ones : 0.0);
   if (sum == 0.0) return Sums{0.0, 0.0, top, 0.f};
-  const double step = fmax(((double)v.top - (double)top) * s, -16384.0);
-  const float x = (float)step;
-  const double grown = (double)power2(x) * (1.0 + 0.6931471805599453 * (step - (double)x));
-  return Sums{sum * grown, ENT ? (v.moment + sum * step) * grown : 0.0, top, 0.f};
+  const double step = step_between(v.top, top, s), factor = grown(step);
+  return Sums{sum * factor, ENT ? (v.moment + sum * step) * factor : 0.0, top, 0.f};
 }
 // A row's sums in W neighbouring lanes, which have the same `top`: the largest logit so far.
 // FINE (without entropy): the few chunks of a likely class are added in 64 bits throughout.  Beside it unlikely classes lose more
@@ -711,7 +715,7 @@ __global__ __launch_bounds__(1024) void preference_pairs_kernel(PreferenceArgs a
       for (int q = 1; q < a.n_parts; ++q) all.top = fmaxf(all.top, parts[q].top);
       all.sum = 0.0;
 #pragma unroll 8
-      for (int q = 0; q < a.n_parts; ++q) all.sum += moved<false>(parts[q], all.top, a.s.s).sum;
+      for (int q = 0; q < a.n_parts; ++q) all.sum += parts[q].sum * grown(step_between(parts[q].top, all.top, a.s.s));
     }
     const RowFacts f = row_facts<false>(all, z, a.inv_t);
     a.rows[row] = preference_row(all, f);

@@ -906,17 +906,21 @@ hipError_t launch_loss_parts(const TokenLossArgs& a, hipStream_t s) {
 
 // Short rows share a wave, up to 256 chunks stay in registers; of longer ones a part does, so that more rows run at once, and
 // the rest is read again from a cache.  What bounds all of these is how many bytes are on their way, so registers are given
-// to the threads up to 8, 6 or 5 waves a SIMD (OCC).  In us, taken and otherwise (threads a row x chunks held in each):
-//   40000 x 1000 bf16, 125 chunks     with entropy 16 x 8 46.9, 32 x 4 53.7, 32 x 8 56.3; without 32 x 4 41.5, 16 x 8 49.0
-//   40000 x 3200 bf16, 400 chunks     64 x 8 112, 128 x 4 114, 128 x 8 (all) 141; of 4096 rows 128 x 4 17.7, 64 x 8 18.4
-//   40000 x 8000 bf16, 1000 chunks    128 x 4 226, 64 x 8 239, 128 x 8 (all) 231
-//   8000 x 12000 bf16, 1500 chunks    256 x 4 83.7, 256 x 8 (all) 85.6
-//   8000 x 20000 bf16, 2500 chunks    256 x 8 128, 256 x 4 130, 512 x 4 154
-//   4096 x 30000 bf16, 3750 chunks    256 x 8 96.4, 512 x 4 95.7, 256 x 4 107
-//   4096 x 64000 bf16, 8000 chunks    512 x 6 200, 512 x 4 205, 512 x 8 in 5 waves a SIMD 215
-//   2000 x 30001 fp32, 7501 chunks    512 x 8 91.3, 512 x 6 94.7, in 5 waves a SIMD 101; 1500 x 50021 126, 128, 128
-//   900 x 30001 fp32                  512 x 3 49.2 (in 8 waves: four rows a unit at once, so all of them), 512 x 8 51.2
-// Without a gradient a row is read once: 20000 x 20000 133 us in 256 threads, 142 in 512; 4096 x 30000 52 in 512, 88 in 1024.
+// to the threads up to 8, 6 or 5 waves a SIMD (OCC); rows of one wave need no barrier and are faster up to
+// longer rows with entropy and where there is no gradient.  In us, taken and otherwise (threads a row x chunks held in each), bf16:
+//                            with entropy and gradient           without entropy             with entropy, no gradient
+//   40000 x 1000, 125 chunks   32 x 4 47.7, 16 x 8 48.1            32 x 4 42.1, 16 x 8 44.4
+//   40000 x 3200, 400          64 x 8 124, 128 x 4 143             64 x 8 116, 128 x 4 118
+//   4096 x 2600, 325           64 x 8 17.8, 128 x 4 18.4           64 x 8 15.8, 128 x 4 15.6   64 x 8 13.8, 128 x 4 14.2
+//   2000 x 5000, 625           128 x 4 15.3, 64 x 8 16.0           128 x 4 13.0, 64 x 8 14.2   128 x 4 11.3, 64 x 8 12.2
+//   16000 x 5000, 625          64 x 8 73.2, 128 x 4 79.0           128 x 4 66.9, 64 x 8 70.2   64 x 8 46.1, 128 x 4 53.4
+//   40000 x 8000, 1000         64 x 8 255, 128 x 4 271             128 x 4 236, 64 x 8 242     64 x 8 134, 128 x 4 154
+//   8000 x 12000, 1500         256 x 4 85.9, 256 x 8 88.2          256 x 4 74.8, 256 x 8 81.5
+//   8000 x 20000, 2500         256 x 8 130, 256 x 4 134, 512 x 4 148
+//   4096 x 30000, 3750         256 x 8 103.4, 512 x 4 104.9, 256 x 4 108                       256 x 0 50.4, 512 x 0 56.7
+//   4096 x 64000, 8000         512 x 6 212.6, 512 x 4 212.6, 512 x 8 in 5 waves a SIMD 237     512 x 0 (50000) 81.2, 256 x 0 78.8
+// and fp32: 2000 x 30001, 7501 chunks, 512 x 8 91.3, 512 x 6 94.0; 900 x 30001 512 x 3 49.1 (in 8 waves: four rows a unit at
+// once, so all of them), 512 x 8 50.4; 4096 x 30000 without a gradient 512 x 0 86.0, 256 x 0 88.8.
 template <int BF16, bool POLICY, bool ENT>
 hipError_t launch_loss_by_length(const TokenLossArgs& args, hipStream_t s) {
   TokenLossArgs a = args;
@@ -926,14 +930,12 @@ hipError_t launch_loss_by_length(const TokenLossArgs& args, hipStream_t s) {
   if (a.n_parts > 1) return launch_loss_parts<BF16, POLICY, ENT>(a, s);
   if (chunks <= 8 * 4) return launch_loss_rows<BF16, POLICY, ENT, 8, 4, 32, false>(a, s);
   if (chunks <= 16 * 4) return launch_loss_rows<BF16, POLICY, ENT, 16, 4, 16, false>(a, s);
-  if (chunks <= 16 * 8) {
-    if constexpr (ENT) return launch_loss_rows<BF16, POLICY, ENT, 16, 8, 16, false, 5>(a, s);
-    else return launch_loss_rows<BF16, POLICY, ENT, 32, 4, 8, false, 8>(a, s);
-  }
+  if (chunks <= 32 * 4) return launch_loss_rows<BF16, POLICY, ENT, 32, 4, 8, false, 8>(a, s);
   if (chunks <= 32 * 8) return launch_loss_rows<BF16, POLICY, ENT, 32, 8, 8, false, ENT ? 5 : 1>(a, s);
-  if (chunks <= 64 * 12 && a.n >= 32 * kUnits) return launch_loss_rows<BF16, POLICY, ENT, 64, 8, 1, true, 6>(a, s);
+  if (chunks <= (ENT || !a.grad ? 64 * 16 : 64 * 7) && a.n >= 16 * kUnits)
+    return launch_loss_rows<BF16, POLICY, ENT, 64, 8, 1, true, 6>(a, s);
   if (chunks <= 128 * 8) return launch_loss_rows<BF16, POLICY, ENT, 128, 4, 1, true, 8>(a, s);
-  if (!a.grad && chunks <= 256 * 12) return launch_loss_rows<BF16, POLICY, ENT, 256, 0, 1, true, 8>(a, s);
+  if (!a.grad && chunks <= 256 * 16) return launch_loss_rows<BF16, POLICY, ENT, 256, 0, 1, true, 8>(a, s);
   if (!a.grad) return launch_loss_rows<BF16, POLICY, ENT, 512, 0, 1, true>(a, s);
   if (chunks <= 256 * 8) return launch_loss_rows<BF16, POLICY, ENT, 256, 4, 1, true, 8>(a, s);
   if (chunks <= 256 * 16) return launch_loss_rows<BF16, POLICY, ENT, 256, 8, 1, true, 6>(a, s);

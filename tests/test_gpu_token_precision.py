@@ -260,3 +260,22 @@ def test_gradient_over_the_logits_is_refused():
         bd.token_logp(z, labels, None, None, apart, f)
         bd.token_logp(z, labels, None, None, grad, f)
         assert torch.equal(grad, apart)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,chunks", [(4100, 129), (4100, 257), (4100, 448), (4100, 449), (4100, 1024), (4100, 1025), (4090, 1024), (600, 4095)])
+def test_rows_at_the_borders_of_their_length(n, chunks, dtype):
+    """Both sides of the numbers of rows and of 16-byte chunks at which a row takes other threads: every value by its bound."""
+    V = 8 if dtype == "bf16" else 4
+    for C in (chunks * V, chunks * V - 3):
+        z, labels = rows_of(n, C, dtype, 4.0, n + C + 4)
+        exact = Exact(z, labels)
+        ref = (exact.logp + 0.02).float()
+        d = ref.double() - exact.logp
+        for ent in (0.0, 0.01):
+            for grad in (True, False):
+                kl = full(n)
+                bd.policy_loss(z, labels, torch.ones(n, device=DEV), None, torch.empty_like(z) if grad else None, ref_logp=ref,
+                               out_kl=kl, temperature=T, entropy_coef=ent)
+                exact.check((torch.expm1(d) - d - kl.double()) / torch.expm1(d))
+        check_entropy(z, labels, T, dtype)

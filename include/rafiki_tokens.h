@@ -116,9 +116,12 @@ int rafiki_distill_loss(const void* logits, int dtype, long long ld_row, int n, 
  * needs one of them); here and below grad_logits shares no element with the logits, which are read again for it (the
  * binding refuses such a call).  A row with a_i = h_i = 0 has gradient 0 whatever it holds.  A masked label
  * (logit -inf) has log p = -inf, as has a log p beyond fp32; NaN, +inf or a row of only -inf gives NaN
- * in all outputs of the row.  Any output may be null, not all.  fp32 arithmetic; log p is exact to fp32 also
- * where p is near 1; each gradient is rounded once.  Scalars are 64 bits here, since what follows subtracts and sums
- * log-probabilities.  2^-20 <= T <= 2^20, 1 <= n <= 2^30. */
+ * in all outputs of the row.  Any output may be null, not all.  Powers of classes are fp32, their sums and what is made of
+ * them 64 bits, since what follows subtracts and sums log-probabilities; each output and each gradient is rounded once.
+ * Before that log p is off by 3e-8 rms, nearly as often up as down (a power is off by at most 2^-23 (4.5 + d), d its distance
+ * below the likeliest class in units of log p, and log p by their mean under p), and relatively where p is near 1.  H is not
+ * negative and is off by a few times that relatively, however small it is and whatever the label.  2^-20 <= T <= 2^20,
+ * 1 <= n <= 2^30. */
 int rafiki_token_logp(const void* logits, int dtype, long long ld_row, int n, int n_classes, const int32_t* labels,
                       double temperature, const float* grad_logp, const float* grad_entropy, float* out_logp,
                       float* out_entropy, void* grad_logits, long long ld_grad, void* workspace,
@@ -150,7 +153,7 @@ int rafiki_policy_loss(const void* logits, int dtype, long long ld_row, int n, i
 /* Preference loss over n_pairs pairs of answers with its gradient.  The rows of pair p's chosen answer are
  * offsets[2 p] .. offsets[2 p + 1] - 1, those of its rejected one offsets[2 p + 1] .. offsets[2 p + 2] - 1
  * (int32 [2 n_pairs + 1], not decreasing, within [0, n]; null: 2 n_pairs answers of n / (2 n_pairs)
- * rows each, which then divides).  Labels, T and log p as above; rows without a token count for nothing.  With
+ * rows each, which then divides).  Answers in another order are brought into this one first.  Labels, T and log p as above; rows without a token count for nothing.  With
  * ref_logp the reference's log p (fp32 [n]; null: 0) and the sums over an answer's tokens (mean != 0: divided by their
  * number, an answer without tokens has score 0):
  *     score  = beta sum (log p - ref),        u = score of the chosen - score of the rejected,

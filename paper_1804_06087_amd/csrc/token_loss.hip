@@ -9,10 +9,10 @@
 //
 // Bound by bytes: logits read once and the gradient written once, where the factors f are the row's own; a preference loss
 // has them from all rows of a pair and reads the logits twice.  Measured on an MI355X (a device copy moves 4.8 TB/s): 8192 x
-// 131072 bf16 log p and entropy 316 us (5.9 TB/s of what has a token), 4096 x 30000 bf16 policy loss with entropy and
-// gradient 102 us (4.5 TB/s; with a maximum that the sums follow 133), 1500 x 50021 fp32 125 us (4.5), 3 pairs of 2 x 880 rows
-// of 131071 bf16 738 us, of which the sums take 219 (5.5 TB/s; 273 with the exponents of fp32 rows) and the
-// gradient 516 (5.1 TB/s).  Pairs in groups that a cache might hold until their gradient is taken were slower (8
+// 131072 bf16 log p and entropy 317 us (5.8 TB/s of what has a token; 11 vector instructions a class, so the clock counts too),
+// 4096 x 30000 bf16 policy loss with entropy and gradient 103 us (4.4 TB/s; with a maximum of each thread 133), 1500 x 50021
+// fp32 125 us (4.5), 3 pairs of 2 x 880 rows of 131071 bf16 740 us, of which the sums take 221 (5.4 TB/s) and the
+// gradient 520 (5.1 TB/s).  Pairs in groups that a cache might hold until their gradient is taken were slower (8
 // groups of 2 pairs of 2 x 500 x 30000 663 us, all at once 557).
 #include "tokens.h"
 
@@ -68,8 +68,8 @@ __device__ __forceinline__ u32x4 pack(const float z[V]) {
 }
 
 // f over W neighbouring lanes, in each of them, all of which call it: neighbours, pairs, fours and eights mirrored, then rows
-// of 16 and halves of the wave exchanged.  All by vector instructions: through LDS (shuffles) a row's maximum took ten times
-// as long, and rows that are only read 4 % longer (4096 x 30000 bf16).
+// of 16 and halves of the wave exchanged.  All by vector instructions: with shuffles, which go through LDS, 20000 x 20000 bf16
+// without a gradient took 138 us instead of 134.
 template <int CTRL>
 __device__ __forceinline__ uint32_t exchanged(uint32_t v) {
   return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xF, 0xF, false);

@@ -325,7 +325,7 @@ struct RowSums {
         double all[2] = {(double)e[0], (double)e[1]};
 #pragma unroll
         for (int j = 2; j < V; ++j) all[j & 1] += (double)e[j];
-        a.sum += all[0] + all[1];
+        a.sum += sum >= 0.25f ? all[0] + all[1] : (double)sum;   // by its own lane's classes, whatever row its neighbours have
         return;
       }
     }

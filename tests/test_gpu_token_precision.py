@@ -279,3 +279,27 @@ def test_rows_at_the_borders_of_their_length(n, chunks, dtype):
                                out_kl=kl, temperature=T, entropy_coef=ent)
                 exact.check((torch.expm1(d) - d - kl.double()) / torch.expm1(d))
         check_entropy(z, labels, T, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("C", [100, 900, 3000])
+def test_rows_do_not_depend_on_their_neighbours(C, dtype):
+    """Rows that share a wave: with other rows between them the even rows keep every bit of log p (through scores of one token and
+    KL estimates, which show 1e-15 and 1e-10 of it), H and the gradient."""
+    n = 4000
+    z, labels = rows_of(n, C, dtype, 3.0, C)
+    ref = Exact(z, labels).logp.float()
+    one = torch.ones(n, device=DEV)
+
+    def results(z, labels):
+        scores, loss, kl, H, grad = full(n // 2, 2), full(n), full(n), full(n), torch.empty_like(z)
+        bd.preference_loss(z, labels, None, None, n_pairs=n // 2, ref_logp=ref, out_scores=scores, temperature=T)
+        bd.policy_loss(z, labels, one, loss, grad, ref_logp=ref + 0.01, out_kl=kl, out_entropy=H, temperature=T, entropy_coef=0.1)
+        kl2 = full(n)
+        bd.policy_loss(z, labels, one, None, None, ref_logp=ref + 0.01, out_kl=kl2, temperature=T)
+        return [v.reshape(n, -1)[::2].clone() for v in (scores, loss, kl, H, grad, kl2)]
+
+    first = results(z, labels)
+    z[1::2], labels[1::2] = z[1::2].flip(0), labels[1::2].flip(0)
+    for a, b in zip(first, results(z, labels)):
+        assert torch.equal(a, b)
